@@ -122,7 +122,7 @@ int lfps_create(const lfps_config* cfg, lfps_ctx** out);
 int lfps_destroy(lfps_ctx* ctx);
 /* Text of the last error on this context (host string owned by the context; "" if none).
  * With ctx == NULL: text of the last failure of a call that takes no context (lfps_create,
- * lfps_workspace_bytes, lfps_sparse_attn_noalloc) in this thread. */
+ * lfps_workspace_bytes, lfps_sparse_attn_noalloc, lfps_pages_workspace_bytes) in this thread. */
 const char* lfps_last_error(const lfps_ctx* ctx);
 /* Device bytes lfps_create will allocate for this config (host out-pointer). */
 int lfps_workspace_bytes(const lfps_config* cfg, int64_t* out);
@@ -270,6 +270,76 @@ int lfps_table_step_gated(lfps_ctx* ctx, const float* q, const lfps_kv* kv, cons
                           const float* vbar, const float* sigma2_hat, int32_t n_local, float eps, int32_t* topk_idx,
                           float* topk_score, float* out, int32_t* gate_out, void* stream);
 
+/* ---- Prompts, forks and pages: what brings rows into a cache and shares them ---------------------------------
+ * Packed tokens: the new tokens of all requests lie one behind the other in the token arrays; those of request b are
+ * cu[b] <= t < cu[b+1] (cu: [B+1] int32, rising), and they are the request's newest: token cu[b] + i is row
+ * n_b - (cu[b+1] - cu[b]) + i of its cache, n_b (seq_lens) with the new rows counted in.  A request may have none.  Tokens
+ * of no request (in front of cu[0], from cu[B] on) are neither read nor written; a request with more new tokens than rows
+ * has its first ones at no row.  n_tokens bounds the arrays: entries of cu are clamped to it. */
+
+/* The newest K and V rows into the cache: k_new, v_new [n_tokens, Hkv, D] of cfg.kv_dtype, element (t, g, c) at
+ * t*stride_t + g*D + c (slices of a fused projection; rows 16-byte aligned, stride_t >= Hkv*D).  The cache behind kv is
+ * WRITTEN, at the rows named above and nowhere else; tokens at no row are dropped.  FP8 caches: rounded to nearest even,
+ * values beyond +-448 and infinities become +-448, NaN stays NaN.  Two requests whose tables name the same block for a row
+ * that both append leave either's (lfps_pages_update gives each its own). */
+int lfps_append(lfps_ctx* ctx, const void* k_new, const void* v_new, int64_t stride_t, const int32_t* cu,
+                int32_t n_tokens, const lfps_kv* kv, void* stream);
+
+/* Causal attention of the new tokens over the cache, their own rows in it included (append first): the token at row p of
+ * request b attends rows 0 ... p:  out[t,h] = sum_j softmax_j(q[t,h].K[b,g(h),j]/sqrt(D)) V[b,g(h),j],  j <= p.  One call takes
+ * whole prompts (n_b tokens), chunks behind rows that are there already, drafted tokens and single ones, mixed.
+ *   q    [n_tokens, Hq, D] of cfg.kv_dtype (bf16 beside FP8 caches), element (t, h, c) at t*stride_t + h*D + c (rows 16-byte
+ *        aligned, stride_t >= Hq*D)
+ *   out  [n_tokens, Hq, D] of the same type, contiguous, 16-byte aligned; must not overlap q.  A token at no row gets zeros, rows
+ *        of tokens of no request are left as they were.
+ * Products and sums are fp32; 16-bit types round the weights to 16 bits for the product with V.  n_tokens * Hq <= 2^27. */
+int lfps_prompt_attn(lfps_ctx* ctx, const void* q, int64_t stride_t, const int32_t* cu, int32_t n_tokens,
+                     const lfps_kv* kv, void* out, void* stream);
+
+/* lfps_full_attn_decode for a batch in which groups of requests share their first rows, which are then read once a group.
+ *   group_start [n_groups + 1] int32, rising: group i is the requests group_start[i] <= b < group_start[i+1]
+ *   prefix_len  [n_groups] int32, clamped to [0, n of the group's first request]: row j < prefix_len[i] of any of them is row
+ *               j of the group's first request (as far as the request has rows); what the others' own slabs or tables hold
+ *               there is not read.
+ *   q, out      [B, Hq, D] fp32.  Rows of out of requests in no group are left as they were.  1 <= n_groups <= B. */
+int lfps_prefix_attn_decode(lfps_ctx* ctx, const float* q, const lfps_kv* kv, const int32_t* group_start,
+                            const int32_t* prefix_len, int32_t n_groups, float* out, void* stream);
+
+/* Pages.  The state of a paged cache is its block table and lengths (the view's); a block is live if the table names it for a
+ * row below some n_b, or if the caller holds it for something else (held [n_blocks] int32, not 0; or NULL).  The calls below
+ * read the view's table and lengths and write new ones, which must not overlap them: swap the two, as the Top-k arrays of two
+ * steps.  They compute whole numbers only and plan the copies of rows as a list [.., 3] of (from block, to block, leading rows;
+ * -1, -1, 0: none), which lfps_pages_copy carries out in the pool of every layer that shares the table.
+ * work: lfps_pages_workspace_bytes(n_blocks) bytes of device memory, 16-byte aligned, that no other call uses meanwhile; nothing
+ * in it is kept from one call to the next.  The view must be paged; n_blocks <= 2^24. */
+int lfps_pages_workspace_bytes(int32_t n_blocks, int64_t* out);
+
+/* The next step's pages.  For every request b (all of it from the state before the call):
+ *   parent [B] int32 or NULL (all continue)   b: continues itself, p: forks request p (p may go on, too), outside [0, B): ends
+ *   new_lens [B] int32    its new length, clamped to [0, max_seq_len]: grows (parent's length + new rows), stays, or is cut
+ *   table_out [B, block_table_stride], lens_out [B]   entries of rows that it has not are -1
+ *   copies [B, 3]         entry b: the copy that request b needs
+ * It keeps the parent's blocks as far as it has rows of them.  New blocks are the lowest ones that are not live before the call,
+ * dealt to the requests in order, to each first the copy of its last block, then those of its growth.  That copy is made where it
+ * will write behind the parent's rows in a block of which others keep rows, or which is held; where all who keep it
+ * write into it, the first of them keeps the block itself.  Copy before anything is appended.
+ * If the blocks do not suffice, a request gets what is left: lens_out says how many rows it has room for (never fewer than it kept)
+ * and LFPS_FLAG_PAGES_FULL is raised.  Blocks that this call frees can be had from the next one on. */
+int lfps_pages_update(lfps_ctx* ctx, const lfps_kv* kv, const int32_t* parent, const int32_t* new_lens,
+                      const int32_t* held, int32_t* table_out, int32_t* lens_out, int32_t* copies, void* work,
+                      int64_t work_bytes, void* stream);
+
+/* Moves the live blocks to the front of the pool: with m of them, those numbered m and above go to the free numbers below m, both
+ * in rising order.  table_out as above, moves [n_blocks / 2, 3] (the moves first, then empty entries), block_map [n_blocks]
+ * (a block's new number; -1: it was free) for the caller's own tables, n_live [1] = m.  Lengths do not change. */
+int lfps_pages_compact(lfps_ctx* ctx, const lfps_kv* kv, const int32_t* held, int32_t* table_out, int32_t* moves,
+                       int32_t* block_map, int32_t* n_live, void* work, int64_t work_bytes, void* stream);
+
+/* Carries out a list of n copies (device array; entries outside the pool, of no rows or onto themselves are skipped; rows are
+ * clamped to the block) in the pools of kv, which are WRITTEN.  For lists of one's own: no block may be written twice, or written
+ * and read, in one list. */
+int lfps_pages_copy(lfps_ctx* ctx, const lfps_kv* kv, const int32_t* list, int32_t n, void* stream);
+
 /* Switches the score filter of the chained steps on or off (on: only for caches it exists for, bf16 / fp16 / FP8
  * keys; a no-op otherwise).  lfps_reset_history makes every head start without a remembered score. */
 int lfps_set_filter(lfps_ctx* ctx, int32_t on);
@@ -282,6 +352,7 @@ int lfps_copy_cand_count(lfps_ctx* ctx, int32_t* dst, void* stream);
  * word to *flags (host) and clears it. */
 #define LFPS_FLAG_CAND_OVERFLOW 1
 #define LFPS_FLAG_TABLE_FULL 2      /* a table update was skipped: max_seq_len - 1 updates since the last import / init */
+#define LFPS_FLAG_PAGES_FULL 8      /* lfps_pages_update: a request did not get the blocks it wanted (lens_out) */
 #define LFPS_FLAG_Q_RANGE 4         /* fp16 cache: a query element beyond +-65504 was clamped to the fp16 range by a
                                        scoring kernel (the scores of that head are those of the clamped query) */
 int lfps_poll_status(lfps_ctx* ctx, int32_t* flags, void* stream);
@@ -315,7 +386,12 @@ enum {
   LFPS_KERNEL_TABLE_UPDATE = 12,
   LFPS_KERNEL_FILTER_SELECT_ATTEND = 13,   /* S3 + S4 from the filtered pass's survivor lists (chained steps) */
   LFPS_KERNEL_SELECT_ATTEND = 14,          /* S3 + S4 from full score rows (heads the filter left short; unfiltered contexts) */
-  LFPS_N_KERNELS = 15
+  LFPS_KERNEL_PROMPT_ATTN = 15,            /* all launches of a call counted as one, here and below */
+  LFPS_KERNEL_PREFIX_ATTN = 16,
+  LFPS_KERNEL_APPEND = 17,
+  LFPS_KERNEL_PAGES_PLAN = 18,
+  LFPS_KERNEL_PAGES_COPY = 19,
+  LFPS_N_KERNELS = 20
 };
 #define LFPS_TIMING_MAX_LAUNCHES 4096
 int lfps_timing_enable(lfps_ctx* ctx, int32_t on);

@@ -22,7 +22,8 @@ LFPS_OK, LFPS_EINVAL, LFPS_ECAP, LFPS_EHIP, LFPS_ENOMEM = 0, -1, -2, -3, -4
 LFPS_FLAG_CAND_OVERFLOW = 1
 LFPS_FLAG_TABLE_FULL = 2
 LFPS_FLAG_Q_RANGE = 4
-N_KERNELS = 15
+LFPS_FLAG_PAGES_FULL = 8
+N_KERNELS = 20
 NOALLOC_MAX_SCORES = 2097152
 
 
@@ -86,6 +87,13 @@ def _load() -> ctypes.CDLL:
         "lfps_table_step": (ctypes.c_int, [P, VP, ctypes.POINTER(lfps_kv), VP, VP, VP, VP, VP]),
         "lfps_priors": (ctypes.c_int, [P, VP, ctypes.POINTER(lfps_kv), VP, VP, VP, VP]),
         "lfps_head_sparsity": (ctypes.c_int, [P, VP, ctypes.POINTER(lfps_kv), VP, VP, I32, ctypes.c_float, VP, VP, VP]),
+        "lfps_append": (ctypes.c_int, [P, VP, VP, ctypes.c_int64, VP, I32, ctypes.POINTER(lfps_kv), VP]),
+        "lfps_prompt_attn": (ctypes.c_int, [P, VP, ctypes.c_int64, VP, I32, ctypes.POINTER(lfps_kv), VP, VP]),
+        "lfps_prefix_attn_decode": (ctypes.c_int, [P, VP, ctypes.POINTER(lfps_kv), VP, VP, I32, VP, VP]),
+        "lfps_pages_workspace_bytes": (ctypes.c_int, [I32, ctypes.POINTER(ctypes.c_int64)]),
+        "lfps_pages_update": (ctypes.c_int, [P, ctypes.POINTER(lfps_kv), VP, VP, VP, VP, VP, VP, VP, ctypes.c_int64, VP]),
+        "lfps_pages_compact": (ctypes.c_int, [P, ctypes.POINTER(lfps_kv), VP, VP, VP, VP, VP, VP, ctypes.c_int64, VP]),
+        "lfps_pages_copy": (ctypes.c_int, [P, ctypes.POINTER(lfps_kv), VP, I32, VP]),
         "lfps_table_step_gated": (ctypes.c_int, [P, VP, ctypes.POINTER(lfps_kv), VP, VP, VP, VP, I32, ctypes.c_float,
                                                  VP, VP, VP, VP, VP]),
     }
@@ -137,6 +145,27 @@ def _ptr(t: Optional[torch.Tensor], dtype, shape, name: str, device) -> Optional
     if not t.is_contiguous():
         raise ValueError(f"{name}: must be contiguous")
     return t.data_ptr()
+
+
+def _token_rows(t: torch.Tensor, dtype, heads: int, name: str, device):
+    """[tokens, heads, D] rows with any stride between tokens -> (address, stride between tokens)."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.device != device:
+        raise TypeError(f"{name}: expected a tensor on {device}")
+    if t.dtype != dtype:
+        raise TypeError(f"{name}: expected dtype {dtype}, got {t.dtype}")
+    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != 128:
+        raise ValueError(f"{name}: expected [tokens, {heads}, 128], got {tuple(t.shape)}")
+    if t.shape[0] and (t.stride(2) != 1 or (heads > 1 and t.stride(1) != 128)):
+        raise ValueError(f"{name}: the heads of a token must be contiguous")
+    return t.data_ptr(), int(t.stride(0)) if t.shape[0] > 1 else heads * 128
+
+
+def pages_workspace_bytes(n_blocks: int) -> int:
+    out = ctypes.c_int64(0)
+    rc = _lib.lfps_pages_workspace_bytes(int(n_blocks), ctypes.byref(out))
+    if rc != LFPS_OK:
+        raise LfpsError(rc, _lib.lfps_last_error(None).decode())
+    return out.value
 
 
 def lfps_calib_copy(dst: torch.Tensor, src: torch.Tensor):
@@ -383,6 +412,65 @@ class Lfps:
             _ptr(topk_score, torch.float32, (self.B, self.Hq, self.kmax), "topk_score", d),
             _ptr(out, torch.float32, (self.B, self.Hq, self.D), "out", d),
             _ptr(gate_out, torch.int32, (self.B, self.Hq), "gate_out", d), self._stream()))
+
+    # ------------------------------------------------------------------ prompts, forks and pages
+    def lfps_append(self, k_new, v_new, cu, kv: lfps_kv):
+        """k_new, v_new: [tokens, Hkv, D] of kv_dtype, packed (slices of one fused projection: equal token strides); the cache
+        behind the view is written."""
+        d = self.device
+        pk, sk = _token_rows(k_new, self.kv_torch_dtype, self.Hkv, "k_new", d)
+        pv, sv = _token_rows(v_new, self.kv_torch_dtype, self.Hkv, "v_new", d)
+        if k_new.shape != v_new.shape or sk != sv:
+            raise ValueError("k_new and v_new must share shape and token stride")
+        if k_new.shape[0] == 0:
+            return
+        self._check(_lib.lfps_append(self._ctx, pk, pv, sk, _ptr(cu, torch.int32, (self.B + 1,), "cu", d), int(k_new.shape[0]),
+                                     ctypes.byref(kv), self._stream()))
+
+    def lfps_prompt_attn(self, q, cu, kv: lfps_kv, out):
+        """q: [tokens, Hq, D] of kv_dtype, packed, any stride between tokens; out: the same shape and type, contiguous."""
+        d = self.device
+        pq, sq = _token_rows(q, self.kv_torch_dtype, self.Hq, "q", d)
+        po = _ptr(out, self.kv_torch_dtype, tuple(q.shape), "out", d)
+        if q.shape[0] == 0:
+            return
+        self._check(_lib.lfps_prompt_attn(self._ctx, pq, sq, _ptr(cu, torch.int32, (self.B + 1,), "cu", d), int(q.shape[0]),
+                                          ctypes.byref(kv), po, self._stream()))
+
+    def lfps_prefix_attn_decode(self, q, kv: lfps_kv, group_start, prefix_len, out):
+        d, n = self.device, int(prefix_len.shape[0])
+        self._check(_lib.lfps_prefix_attn_decode(
+            self._ctx, _ptr(q, torch.float32, (self.B, self.Hq, self.D), "q", d), ctypes.byref(kv),
+            _ptr(group_start, torch.int32, (n + 1,), "group_start", d), _ptr(prefix_len, torch.int32, (n,), "prefix_len", d), n,
+            _ptr(out, torch.float32, (self.B, self.Hq, self.D), "out", d), self._stream()))
+
+    def pages_workspace(self, n_blocks: int) -> torch.Tensor:
+        """Working memory for lfps_pages_update and lfps_pages_compact on a pool of n_blocks."""
+        return torch.empty(pages_workspace_bytes(n_blocks), dtype=torch.uint8, device=self.device)
+
+    def lfps_pages_update(self, kv: lfps_kv, parent, new_lens, table_out, lens_out, copies, work, held=None):
+        d, B = self.device, self.B
+        self._check(_lib.lfps_pages_update(
+            self._ctx, ctypes.byref(kv), _ptr(parent, torch.int32, (B,), "parent", d), _ptr(new_lens, torch.int32, (B,), "new_lens", d),
+            _ptr(held, torch.int32, (kv.n_blocks,), "held", d),
+            _ptr(table_out, torch.int32, (B, kv.block_table_stride), "table_out", d), _ptr(lens_out, torch.int32, (B,), "lens_out", d),
+            _ptr(copies, torch.int32, (B, 3), "copies", d), _ptr(work, torch.uint8, (work.numel(),), "work", d), work.numel(),
+            self._stream()))
+
+    def lfps_pages_compact(self, kv: lfps_kv, table_out, moves, block_map, n_live, work, held=None):
+        d, n = self.device, kv.n_blocks
+        self._check(_lib.lfps_pages_compact(
+            self._ctx, ctypes.byref(kv), _ptr(held, torch.int32, (n,), "held", d),
+            _ptr(table_out, torch.int32, (self.B, kv.block_table_stride), "table_out", d),
+            _ptr(moves, torch.int32, (n // 2, 3), "moves", d), _ptr(block_map, torch.int32, (n,), "block_map", d),
+            _ptr(n_live, torch.int32, (1,), "n_live", d), _ptr(work, torch.uint8, (work.numel(),), "work", d), work.numel(),
+            self._stream()))
+
+    def lfps_pages_copy(self, kv: lfps_kv, copies):
+        n = int(copies.shape[0])
+        p = _ptr(copies, torch.int32, (n, 3), "copies", self.device)
+        if n:
+            self._check(_lib.lfps_pages_copy(self._ctx, ctypes.byref(kv), p, n, self._stream()))
 
     def lfps_set_filter(self, on: bool):
         self._check(_lib.lfps_set_filter(self._ctx, int(bool(on))))

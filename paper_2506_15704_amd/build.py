@@ -13,7 +13,8 @@ INCLUDE = os.path.join(os.path.dirname(PKG_DIR), "include")
 LIB_PATH = os.path.join(PKG_DIR, "liblfps.so")
 SOURCES = ["lfps_api.hip", "candidates.hip", "score.hip", "range_score.hip", "wide_score.hip", "select.hip",
            "select_attend_bf16.hip", "select_attend_bf16_fp8.hip", "select_attend_fp8.hip",
-           "select_attend_f16.hip", "select_attend.hip", "attention.hip", "tables.hip", "prefill.hip", "exact_topk.hip"]
+           "select_attend_f16.hip", "select_attend.hip", "attention.hip", "tables.hip", "prefill.hip", "exact_topk.hip",
+           "append.hip", "prompt_attn.hip", "prefix_attn.hip", "pages.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",

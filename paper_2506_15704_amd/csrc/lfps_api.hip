@@ -46,7 +46,7 @@ struct lfps_ctx {
   int32_t* cand;       // [B, Hkv, cand_cap]
   int32_t* cand_count; // [B, Hkv]
   float* sel_score;    // [B, Hq, kmax]
-  float* part;         // split partials of the full-attention baseline
+  float* part;         // split partials of the full-attention baseline, of prompts and of shared prefixes
   // exact Top-k baseline in its filtered form (x_fast): the dense rows on the line, the sample and its rank
   int x_fast;
   int32_t* x_cnt;      // [B, Hkv] rows of each group
@@ -71,7 +71,8 @@ static thread_local char g_create_err[512] = "";
 static const char* const kKernelNames[LFPS_N_KERNELS] = {
     "candidates", "gather_score", "select", "sparse_attn",
     "dense_score", "full_attn", "full_merge", "head_score", "filter_score", "filter_select",
-    "table_flags", "table_candidates", "table_update", "filter_select_attend", "select_attend"};
+    "table_flags", "table_candidates", "table_update", "filter_select_attend", "select_attend",
+    "prompt_attn", "prefix_attn", "append", "pages_plan", "pages_copy"};
 
 // Margin below the previous step's k-th best score at which the filtered pass keeps a row.
 static const float kFilterMargin = 0.125f;
@@ -150,6 +151,7 @@ int check_config(const lfps_config* c, Sizes* z, char* err, size_t errn) {
   z->count_b = align256((int64_t)c->batch * c->n_kv_heads * 4);
   z->sel_b = align256((int64_t)c->batch * c->n_q_heads * c->max_k * 4);
   z->part_b = align256((int64_t)c->batch * c->n_kv_heads * z->n_split_full * G * (kD + 2) * 4);
+  if (z->part_b < align256(attn_part_rows(s) * kPartFloats * 4)) z->part_b = align256(attn_part_rows(s) * kPartFloats * 4);
   const bool filt = c->kv_dtype == LFPS_BF16 || c->kv_dtype == LFPS_F16;
   z->nseg = filter_nseg(s);
   {
@@ -927,6 +929,156 @@ int lfps_table_step_gated(lfps_ctx* ctx, const float* q, const lfps_kv* kv, cons
                                       gate, vbar, topk_idx, topk_score, out, st);
   if (e != hipSuccess) return fail(ctx, LFPS_EHIP, "lfps_table_step_gated (gate)", e);
   return table_step_impl(ctx, q, v, k, topk_idx, topk_score, out, gate, st);
+}
+
+// ---- prompts, forks and pages ----------------------------------------------------------------------------------
+
+// Launches go to the context's device, whichever is the thread's current one.
+namespace {
+struct OnDevice {
+  int before;
+  explicit OnDevice(int device) : before(-1) {
+    int now = device;
+    if (hipGetDevice(&now) == hipSuccess && now != device && hipSetDevice(device) == hipSuccess) before = now;
+  }
+  ~OnDevice() {
+    if (before >= 0) (void)hipSetDevice(before);
+  }
+};
+
+int elem_bytes(const lfps_config& c) { return c.kv_dtype == LFPS_F32 ? 4 : 2; }
+
+// Packed token rows: `heads` rows of D elements a token.
+int check_tokens(lfps_ctx* ctx, const void* p, int64_t stride_t, int heads, const char* what) {
+  if (stride_t < (int64_t)heads * kD || (stride_t * elem_bytes(ctx->cfg)) % 16 || (uintptr_t)p % 16) return fail(ctx, LFPS_EINVAL, what);
+  return LFPS_OK;
+}
+int check_n_tokens(lfps_ctx* ctx, int32_t n_tokens) {
+  if (n_tokens < 0 || (int64_t)n_tokens * ctx->shape.Hq > (1 << 27)) return fail(ctx, LFPS_EINVAL, "n_tokens must be >= 0 and n_tokens * n_q_heads at most 2^27");
+  return LFPS_OK;
+}
+int check_kv_both(lfps_ctx* ctx, const lfps_kv* kv, KvView* v) {
+  const int rc = check_kv(ctx, kv, false, v);
+  if (rc != LFPS_OK) return rc;
+  return kv->v ? LFPS_OK : fail(ctx, LFPS_EINVAL, "kv->v is NULL");
+}
+int check_pages(lfps_ctx* ctx, const lfps_kv* kv, const void* table_out, const void* work, int64_t work_bytes, KvView* v) {
+  const int rc = check_kv(ctx, kv, false, v);
+  if (rc != LFPS_OK) return rc;
+  if (!kv->block_table) return fail(ctx, LFPS_EINVAL, "pages: the view has no block table");
+  if (kv->n_blocks > (1 << 24)) return fail(ctx, LFPS_ECAP, "pages: n_blocks exceeds 2^24");
+  if ((uintptr_t)work % 16 || work_bytes < pages_workspace_bytes(kv->n_blocks))
+    return fail(ctx, LFPS_EINVAL, "pages: work must be 16-byte aligned and hold lfps_pages_workspace_bytes(n_blocks)");
+  const uintptr_t bytes = (uintptr_t)ctx->shape.B * kv->block_table_stride * 4, from = (uintptr_t)kv->block_table, to = (uintptr_t)table_out;
+  if (from < to + bytes && to < from + bytes) return fail(ctx, LFPS_EINVAL, "pages: table_out overlaps the view's block table");
+  return LFPS_OK;
+}
+}  // namespace
+
+int lfps_append(lfps_ctx* ctx, const void* k_new, const void* v_new, int64_t stride_t, const int32_t* cu, int32_t n_tokens,
+                const lfps_kv* kv, void* stream) {
+  if (!ctx) return LFPS_EINVAL;
+  if (!k_new || !v_new || !cu) return fail(ctx, LFPS_EINVAL, "lfps_append: NULL argument");
+  KvView v;
+  int rc = check_kv_both(ctx, kv, &v);
+  if (rc == LFPS_OK) rc = check_n_tokens(ctx, n_tokens);
+  const char* rows = "lfps_append: k_new and v_new need 16-byte aligned rows and stride_t >= n_kv_heads * head_dim";
+  if (rc == LFPS_OK) rc = check_tokens(ctx, k_new, stride_t, ctx->shape.Hkv, rows);
+  if (rc == LFPS_OK) rc = check_tokens(ctx, v_new, stride_t, ctx->shape.Hkv, rows);
+  if (rc != LFPS_OK) return rc;
+  if (n_tokens == 0) return LFPS_OK;
+  const OnDevice on(ctx->cfg.device);
+  hipStream_t st = (hipStream_t)stream;
+  LAUNCH(ctx, LFPS_KERNEL_APPEND, st, launch_append(ctx->shape, ctx->cfg.kv_dtype, v, k_new, v_new, stride_t, cu, n_tokens, st));
+  return LFPS_OK;
+}
+
+int lfps_prompt_attn(lfps_ctx* ctx, const void* q, int64_t stride_t, const int32_t* cu, int32_t n_tokens, const lfps_kv* kv, void* out,
+                     void* stream) {
+  if (!ctx) return LFPS_EINVAL;
+  if (!q || !cu || !out) return fail(ctx, LFPS_EINVAL, "lfps_prompt_attn: NULL argument");
+  KvView v;
+  int rc = check_kv_both(ctx, kv, &v);
+  if (rc == LFPS_OK) rc = check_n_tokens(ctx, n_tokens);
+  if (rc == LFPS_OK)
+    rc = check_tokens(ctx, q, stride_t, ctx->shape.Hq, "lfps_prompt_attn: q needs 16-byte aligned rows and stride_t >= n_q_heads * head_dim");
+  if (rc != LFPS_OK) return rc;
+  if ((uintptr_t)out % 16) return fail(ctx, LFPS_EINVAL, "lfps_prompt_attn: out must be 16-byte aligned");
+  if (n_tokens == 0) return LFPS_OK;
+  const OnDevice on(ctx->cfg.device);
+  hipStream_t st = (hipStream_t)stream;
+  LAUNCH(ctx, LFPS_KERNEL_PROMPT_ATTN, st,
+         launch_prompt_attn(ctx->shape, ctx->cfg.kv_dtype, v, q, stride_t, cu, n_tokens, out, ctx->part, attn_part_rows(ctx->shape), st));
+  return LFPS_OK;
+}
+
+int lfps_prefix_attn_decode(lfps_ctx* ctx, const float* q, const lfps_kv* kv, const int32_t* group_start, const int32_t* prefix_len,
+                            int32_t n_groups, float* out, void* stream) {
+  if (!ctx) return LFPS_EINVAL;
+  if (!q || !group_start || !prefix_len || !out) return fail(ctx, LFPS_EINVAL, "lfps_prefix_attn_decode: NULL argument");
+  KvView v;
+  const int rc = check_kv_both(ctx, kv, &v);
+  if (rc != LFPS_OK) return rc;
+  if (n_groups < 1 || n_groups > ctx->shape.B) return fail(ctx, LFPS_EINVAL, "lfps_prefix_attn_decode: n_groups must be in [1, batch]");
+  if ((uintptr_t)q % 16 || (uintptr_t)out % 16) return fail(ctx, LFPS_EINVAL, "lfps_prefix_attn_decode: q and out must be 16-byte aligned");
+  const OnDevice on(ctx->cfg.device);
+  hipStream_t st = (hipStream_t)stream;
+  LAUNCH(ctx, LFPS_KERNEL_PREFIX_ATTN, st,
+         launch_prefix_attn(ctx->shape, ctx->cfg.kv_dtype, v, q, group_start, prefix_len, n_groups, out, ctx->part, attn_part_rows(ctx->shape), st));
+  return LFPS_OK;
+}
+
+int lfps_pages_workspace_bytes(int32_t n_blocks, int64_t* out) {
+  if (n_blocks < 1 || n_blocks > (1 << 24) || !out) {
+    snprintf(g_create_err, sizeof g_create_err, "lfps_pages_workspace_bytes: n_blocks must be in [1, 2^24] (got %d)", n_blocks);
+    return n_blocks > (1 << 24) ? LFPS_ECAP : LFPS_EINVAL;
+  }
+  *out = pages_workspace_bytes(n_blocks);
+  return LFPS_OK;
+}
+
+int lfps_pages_update(lfps_ctx* ctx, const lfps_kv* kv, const int32_t* parent, const int32_t* new_lens, const int32_t* held,
+                      int32_t* table_out, int32_t* lens_out, int32_t* copies, void* work, int64_t work_bytes, void* stream) {
+  if (!ctx) return LFPS_EINVAL;
+  if (!new_lens || !table_out || !lens_out || !copies || !work) return fail(ctx, LFPS_EINVAL, "lfps_pages_update: NULL argument");
+  KvView v;
+  const int rc = check_pages(ctx, kv, table_out, work, work_bytes, &v);
+  if (rc != LFPS_OK) return rc;
+  if (lens_out == kv->seq_lens) return fail(ctx, LFPS_EINVAL, "lfps_pages_update: lens_out is the view's seq_lens");
+  const OnDevice on(ctx->cfg.device);
+  hipStream_t st = (hipStream_t)stream;
+  LAUNCH(ctx, LFPS_KERNEL_PAGES_PLAN, st,
+         launch_pages_update(ctx->shape, v, parent, new_lens, held, table_out, lens_out, copies, work, ctx->flags, st));
+  return LFPS_OK;
+}
+
+int lfps_pages_compact(lfps_ctx* ctx, const lfps_kv* kv, const int32_t* held, int32_t* table_out, int32_t* moves, int32_t* block_map,
+                       int32_t* n_live, void* work, int64_t work_bytes, void* stream) {
+  if (!ctx) return LFPS_EINVAL;
+  if (!table_out || !block_map || !n_live || !work) return fail(ctx, LFPS_EINVAL, "lfps_pages_compact: NULL argument");
+  KvView v;
+  const int rc = check_pages(ctx, kv, table_out, work, work_bytes, &v);
+  if (rc != LFPS_OK) return rc;
+  if (!moves && kv->n_blocks > 1) return fail(ctx, LFPS_EINVAL, "lfps_pages_compact: moves is NULL");
+  const OnDevice on(ctx->cfg.device);
+  hipStream_t st = (hipStream_t)stream;
+  LAUNCH(ctx, LFPS_KERNEL_PAGES_PLAN, st, launch_pages_compact(ctx->shape, v, held, table_out, moves, block_map, n_live, work, st));
+  return LFPS_OK;
+}
+
+int lfps_pages_copy(lfps_ctx* ctx, const lfps_kv* kv, const int32_t* list, int32_t n, void* stream) {
+  if (!ctx) return LFPS_EINVAL;
+  if (!list) return fail(ctx, LFPS_EINVAL, "lfps_pages_copy: NULL argument");
+  KvView v;
+  const int rc = check_kv_both(ctx, kv, &v);
+  if (rc != LFPS_OK) return rc;
+  if (!kv->block_table) return fail(ctx, LFPS_EINVAL, "lfps_pages_copy: the view has no block table");
+  if (n < 0) return fail(ctx, LFPS_EINVAL, "lfps_pages_copy: n must be >= 0");
+  if (n == 0) return LFPS_OK;
+  const OnDevice on(ctx->cfg.device);
+  hipStream_t st = (hipStream_t)stream;
+  LAUNCH(ctx, LFPS_KERNEL_PAGES_COPY, st, launch_pages_copy(ctx->shape, ctx->cfg.kv_dtype, v, list, n, st));
+  return LFPS_OK;
 }
 
 __global__ void k_fill_f32(float* p, int n, float v) {

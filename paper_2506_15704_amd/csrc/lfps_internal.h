@@ -295,6 +295,27 @@ int64_t prior_scratch_bytes(const Shape& s);
 hipError_t launch_priors(const Shape& s, int dtype, const float* q, const KvView& kv, float* kbar, float* vbar,
                          float* sigma2_hat, void* scratch, int32_t* flags, hipStream_t st);
 
+// Packed new tokens into the cache; their causal attention over it; full attention with shared first rows; pages.  See append.hip,
+// prompt_attn.hip, prefix_attn.hip and pages.hip.  part: room for part_rows (attn_part_rows) partial results of a query row.
+constexpr int kPartFloats = kD + 4;        // weighted sum of the values, largest score (powers of two), sum of the weights
+inline int64_t attn_part_rows(const Shape& s) {
+  // Two parts at least of every (request, head); otherwise what splits a few hundred tokens of 32 heads over all CUs.
+  const int64_t two = 2 * (int64_t)s.B * s.Hq;
+  return two > 65536 ? two : 65536;
+}
+hipError_t launch_append(const Shape& s, int dtype, const KvView& kv, const void* k_new, const void* v_new, int64_t stride_t,
+                         const int32_t* cu, int n_tokens, hipStream_t st);
+hipError_t launch_prompt_attn(const Shape& s, int dtype, const KvView& kv, const void* q, int64_t q_stride, const int32_t* cu,
+                              int n_tokens, void* out, float* part, int64_t part_rows, hipStream_t st);
+hipError_t launch_prefix_attn(const Shape& s, int dtype, const KvView& kv, const float* q, const int32_t* group_start,
+                              const int32_t* prefix_len, int n_groups, float* out, float* part, int64_t part_rows, hipStream_t st);
+int64_t pages_workspace_bytes(int32_t n_blocks);
+hipError_t launch_pages_update(const Shape& s, const KvView& kv, const int32_t* parent, const int32_t* new_lens, const int32_t* held,
+                               int32_t* table_out, int32_t* lens_out, int32_t* copies_out, void* work, int32_t* flags, hipStream_t st);
+hipError_t launch_pages_compact(const Shape& s, const KvView& kv, const int32_t* held, int32_t* table_out, int32_t* moves, int32_t* map,
+                                int32_t* n_live, void* work, hipStream_t st);
+hipError_t launch_pages_copy(const Shape& s, int dtype, const KvView& kv, const int32_t* list, int n, hipStream_t st);
+
 // ---- small device helpers ------------------------------------------------------------
 // A kernel's arguments come through the scalar cache, where none of them is when it starts, and the compiler asks for an argument where
 // it is used: every further 64-byte line of them is a trip to memory that all waves wait for, 0.4 us, and the longest kernels here have

@@ -1,0 +1,208 @@
+// Causal attention of the newest tokens of every request over its cache: whole prompts, chunks behind rows that are there already, a
+// few drafted tokens, single ones.  Tokens of all requests are packed; token i of the t_b of request b sits at row n_b - t_b + i
+// and sees the rows up to its own.
+//
+// Two kernels, both the body of tile_attn.h.  k_prompt_tiles: a workgroup has 128 query rows of one (request, KV head), 32 a wave,
+// and streams the rows they see; bound by the matrix units.  k_prompt_few: a request whose tokens fill no more than one wave's
+// rows; the four waves share the keys, and the rows are cut into parts that are joined afterwards; bound by the bytes of K and V.
+// Which one takes a request is decided on the device by its number of tokens, so one call takes any mixture.
+#include "tile_attn.h"
+
+namespace lfps {
+
+namespace {
+
+template <typename TQ>
+struct PromptArgs {
+  Shape s;
+  KvView kv;
+  const TQ* q;
+  int64_t q_stride;        // elements between tokens of q
+  const int32_t* cu;
+  int32_t n_tokens;
+  TQ* out;
+  float* part;
+  int32_t splits, few_splits;    // parts of a tile's rows in the two kernels; few_splits 0: k_prompt_few is not launched
+  int64_t few_part;              // where the latter's partial results begin, in rows
+  int32_t few_by_token;          // and whether they lie by token, or else in room for few_tokens of every request
+};
+
+// Tokens [c0, c1) of request b, whatever cu holds.
+template <typename A>
+__device__ __forceinline__ void tokens_of(const A& a, int b, int* c0, int* c1) {
+  const int x = a.cu[b], y = a.cu[b + 1];
+  *c0 = x < 0 ? 0 : (x > a.n_tokens ? a.n_tokens : x);
+  *c1 = y < *c0 ? *c0 : (y > a.n_tokens ? a.n_tokens : y);
+}
+__device__ __forceinline__ int length_of(const Shape& s, const int32_t* seq_lens, int b) {
+  const int n = seq_lens[b];
+  return n < 0 ? 0 : (n > s.Lcap ? s.Lcap : n);
+}
+template <typename TK>
+constexpr int few_most() { return 32 * (4 / few_key_waves<TK>()); }      // query rows of a request that k_prompt_few takes
+// The partial results of token i (of those from c0 on of request b), a row of `splits` of them.
+template <typename A>
+__device__ __forceinline__ int64_t part_row(const A& a, bool few, int most, int b, int c0, int i, int head) {
+  if (!few) return ((int64_t)(c0 + i) * a.s.Hq + head) * a.splits;
+  const int64_t token = a.few_by_token ? c0 + i : (int64_t)b * (most / a.s.G) + i;
+  return a.few_part + (token * a.s.Hq + head) * a.few_splits;
+}
+
+// Rows [row0, row0 + 32 * row waves) of request b's tokens (token row0 / G, heads fastest), KV head g, part `split` of `splits`.
+template <typename TK, typename TV, typename TQ, int kKeyWaves>
+__device__ __forceinline__ void prompt_tile(char* lds, const PromptArgs<TQ>& a, int b, int g, int c0, int c1, int row0, int split) {
+  constexpr bool kFew = kKeyWaves > 1;
+  const int splits = kFew ? a.few_splits : a.splits;
+  typedef typename InLds<TK>::Op Op;
+  constexpr int kRowWaves = 4 / kKeyWaves;
+  const Shape& s = a.s;
+  const int G = s.G, shift = G == 4 ? 2 : G - 1;                // G = 1, 2, 4
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), nrow = lane & 31, h = lane >> 5;
+  const int n = length_of(s, a.kv.seq_lens, b), t = c1 - c0, rows = t << shift;
+  auto seen = [&](int token) {                                  // cache rows that a token of the request sees
+    const int pos = n - t + token + 1;
+    return pos < 0 ? 0 : pos;
+  };
+  int m = row0 + (wave / kKeyWaves) * 32 + nrow;
+  const bool valid = m < rows;
+  m = valid ? m : rows - 1;
+  const int token = m >> shift, head = g * G + (m & (G - 1));
+  const int limit = valid ? seen(token) : 0;
+  const int last = (row0 + 32 * kRowWaves < rows ? row0 + 32 * kRowWaves : rows) - 1;
+  int lo, hi;
+  split_rows(0, seen(last >> shift), splits, split, tile_rows(kKeyWaves), &lo, &hi);
+  RowState<Op, 1> st;
+  st.clear();
+  if (lo < hi) {
+    typename RowState<Op, 1>::Query q;
+    q.load(a.q + (int64_t)(c0 + token) * a.q_stride + head * kD, h);
+    const CacheRows<TK> K(a.kv.k, a.kv, b, g);
+    const CacheRows<TV> V(a.kv.v, a.kv, b, g);
+    tile_loop<TK, TV, Op, 1, kKeyWaves>(lds, K, V, lo, hi, q, limit, st);
+  }
+  RowOut<TQ> to = {nullptr, nullptr};
+  if (valid) {
+    if (splits > 1) to.part = a.part + (part_row(a, kFew, few_most<TK>(), b, c0, token, head) + split) * kPartFloats;
+    else to.out = a.out + ((int64_t)(c0 + token) * s.Hq + head) * kD;
+  }
+  tile_finish<Op, 1, kKeyWaves>(lds, st, to);
+}
+
+}  // namespace
+
+// grid Hkv * splits * (tiles of all requests, at most T G / 128 + B), the latest rows of a request first: they see most
+template <typename TK, typename TV, typename TQ>
+__global__ __launch_bounds__(kTileThreads) void k_prompt_tiles(PromptArgs<TQ> a, int tiles) {
+  __shared__ __attribute__((aligned(16))) char lds[tile_lds<TK, TV, 1>()];
+  const int G = a.s.G, per = 128 / G;
+  const int g = blockIdx.x % a.s.Hkv, x0 = blockIdx.x / a.s.Hkv, split = x0 % a.splits, x = tiles - 1 - x0 / a.splits;
+  // tile x is among those of the last request b with cu[b] / per + b <= x: a request has no more tiles than lie between
+  auto first_tile = [&](int i) {
+    const int c = a.cu[i];
+    return (c < 0 ? 0 : (c > a.n_tokens ? a.n_tokens : c)) / per + i;
+  };
+  const int b = last_not_above(a.s.B - 1, x, first_tile);
+  int c0, c1;
+  tokens_of(a, b, &c0, &c1);
+  const int row0 = (x - first_tile(b)) * 128;
+  if (row0 < 0 || row0 >= (c1 - c0) * G) return;
+  if (a.few_splits && (c1 - c0) * G <= few_most<TK>()) return;
+  prompt_tile<TK, TV, TQ, 1>(lds, a, b, g, c0, c1, row0, split);
+}
+
+// grid Hkv * few_splits * B
+template <typename TK, typename TV, typename TQ>
+__global__ __launch_bounds__(kTileThreads) void k_prompt_few(PromptArgs<TQ> a) {
+  constexpr int kKeyWaves = few_key_waves<TK>();
+  __shared__ __attribute__((aligned(16))) char lds[tile_lds<TK, TV, kKeyWaves>()];
+  const int g = blockIdx.x % a.s.Hkv, x0 = blockIdx.x / a.s.Hkv, split = x0 % a.few_splits, b = x0 / a.few_splits;
+  int c0, c1;
+  tokens_of(a, b, &c0, &c1);
+  if (c0 >= c1 || (int64_t)(c1 - c0) * a.s.G > few_most<TK>()) return;
+  prompt_tile<TK, TV, TQ, kKeyWaves>(lds, a, b, g, c0, c1, 0, split);
+}
+
+// The parts of a row -> its output row: 32 lanes a (token, head).  few: of every request's first most / G tokens, if it has no more; else
+// of every token of the other requests.
+template <typename TQ>
+__global__ __launch_bounds__(kTileThreads) void k_prompt_merge(PromptArgs<TQ> a, int few, int most) {
+  const int lane32 = threadIdx.x & 31, Hq = a.s.Hq;
+  const int64_t x = (int64_t)blockIdx.x * (kTileThreads / 32) + threadIdx.x / 32;
+  const int head = (int)(x % Hq), y = (int)(x / Hq);
+  int b, i, c0, c1;
+  if (few) {
+    b = y / (most / a.s.G);
+    i = y % (most / a.s.G);
+    if (b >= a.s.B) return;
+    tokens_of(a, b, &c0, &c1);
+  } else {
+    if (y >= a.n_tokens) return;
+    int lo = 0, hi = a.s.B - 1;                                // the last request whose tokens do not begin behind y
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) / 2;
+      if (a.cu[mid] <= y) lo = mid;
+      else hi = mid - 1;
+    }
+    b = lo;
+    tokens_of(a, b, &c0, &c1);
+    i = y - c0;
+  }
+  const int t = c1 - c0;
+  if (i < 0 || i >= t || (few != 0) != (a.few_splits && (int64_t)t * a.s.G <= most)) return;
+  put4(a.out + ((int64_t)(c0 + i) * Hq + head) * kD + 4 * lane32,
+       merge_parts(a.part + part_row(a, few != 0, most, b, c0, i, head) * kPartFloats, few ? a.few_splits : a.splits, lane32));
+}
+
+namespace {
+
+template <typename TK, typename TV, typename TQ>
+hipError_t prompt_t(const Shape& s, const KvView& kv, const void* q, int64_t q_stride, const int32_t* cu, int n_tokens, void* out,
+                    float* part, int64_t part_rows, hipStream_t st) {
+  constexpr int kMost = few_most<TK>();
+  PromptArgs<TQ> a = {s, kv, (const TQ*)q, q_stride, cu, n_tokens, (TQ*)out, part, 1, 0, 0, 0};
+  const int per = 128 / s.G;
+  // As many parts as give every CU two workgroups, where the rows' partial results have room.
+  auto parts = [&](int64_t groups, int64_t rows, int64_t room) {
+    int64_t n = (512 + groups - 1) / groups;
+    if (n * rows > room) n = room / rows;
+    const int64_t by_len = (s.Lcap + 255) / 256;
+    if (n > by_len) n = by_len;
+    if (n > kMaxSplits) n = kMaxSplits;
+    return (int)(n < 1 ? 1 : n);
+  };
+  const bool all_few = (int64_t)n_tokens * s.G <= kMost, none_few = !all_few && s.B == 1;
+  const int tiles = n_tokens / per + s.B;
+  if (!all_few) a.splits = parts((int64_t)tiles * s.Hkv, (int64_t)n_tokens * s.Hq, part_rows);
+  if (a.splits > 1) a.few_part = (int64_t)n_tokens * s.Hq * a.splits;
+  if (!none_few) {
+    const int64_t room = (int64_t)s.B * (kMost / s.G);
+    a.few_by_token = n_tokens <= room;
+    a.few_splits = parts((int64_t)(s.B < n_tokens ? s.B : n_tokens) * s.Hkv, (a.few_by_token ? n_tokens : room) * s.Hq, part_rows - a.few_part);
+  }
+  if (!all_few)
+    hipLaunchKernelGGL((k_prompt_tiles<TK, TV, TQ>), dim3((unsigned)(s.Hkv * a.splits * tiles)), dim3(kTileThreads), 0, st, a, tiles);
+  if (!none_few)
+    hipLaunchKernelGGL((k_prompt_few<TK, TV, TQ>), dim3((unsigned)(s.Hkv * a.few_splits * s.B)), dim3(kTileThreads), 0, st, a);
+  auto merge = [&](int few, int64_t rows) {
+    hipLaunchKernelGGL((k_prompt_merge<TQ>), dim3((unsigned)((rows + 7) / 8)), dim3(kTileThreads), 0, st, a, few, kMost);
+  };
+  if (a.splits > 1) merge(0, (int64_t)n_tokens * s.Hq);
+  if (a.few_splits > 1) merge(1, (int64_t)s.B * (kMost / s.G) * s.Hq);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_prompt_attn(const Shape& s, int dtype, const KvView& kv, const void* q, int64_t q_stride, const int32_t* cu,
+                              int n_tokens, void* out, float* part, int64_t part_rows, hipStream_t st) {
+#define LFPS_PROMPT(TK, TV, TQ) return prompt_t<TK, TV, TQ>(s, kv, q, q_stride, cu, n_tokens, out, part, part_rows, st)
+  if (dtype == LFPS_F32) LFPS_PROMPT(float, float, float);
+  if (dtype == LFPS_F16) LFPS_PROMPT(_Float16, _Float16, _Float16);
+  if (kv.k_fp8 && kv.v_fp8) LFPS_PROMPT(uint8_t, uint8_t, uint16_t);
+  if (kv.k_fp8) LFPS_PROMPT(uint8_t, uint16_t, uint16_t);
+  if (kv.v_fp8) LFPS_PROMPT(uint16_t, uint8_t, uint16_t);
+  LFPS_PROMPT(uint16_t, uint16_t, uint16_t);
+#undef LFPS_PROMPT
+}
+
+}  // namespace lfps

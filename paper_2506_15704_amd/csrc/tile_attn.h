@@ -1,0 +1,522 @@
+// Attention of many query rows over a range of a request's cache rows on the matrix units: the body shared by the prompt kernel
+// (prompt_attn.hip) and the shared-prefix kernel (prefix_attn.hip).
+//
+//   o[m] = sum_j p_mj V_j / sum_j p_mj,   p_mj = exp((q_m . K_j - max_j q_m . K_j) / sqrt(D)),   j < limit(m)
+//
+// in one pass over K and V: a running maximum per row, sums rescaled when it grows (online softmax).  The G heads of a KV group see
+// the same rows, so a query row m is a (token, head) pair, heads fastest, and a workgroup's rows share every K and V row.
+//
+// A wave owns 32 query rows.  Scores are computed transposed, S^T = K Q^T, by 32x32 matrix instructions: a lane then holds one
+// query row's scores (its column) for 16 of 32 keys, so maximum and sum are taken in registers with one exchange between
+// the wave's halves, and the weights are the second product's operand (O^T = V^T P^T) as they lie, if the keys of that
+// product are taken in the order in which the first one leaves them: V is read from LDS transposed, four keys a lane
+// (ds_read_b64_tr), with each half of the wave reading the keys it holds weights for.
+#pragma once
+#include "lfps_internal.h"
+
+#include <type_traits>
+
+namespace lfps {
+
+constexpr int kTileThreads = 256;            // four waves
+constexpr float kLog2e = 1.4426950408889634f;
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x2t __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2t __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x2t __attribute__((ext_vector_type(2)));
+
+// The rows [.., end) of one request and KV head as a kernel reads them.
+template <typename T>
+struct CacheRows {
+  const T* base;                             // row 0 of the request (contiguous) or of the pool, at the KV head
+  int64_t stride_b, stride_n;
+  KvPage pg;
+  int b;
+  __device__ __forceinline__ CacheRows(const void* p, const KvView& kv, int b_, int g) : stride_b(kv.stride_b), stride_n(kv.stride_n), pg(kv.page), b(b_) {
+    base = (const T*)p + (kv.page.table ? (int64_t)0 : (int64_t)b_ * kv.stride_b) + (int64_t)g * kv.stride_h;
+  }
+  __device__ __forceinline__ int entry(int r) const { return pg.table ? RowMap<true>::block(pg, b, r) : 0; }
+  __device__ __forceinline__ const T* at(int r, int e) const {
+    return base + (pg.table ? RowMap<true>::offset_in(pg, e, r, stride_b, stride_n) : (int64_t)r * stride_n);
+  }
+};
+
+// ---- the elements in LDS and in the matrix instructions ------------------------------------------------------
+// A row in LDS is kRowBytes long, in chunks of 16 bytes; chunk c of row r lies at place c ^ 2 (r & 7) of the row, so that eight
+// consecutive rows read at one chunk (scores), and four rows read at two neighbouring chunks (values), touch all banks evenly.
+__device__ __forceinline__ int chunk_place(int r, int c) { return c ^ (2 * (r & 7)); }
+
+template <typename T>
+struct InLds { typedef bf16x8 Op; static constexpr int kRowBytes = 256; };       // bf16, and FP8 (every value is a bf16 value)
+template <>
+struct InLds<_Float16> { typedef f16x8 Op; static constexpr int kRowBytes = 256; };
+template <>
+struct InLds<float> { typedef float Op; static constexpr int kRowBytes = 512; };
+
+__device__ __forceinline__ f32x16 mfma32(bf16x8 a, bf16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f32x16 mfma32(f16x8 a, f16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f32x16 mfma32(float a, float b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x2f32(a, b, c, 0, 0, 0); }
+
+// Rows [k0, k0 + kRows) of K or V on their way from the cache to LDS, in the registers of the workgroup's threads.
+template <typename T, int kRows>
+struct Staged {
+  static constexpr int kChunks = kD * (int)sizeof(T) / 16;                // 16-byte loads a row
+  static constexpr int kLoads = kRows * kChunks / kTileThreads;
+  u32x4 x[kLoads];
+  int e[kLoads];                                                          // the block table's entries of the rows of the tile after
+
+  __device__ __forceinline__ static int row(int i, int tid) { return (tid + kTileThreads * i) / kChunks; }
+  __device__ __forceinline__ void look_up(const CacheRows<T>& c, int k0, int end, int tid) {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int r = k0 + row(i, tid);
+      e[i] = c.entry(r < end ? r : end - 1);
+    }
+  }
+  // Rows from `end` on are loaded from the last row (a caller's rows beyond it may be anything, also unmapped) and stored as zeros:
+  // their weights are 0, and 0 times what they hold need not be.
+  __device__ __forceinline__ void load(const CacheRows<T>& c, int k0, int end, int tid) {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int r = k0 + row(i, tid);
+      x[i] = *reinterpret_cast<const u32x4*>(reinterpret_cast<const char*>(c.at(r < end ? r : end - 1, e[i])) + 16 * (tid % kChunks));
+    }
+  }
+  __device__ __forceinline__ void store(char* lds, int k0, int end, int tid) const {
+    const int c = tid % kChunks;
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int r = row(i, tid);
+      const bool in = k0 + r < end;
+      u32x4 w = x[i];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) w[u] = in ? w[u] : 0u;
+      char* at = lds + r * InLds<T>::kRowBytes;
+      if constexpr (sizeof(T) == 1) {
+        *reinterpret_cast<bf16x8*>(at + 16 * chunk_place(r, 2 * c)) = fp8x8_to_bf16x8(w[0], w[1]);
+        *reinterpret_cast<bf16x8*>(at + 16 * chunk_place(r, 2 * c + 1)) = fp8x8_to_bf16x8(w[2], w[3]);
+      } else {
+        *reinterpret_cast<u32x4*>(at + 16 * chunk_place(r, c)) = w;
+      }
+    }
+  }
+};
+
+// ---- the query rows of a wave ---------------------------------------------------------------------------------
+// Lane (n, h) (n = lane % 32, h = lane / 32) holds of query row n the channels that the first product wants from it: of step s
+// the chunk 16 s + 8 h .. + 7 (16-bit operands; kTerms > 1: an fp32 query as a sum of that many 16-bit terms), of fp32 operands
+// the channels 8 s + 4 h .. + 3.  `unit`: the factor from the products to scores in powers of two.
+template <typename Op, int kTerms>
+struct QueryTile {
+  Op x[kTerms][8];
+  float unit;
+  __device__ __forceinline__ void load(const typename std::conditional<std::is_same<Op, bf16x8>::value, uint16_t, _Float16>::type* q, int h) {
+    static_assert(kTerms == 1, "");
+#pragma unroll
+    for (int s = 0; s < 8; ++s) x[0][s] = *reinterpret_cast<const Op*>(q + 16 * s + 8 * h);
+    unit = kLog2e * 0.08838834764831845f;
+  }
+  // An fp32 row.  fp16 terms are taken of the row scaled by a power of two that
+  // puts its largest element just below 2^14, so that any fp32 query fits and the second term keeps its bits.
+  __device__ __forceinline__ void load(const float* q, int h) {
+    float f[8][8];
+    float big = 0.f;
+#pragma unroll
+    for (int s = 0; s < 8; ++s) {
+      const f32x4 a = *reinterpret_cast<const f32x4*>(q + 16 * s + 8 * h), b = *reinterpret_cast<const f32x4*>(q + 16 * s + 8 * h + 4);
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        f[s][c] = a[c];
+        f[s][4 + c] = b[c];
+      }
+#pragma unroll
+      for (int c = 0; c < 8; ++c) big = fmaxf(big, fabsf(f[s][c]));
+    }
+    unit = kLog2e * 0.08838834764831845f;
+    float up = 1.f;
+    if constexpr (std::is_same<Op, f16x8>::value) {
+      big = fmaxf(big, __shfl_xor(big, 32));
+      int e = 0;
+      if (big > 0.f && big < INFINITY) e = 14 - (((__float_as_int(big) >> 23) & 255) - 126);
+      e = e > 100 ? 100 : e;                                   // (2^e and its inverse stay normal; below 2^-86 a row scores 0 in any case)
+      up = __int_as_float((127 + e) << 23);
+      unit *= __int_as_float((127 - e) << 23);
+    }
+#pragma unroll
+    for (int s = 0; s < 8; ++s)
+#pragma unroll
+      for (int c = 0; c < 8; c += 2) {
+        f32x2t y = {f[s][c] * up, f[s][c + 1] * up};
+#pragma unroll
+        for (int t = 0; t < kTerms; ++t) {
+          if constexpr (std::is_same<Op, bf16x8>::value) {
+            const bf16x2t z = __builtin_convertvector(y, bf16x2t);
+            x[t][s][c] = z[0];
+            x[t][s][c + 1] = z[1];
+            y[0] -= (float)z[0];
+            y[1] -= (float)z[1];
+          } else {
+            const _Float16 z0 = (_Float16)y[0], z1 = (_Float16)y[1];
+            x[t][s][c] = z0;
+            x[t][s][c + 1] = z1;
+            y[0] -= (float)z0;
+            y[1] -= (float)z1;
+          }
+        }
+      }
+  }
+};
+template <int kTerms>
+struct QueryTile<float, kTerms> {
+  f32x4 x[16];
+  float unit;
+  __device__ __forceinline__ void load(const float* q, int h) {
+#pragma unroll
+    for (int s = 0; s < 16; ++s) x[s] = *reinterpret_cast<const f32x4*>(q + 8 * s + 4 * h);
+    unit = kLog2e * 0.08838834764831845f;
+  }
+};
+
+// ---- the state of a wave's 32 rows ----------------------------------------------------------------------------
+// kTerms: 16-bit terms of the weights (1: rounded to 16 bits, as the output will be; 2: fp32 results).  An fp32 query is the sum of
+// query_terms of them: three of bf16, which hold it whole (two leave 2^-18 of every element, and the error of a score grows with it:
+// 3e-6 of the output instead of 1e-6 where a few rows carry most of the weight), two of fp16 (2^-22 is left).
+template <typename Op, int kTerms>
+constexpr int query_terms() { return kTerms == 1 ? 1 : (std::is_same<Op, bf16x8>::value ? 3 : 2); }
+template <typename Op, int kTerms>
+struct RowState {
+  typedef QueryTile<Op, query_terms<Op, kTerms>()> Query;
+  static constexpr bool kF32 = std::is_same<Op, float>::value;
+  // Weights of fp16 values are held 2^14 (2^8 with one term) times as large, or those below 2^-24 of the row's largest would be lost.
+  static constexpr float kLift = std::is_same<Op, f16x8>::value ? (kTerms == 1 ? 8.f : 14.f) : 0.f;
+  f32x16 o[4];                               // channels 32 d + 8 (r / 4) + 4 h + r % 4 of row n
+  float m, l;                                // largest score so far, in powers of two; the sum of the weights of my half's keys
+
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) o[d][r] = 0.f;
+    m = -INFINITY;
+    l = 0.f;
+  }
+
+  // Scores of the 32 keys whose rows begin at `k`.
+  __device__ __forceinline__ static f32x16 scores(const char* k, const Query& q, int n, int h) {
+    f32x16 s;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s[r] = 0.f;
+    if constexpr (kF32) {
+#pragma unroll
+      for (int c = 0; c < 16; ++c) {
+        const f32x4 a = *reinterpret_cast<const f32x4*>(k + n * 512 + 16 * chunk_place(n, 2 * c + h));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s = mfma32(a[i], q.x[c][i], s);
+      }
+    } else {
+#pragma unroll
+      for (int c = 0; c < 8; ++c) {
+        const Op a = *reinterpret_cast<const Op*>(k + n * 256 + 16 * chunk_place(n, 2 * c + h));
+#pragma unroll
+        for (int t = query_terms<Op, kTerms>() - 1; t >= 0; --t) s = mfma32(a, q.x[t][c], s);
+      }
+    }
+    return s;
+  }
+
+  // The eight values that lane (n, h) puts into the second product's step t (keys 16 t .. + 15 of those at `v`), channel block d.
+  __device__ __forceinline__ static Op values(const char* v, int t, int d, int lane) {
+    const int h = lane >> 5, i = lane & 15, key = 16 * t + 4 * h + (i >> 2), chunk = 4 * d + 2 * ((lane >> 4) & 1) + ((i & 3) >> 1);
+    typedef __attribute__((address_space(3))) s16x4* Lds;
+    union {
+      s16x4 half[2];
+      Op op;
+    } x;
+    x.half[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(v + key * 256 + 16 * chunk_place(key, chunk) + 8 * (i & 1)));
+    x.half[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(v + (key + 8) * 256 + 16 * chunk_place(key + 8, chunk) + 8 * (i & 1)));
+    return x.op;
+  }
+
+  // One step of kBlocks * 32 keys: scores s (products) -> weights, sums and values.  first: position of the first key; limit: the
+  // keys that row n sees; masked: some row of the wave sees fewer than all of these.
+  template <int kBlocks>
+  __device__ __forceinline__ void step(f32x16 (&s)[kBlocks], const char* v, float unit, int first, int limit, bool masked, int lane) {
+    const int h = lane >> 5, n = lane & 31;
+    float mx = m;
+#pragma unroll
+    for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        s[b][r] *= unit;
+        if (masked && first + 32 * b + 8 * (r / 4) + 4 * h + r % 4 >= limit) s[b][r] = -INFINITY;
+        mx = fmaxf(mx, s[b][r]);
+      }
+    mx = fmaxf(mx, __shfl_xor(mx, 32));
+    const float at = mx == -INFINITY ? 0.f : mx - kLift;       // (a row that has seen nothing yet: weights 0, not NaN)
+    const float shrink = mx == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mx);
+    m = mx;
+    l *= shrink;
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) o[d][r] *= shrink;
+#pragma unroll
+    for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        s[b][r] = __builtin_amdgcn_exp2f(s[b][r] - at);
+        l += s[b][r];
+      }
+#pragma unroll
+    for (int b = 0; b < kBlocks; ++b) add_values(s[b], v + 32 * b * InLds<typename std::conditional<kF32, float, uint16_t>::type>::kRowBytes, lane);
+  }
+
+  // o += weights of 32 keys times their values
+  __device__ __forceinline__ void add_values(const f32x16& p, const char* v, int lane) {
+    if constexpr (kF32) {
+      const int h = lane >> 5, n = lane & 31;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int key = 8 * (r / 4) + 4 * h + r % 4;
+#pragma unroll
+        for (int d = 0; d < 4; ++d) {
+          const int c = 32 * d + n;
+          o[d] = mfma32(*reinterpret_cast<const float*>(v + key * 512 + 16 * chunk_place(key, c >> 2) + 4 * (c & 3)), p[r], o[d]);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        Op w[kTerms];
+#pragma unroll
+        for (int i = 0; i < 8; i += 2) {
+          f32x2t y = {p[8 * t + i], p[8 * t + i + 1]};
+#pragma unroll
+          for (int u = 0; u < kTerms; ++u) {
+            if constexpr (std::is_same<Op, bf16x8>::value) {
+              const bf16x2t z = __builtin_convertvector(y, bf16x2t);
+              w[u][i] = z[0];
+              w[u][i + 1] = z[1];
+              y[0] -= (float)z[0];
+              y[1] -= (float)z[1];
+            } else {
+              const _Float16 z0 = (_Float16)y[0], z1 = (_Float16)y[1];
+              w[u][i] = z0;
+              w[u][i + 1] = z1;
+              y[0] -= (float)z0;
+              y[1] -= (float)z1;
+            }
+          }
+        }
+#pragma unroll
+        for (int d = 0; d < 4; ++d) {
+          const Op a = values(v, t, d, lane);
+#pragma unroll
+          for (int u = kTerms - 1; u >= 0; --u) o[d] = mfma32(a, w[u], o[d]);
+        }
+      }
+    }
+  }
+};
+
+// LDS of one workgroup: two stages of kRows rows of K and of V.
+template <typename T>
+constexpr int stage_bytes(int rows) { return rows * InLds<T>::kRowBytes; }
+constexpr int tile_rows(int key_waves) { return key_waves == 4 ? 128 : 64; }
+constexpr int kJoinRow = kD + 4;             // floats of a row whose key waves' results are added up in LDS
+template <typename TK, typename TV, int kKeyWaves>
+constexpr int tile_lds() {
+  const int stages = 2 * (stage_bytes<TK>(tile_rows(kKeyWaves)) + stage_bytes<TV>(tile_rows(kKeyWaves))), join = kKeyWaves > 1 ? 4 * 32 * kJoinRow * 4 : 0;
+  return stages > join ? stages : join;
+}
+// Few rows: all four waves share the keys of one tile of 32 rows; two tiles of fp32, whose stages are twice as large.
+template <typename T>
+constexpr int few_key_waves() { return sizeof(T) == 4 ? 2 : 4; }
+
+// The loop of a workgroup whose four waves are kRowWaves rows of waves (32 query rows each) by kKeyWaves (which share a stage's
+// keys).  q, limit: my query row's operand and the keys it sees.  wave_limit: the most that a row of my wave sees, and least.
+template <typename TK, typename TV, typename Op, int kTerms, int kKeyWaves>
+__device__ __forceinline__ void tile_loop(char* lds, const CacheRows<TK>& K, const CacheRows<TV>& V, int first, int end,
+                                          const typename RowState<Op, kTerms>::Query& q, int limit, RowState<Op, kTerms>& st) {
+  constexpr int kRows = tile_rows(kKeyWaves), kBlocks = kRows / 32 / kKeyWaves;
+  constexpr int kStageK = stage_bytes<TK>(kRows), kStage = kStageK + stage_bytes<TV>(kRows);
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int n = lane & 31, h = lane >> 5, mine = (wave % kKeyWaves) * kBlocks * 32;
+  int most = limit, least = limit;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    most = max(most, __shfl_xor(most, d));
+    least = min(least, __shfl_xor(least, d));
+  }
+  most = __builtin_amdgcn_readfirstlane(most);
+  least = __builtin_amdgcn_readfirstlane(least);
+  Staged<TK, kRows> sk;
+  Staged<TV, kRows> sv;
+  sk.look_up(K, first, end, tid);
+  sv.look_up(V, first, end, tid);
+  sk.load(K, first, end, tid);
+  sv.load(V, first, end, tid);
+  sk.look_up(K, first + kRows, end, tid);
+  sv.look_up(V, first + kRows, end, tid);
+  sk.store(lds, first, end, tid);
+  sv.store(lds + kStageK, first, end, tid);
+  int at = 0;
+  for (int k0 = first; k0 < end; k0 += kRows, at ^= 1) {
+    const bool more = k0 + kRows < end;
+    if (more) {
+      sk.load(K, k0 + kRows, end, tid);
+      sv.load(V, k0 + kRows, end, tid);
+      sk.look_up(K, k0 + 2 * kRows, end, tid);
+      sv.look_up(V, k0 + 2 * kRows, end, tid);
+    }
+    __syncthreads();                          // this stage is written, and nobody reads the other one any more
+    const int k_mine = k0 + mine;
+    if (k_mine < most) {
+      const char* k = lds + at * kStage + mine * InLds<TK>::kRowBytes;
+      const char* v = lds + at * kStage + kStageK + mine * InLds<TV>::kRowBytes;
+      f32x16 s[kBlocks];
+#pragma unroll
+      for (int b = 0; b < kBlocks; ++b) s[b] = RowState<Op, kTerms>::scores(k + 32 * b * InLds<TK>::kRowBytes, q, n, h);
+      st.template step<kBlocks>(s, v, q.unit, k_mine, limit, k_mine + 32 * kBlocks > least, lane);
+    }
+    if (more) {
+      sk.store(lds + (at ^ 1) * kStage, k0 + kRows, end, tid);
+      sv.store(lds + (at ^ 1) * kStage + kStageK, k0 + kRows, end, tid);
+    }
+  }
+}
+
+// Where a row's result goes: the output row, or a partial.  Both null: nowhere.
+template <typename TO>
+struct RowOut {
+  TO* out;
+  float* part;
+};
+__device__ __forceinline__ void put4(float* p, f32x4 x) { *reinterpret_cast<f32x4*>(p) = x; }
+__device__ __forceinline__ void put4(uint16_t* p, f32x4 x) {
+  typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+  *reinterpret_cast<bf16x4*>(p) = __builtin_convertvector(x, bf16x4);
+}
+__device__ __forceinline__ void put4(_Float16* p, f32x4 x) {
+  typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
+  *reinterpret_cast<f16x4*>(p) = __builtin_convertvector(x, f16x4);
+}
+
+// The results of a workgroup's rows, after its loop.  All threads call; `to`: of my query row.  Key waves are added up in LDS first.
+template <typename Op, int kTerms, int kKeyWaves, typename TO>
+__device__ __forceinline__ void tile_finish(char* lds, RowState<Op, kTerms>& st, RowOut<TO> to) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 31, h = lane >> 5;
+  st.l += __shfl_xor(st.l, 32);
+  if constexpr (kKeyWaves > 1) {
+    constexpr int kRow = kJoinRow;
+    float* mine = reinterpret_cast<float*>(lds) + (wave * 32 + n) * kRow;
+    __syncthreads();                          // (the stages have been read)
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; r += 4)
+        *reinterpret_cast<f32x4*>(mine + 32 * d + 2 * r + 4 * h) = f32x4{st.o[d][r], st.o[d][r + 1], st.o[d][r + 2], st.o[d][r + 3]};
+    if (h == 0) {
+      mine[kD] = st.m;
+      mine[kD + 1] = st.l;
+    }
+    __syncthreads();
+    // wave w of its row of waves makes the channel block(s) w * 4 / kKeyWaves ..
+    const float* rows = reinterpret_cast<const float*>(lds) + ((wave / kKeyWaves) * kKeyWaves * 32 + n) * kRow;
+    float mx = -INFINITY, f[kKeyWaves], ls = 0.f;
+#pragma unroll
+    for (int w = 0; w < kKeyWaves; ++w) mx = fmaxf(mx, rows[w * 32 * kRow + kD]);
+#pragma unroll
+    for (int w = 0; w < kKeyWaves; ++w) {
+      const float mw = rows[w * 32 * kRow + kD];
+      f[w] = mw == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mw - mx);
+      ls = fmaf(rows[w * 32 * kRow + kD + 1], f[w], ls);
+    }
+    st.m = mx;
+    st.l = ls;
+    constexpr int kMine = 4 / kKeyWaves;
+#pragma unroll
+    for (int j = 0; j < kMine; ++j) {
+      const int d = (wave % kKeyWaves) * kMine + j;
+#pragma unroll
+      for (int r = 0; r < 16; r += 4) {
+        f32x4 a = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < kKeyWaves; ++w) {
+          const f32x4 x = *reinterpret_cast<const f32x4*>(rows + w * 32 * kRow + 32 * d + 2 * r + 4 * h);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) a[i] = f[w] == 0.f ? a[i] : fmaf(x[i], f[w], a[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) st.o[j][r + i] = a[i];
+      }
+    }
+  }
+  constexpr int kMine = 4 / kKeyWaves;
+  const int d0 = (wave % kKeyWaves) * kMine;
+  const float inv = st.l == 0.f ? 0.f : 1.f / st.l;
+#pragma unroll
+  for (int j = 0; j < kMine; ++j)
+#pragma unroll
+    for (int r = 0; r < 16; r += 4) {
+      const int c = 32 * (d0 + j) + 2 * r + 4 * h;
+      const f32x4 x = {st.o[j][r], st.o[j][r + 1], st.o[j][r + 2], st.o[j][r + 3]};
+      if (to.part) put4(to.part + c, x);
+      else if (to.out) put4(to.out + c, f32x4{x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv});
+    }
+  if (to.part && h == 0 && d0 == 0) {
+    to.part[kD] = st.m;
+    to.part[kD + 1] = st.l;
+  }
+}
+
+// sum over n parts of a row, four channels a lane (32 lanes a row); parts whose largest score is -inf hold nothing.
+__device__ __forceinline__ f32x4 merge_parts(const float* part, int n, int lane32) {
+  float mx = -INFINITY;
+  for (int i = 0; i < n; ++i) mx = fmaxf(mx, part[(int64_t)i * kPartFloats + kD]);
+  f32x4 a = {0.f, 0.f, 0.f, 0.f};
+  float l = 0.f;
+  for (int i = 0; i < n; ++i) {
+    const float* p = part + (int64_t)i * kPartFloats;
+    const float m = p[kD];
+    if (m == -INFINITY) continue;
+    const float f = __builtin_amdgcn_exp2f(m - mx);
+    const f32x4 x = *reinterpret_cast<const f32x4*>(p + 4 * lane32);
+    l = fmaf(p[kD + 1], f, l);
+#pragma unroll
+    for (int c = 0; c < 4; ++c) a[c] = fmaf(x[c], f, a[c]);
+  }
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  return f32x4{a[0] * inv, a[1] * inv, a[2] * inv, a[3] * inv};
+}
+
+// Part `split` of n of the rows [first, end): whole stages, and no part smaller than two of them while another has rows.
+__device__ __forceinline__ void split_rows(int first, int end, int n, int split, int stage, int* lo, int* hi) {
+  int per = (end - first + n - 1) / n;
+  per = (per + stage - 1) / stage * stage;
+  per = per < 2 * stage ? 2 * stage : per;
+  const int64_t at = first + (int64_t)split * per;
+  *lo = at < end ? (int)at : end;
+  *hi = at + per < end ? (int)(at + per) : end;
+}
+
+// The last i in [0, n] with start(i) <= x, for a rising start with start(0) <= x: 64 places a round, by the whole wave.
+template <typename Start>
+__device__ __forceinline__ int last_not_above(int n, int x, Start start) {
+  const int lane = threadIdx.x & 63;
+  int lo = 0, span = n + 1;
+  while (span > 1) {
+    const int step = (span + 63) >> 6;
+    const int i = lo + lane * step;
+    const int last = i < lo + span ? i : lo + span - 1;
+    const int got = __popcll(__ballot(i < lo + span && start(last) <= x));
+    const int to = lo + (got > 0 ? got - 1 : 0) * step;
+    span = lo + span - to < step ? lo + span - to : step;
+    lo = to;
+  }
+  return __builtin_amdgcn_readfirstlane(lo);
+}
+
+}  // namespace lfps

@@ -1,0 +1,115 @@
+"""Full attention of a batch whose groups share their first rows, against 64 bits."""
+import pytest
+import torch
+
+from tests.cache_case import CacheCase, D, attend64, ints
+from tests.harness import DEV
+
+pytestmark = pytest.mark.gpu
+
+
+def _tolerance(dtype, ref, weighted, dots, n):
+    """Query and weights as sums of 16-bit terms, of which at most 2^-18 (bf16) or 2^-22 (fp16) is left (fp32 caches: nothing); products and sums as
+    everywhere fp32, 2^-24 of the absolute sum a term; the scores' errors come twice (weights and their sum); the exponential 2^-21."""
+    left = {"f16": 2.0 ** -22, "f32": 0.0}.get(dtype, 2.0 ** -18)
+    return (2 * (left + 260 * 2.0 ** -24) * dots + 2 * left + 2.0 ** -21 + (n + 80) * 2.0 ** -24) * weighted + 1e-7
+
+
+def _check(c, starts, prefixes, q=None, scale=1.0):
+    """The shared rows are read from the group's first request: the others' hold NaN there."""
+    for i, p in enumerate(prefixes):
+        b0, b1 = starts[i], starts[i + 1]
+        p = max(0, min(p, c.lens[b0]))
+        for b in range(b0 + 1, b1):
+            m = min(p, c.lens[b])
+            nan = torch.full((m, c.Hkv, D), float("nan"), device=DEV)
+            c.put(c.K, b, 0, nan.to(c.kd))
+            c.put(c.V, b, 0, nan.to(c.vd))
+    q = scale * c.randn(c.B, c.Hq, D) if q is None else q
+    out = torch.full((c.B, c.Hq, D), 7.0, device=DEV)
+    c.ctx.lfps_prefix_attn_decode(q, c.kv, ints(starts), ints(prefixes), out)
+    inside = set()
+    for i, p in enumerate(prefixes):
+        b0, b1 = starts[i], starts[i + 1]
+        p = max(0, min(p, c.lens[b0]))
+        for b in range(b0, b1):
+            inside.add(b)
+            n = c.lens[b]
+            if n == 0:
+                assert torch.equal(out[b], torch.zeros_like(out[b]))
+                continue
+            m = min(p, n)
+            k, v = (torch.cat([c.values(x, b0, 0, m), c.values(x, b, m, n)], 1) for x in (c.K, c.V))
+            for h in range(c.Hq):
+                ref, weighted, dots = attend64(q[b, h:h + 1].double(), k[h // c.G], v[h // c.G])
+                err = (out[b, h].double() - ref[0]).abs()
+                assert bool((err <= _tolerance(c.dtype, ref, weighted, dots, n)[0]).all()), (b, h, float(err.max()))
+    for b in set(range(c.B)) - inside:
+        assert bool((out[b] == 7).all())
+    return q, out
+
+
+@pytest.mark.parametrize("layout", [0, 16, "rows", ("rows", 64)])
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32", "fp8k", "fp8v", "fp8kv"])
+def test_prefix_formats_and_layouts(dtype, layout):
+    c = CacheCase(dtype, 8, 2, [150, 101, 130, 70, 200, 65], layout, seed=1)
+    _check(c, [0, 3, 4, 6], [100, 0, 64])
+    c.ctx.close()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32", "f16"])
+@pytest.mark.parametrize("Hq,Hkv,members,prefix", [(1, 1, 1, 5), (4, 1, 8, 63), (4, 1, 9, 64), (2, 1, 33, 65), (1, 1, 70, 129), (4, 4, 40, 1), (4, 1, 33, 300), (8, 2, 16, 1025)])
+def test_prefix_members_and_heads(dtype, Hq, Hkv, members, prefix):
+    c = CacheCase(dtype, Hq, Hkv, [prefix + i % 5 for i in range(members)], seed=members)
+    _check(c, [0, members], [prefix])
+    c.ctx.close()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp8kv"])
+def test_prefix_long_and_ragged(dtype):
+    """Parts of the shared and of the own rows; members shorter than the prefix, empty ones, prefixes beyond the first member's rows."""
+    lens = [3000, 2500, 40, 0, 2999] + [700, 1900, 1, 650] + [500]
+    c = CacheCase(dtype, 8, 2, lens, 64, seed=3)
+    _check(c, [0, 5, 9, 10], [2600, 100000, -4])
+    c.ctx.close()
+
+
+def test_prefix_requests_in_no_group_are_left_alone():
+    c = CacheCase("bf16", 4, 2, [60] * 7, 16, seed=4)
+    _check(c, [1, 3, 3, 6], [50, 20, 33])
+    c.ctx.close()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("scale", [1e-30, 30.0, 1e4])
+def test_prefix_queries_of_any_size(dtype, scale):
+    """(fp16 terms: any fp32 query fits.)"""
+    c = CacheCase(dtype, 4, 2, [300, 280, 270], seed=5, scale=1.0 if scale < 100 else 1e-4)
+    _check(c, [0, 3], [256], scale=scale)
+    c.ctx.close()
+
+
+def test_prefix_of_one_request_is_full_attention():
+    """The same numbers as the plain call, to its precision and this one's."""
+    c = CacheCase("bf16", 8, 2, [777, 123], 16, seed=6)
+    q, out = _check(c, [0, 1, 2], [500, 0])
+    full = torch.zeros_like(out)
+    c.ctx.lfps_full_attn_decode(q, c.kv, full)
+    assert float((out - full).abs().max()) <= 2e-5 * float(full.abs().max().clamp_min(1))
+    c.ctx.close()
+
+
+def test_prefix_refusals():
+    from paper_2506_15704_amd.binding import LfpsError
+    c = CacheCase("bf16", 4, 2, [64, 64])
+    q, out = torch.zeros((2, 4, D), device=DEV), torch.zeros((2, 4, D), device=DEV)
+    ok = dict(q=q, kv=c.kv, group_start=ints([0, 2]), prefix_len=ints([8]), out=out)
+    for bad, err in ((dict(q=q.half()), TypeError), (dict(group_start=ints([0, 1, 2])), ValueError), (dict(out=out[:1]), ValueError),
+                     (dict(group_start=ints([0, 1, 2, 2]), prefix_len=ints([1, 1, 1])), LfpsError), (dict(group_start=ints([0]), prefix_len=ints([])), LfpsError),
+                     (dict(kv=c.ctx.kv_view(c.K, None, c.seq)), LfpsError)):
+        with pytest.raises(err):
+            c.ctx.lfps_prefix_attn_decode(**{**ok, **bad})
+    for starts in ([0, -5, 900], [2, 0, 1], [5, 9, 9]):      # no sense, but inside
+        c.ctx.lfps_prefix_attn_decode(q, c.kv, ints(starts), ints([70, 3]), out)
+    torch.cuda.synchronize()
+    c.ctx.close()
