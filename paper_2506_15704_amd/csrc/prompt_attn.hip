@@ -6,7 +6,7 @@
 // and streams the rows they see; bound by the matrix units.  k_prompt_few: a request whose tokens fill no more than one wave's
 // rows; the four waves share the keys, and the rows are cut into parts that are joined afterwards; bound by the bytes of K and V.
 // Which one takes a request is decided on the device by its number of tokens, so one call takes any mixture.
-#include "tile_attn.h"
+#include "tile_pipe.h"
 
 namespace lfps {
 
@@ -88,13 +88,64 @@ __device__ __forceinline__ void prompt_tile(char* lds, const PromptArgs<TQ>& a, 
   tile_finish<Op, 1, kKeyWaves>(lds, st, to);
 }
 
+// The same with the loop of tile_pipe.h.
+template <typename TK, typename TV, typename TQ>
+__device__ __forceinline__ void prompt_pipe(char* lds, const PromptArgs<TQ>& a, int b, int g, int c0, int c1, int row0, int split) {
+  typedef typename InLds<TK>::Op Op;
+  const Shape& s = a.s;
+  const int G = s.G, shift = G == 4 ? 2 : G - 1;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
+  const int n = length_of(s, a.kv.seq_lens, b), t = c1 - c0, rows = t << shift;
+  auto seen = [&](int token) {
+    const int pos = n - t + token + 1;
+    return pos < 0 ? 0 : pos;
+  };
+  const int last = (row0 + kPipeRows < rows ? row0 + kPipeRows : rows) - 1;
+  int lo, hi;
+  split_rows(0, seen(last >> shift), a.splits, split, kPipeKeys, &lo, &hi);
+  PipeState<Op> st;
+  st.clear();
+  int m = row0 + 32 * wave + (lane & 31);
+  const bool valid = m < rows;
+  m = valid ? m : rows - 1;                                     // (rows that are not there repeat the last one)
+  const int token = m >> shift, head = g * G + (m & (G - 1));
+  st.limit = seen(token);
+  if (lo < hi) {
+    st.q.load(a.q + (int64_t)(c0 + token) * a.q_stride + head * kD, h);
+    const CacheRows<TK> K(a.kv.k, a.kv, b, g);
+    const CacheRows<TV> V(a.kv.v, a.kv, b, g);
+    pipe_loop<TK, TV, Op>(lds, K, V, lo, hi, st);
+  }
+  if (!valid) return;
+  TQ* const out = a.out + ((int64_t)(c0 + token) * s.Hq + head) * kD;
+  float* const part = a.part + (part_row(a, false, 0, b, c0, token, head) + split) * kPartFloats;
+  const float l = st.l + __shfl_xor(st.l, 32), inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+  for (int d = 0; d < 4; ++d)
+#pragma unroll
+    for (int r = 0; r < 16; r += 4) {
+      const f32x4 y = {st.o[d][r], st.o[d][r + 1], st.o[d][r + 2], st.o[d][r + 3]};
+      const int c = 32 * d + 2 * r + 4 * h;
+      if (a.splits > 1) put4(part + c, y);
+      else put4(out + c, f32x4{y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv});
+    }
+  if (a.splits > 1 && h == 0) {
+    part[kD] = st.m;
+    part[kD + 1] = l;
+  }
+}
+
 }  // namespace
 
-// grid Hkv * splits * (tiles of all requests, at most T G / 128 + B), the latest rows of a request first: they see most
+template <typename TK>
+constexpr int tile_query_rows() { return kPipeRows; }      // of a workgroup of k_prompt_tiles
+
+// grid Hkv * splits * (tiles of all requests, at most T G / tile_query_rows + B), the latest rows of a request first: they see most
 template <typename TK, typename TV, typename TQ>
-__global__ __launch_bounds__(kTileThreads) void k_prompt_tiles(PromptArgs<TQ> a, int tiles) {
-  __shared__ __attribute__((aligned(16))) char lds[tile_lds<TK, TV, 1>()];
-  const int G = a.s.G, per = 128 / G;
+__global__ __launch_bounds__(kTileThreads, sizeof(TK) == 4 ? 1 : 2) void k_prompt_tiles(PromptArgs<TQ> a, int tiles) {
+  constexpr int kRows = tile_query_rows<TK>();
+  __shared__ __attribute__((aligned(16))) char lds[sizeof(TK) != 4 ? kPipeLds : tile_lds<TK, TV, 1>()];
+  const int G = a.s.G, per = kRows / G;
   const int g = blockIdx.x % a.s.Hkv, x0 = blockIdx.x / a.s.Hkv, split = x0 % a.splits, x = tiles - 1 - x0 / a.splits;
   // tile x is among those of the last request b with cu[b] / per + b <= x: a request has no more tiles than lie between
   auto first_tile = [&](int i) {
@@ -104,10 +155,11 @@ __global__ __launch_bounds__(kTileThreads) void k_prompt_tiles(PromptArgs<TQ> a,
   const int b = last_not_above(a.s.B - 1, x, first_tile);
   int c0, c1;
   tokens_of(a, b, &c0, &c1);
-  const int row0 = (x - first_tile(b)) * 128;
+  const int row0 = (x - first_tile(b)) * kRows;
   if (row0 < 0 || row0 >= (c1 - c0) * G) return;
   if (a.few_splits && (c1 - c0) * G <= few_most<TK>()) return;
-  prompt_tile<TK, TV, TQ, 1>(lds, a, b, g, c0, c1, row0, split);
+  if constexpr (sizeof(TK) != 4) prompt_pipe<TK, TV, TQ>(lds, a, b, g, c0, c1, row0, split);
+  else prompt_tile<TK, TV, TQ, 1>(lds, a, b, g, c0, c1, row0, split);
 }
 
 // grid Hkv * few_splits * B
@@ -160,7 +212,7 @@ hipError_t prompt_t(const Shape& s, const KvView& kv, const void* q, int64_t q_s
                     float* part, int64_t part_rows, hipStream_t st) {
   constexpr int kMost = few_most<TK>();
   PromptArgs<TQ> a = {s, kv, (const TQ*)q, q_stride, cu, n_tokens, (TQ*)out, part, 1, 0, 0, 0};
-  const int per = 128 / s.G;
+  const int per = tile_query_rows<TK>() / s.G;
   // As many parts as give every CU two workgroups, where the rows' partial results have room.
   auto parts = [&](int64_t groups, int64_t rows, int64_t room) {
     int64_t n = (512 + groups - 1) / groups;

@@ -243,7 +243,7 @@ struct RowState {
   // keys that row n sees; masked: some row of the wave sees fewer than all of these.
   template <int kBlocks>
   __device__ __forceinline__ void step(f32x16 (&s)[kBlocks], const char* v, float unit, int first, int limit, bool masked, int lane) {
-    const int h = lane >> 5, n = lane & 31;
+    const int h = lane >> 5;
     float mx = m;
 #pragma unroll
     for (int b = 0; b < kBlocks; ++b)
