@@ -89,8 +89,8 @@ __device__ __forceinline__ void prompt_tile(char* lds, const PromptArgs<TQ>& a, 
 }
 
 // The same with the loop of tile_pipe.h.
-template <typename TK, typename TV, typename TQ>
-__device__ __forceinline__ void prompt_pipe(char* lds, const PromptArgs<TQ>& a, int b, int g, int c0, int c1, int row0, int split) {
+template <int kKind, typename TK, typename TV, typename TQ>
+__device__ __forceinline__ void prompt_pipe(const PipeLds& lds, const PromptArgs<TQ>& a, int b, int g, int c0, int c1, int row0, int split) {
   typedef typename InLds<TK>::Op Op;
   const Shape& s = a.s;
   const int G = s.G, shift = G == 4 ? 2 : G - 1;
@@ -114,7 +114,7 @@ __device__ __forceinline__ void prompt_pipe(char* lds, const PromptArgs<TQ>& a, 
     st.q.load(a.q + (int64_t)(c0 + token) * a.q_stride + head * kD, h);
     const CacheRows<TK> K(a.kv.k, a.kv, b, g);
     const CacheRows<TV> V(a.kv.v, a.kv, b, g);
-    pipe_loop<TK, TV, Op>(lds, K, V, lo, hi, st);
+    pipe_loop<kKind, TK, TV, Op>(lds, K, V, lo, hi, st);
   }
   if (!valid) return;
   TQ* const out = a.out + ((int64_t)(c0 + token) * s.Hq + head) * kD;
@@ -138,13 +138,14 @@ __device__ __forceinline__ void prompt_pipe(char* lds, const PromptArgs<TQ>& a, 
 }  // namespace
 
 template <typename TK>
-constexpr int tile_query_rows() { return kPipeRows; }      // of a workgroup of k_prompt_tiles
+constexpr int tile_query_rows() { return sizeof(TK) == 4 ? 128 : kPipeRows; }      // of a workgroup of k_prompt_tiles
+template <typename TK>
+constexpr int tile_threads() { return sizeof(TK) == 4 ? kTileThreads : kPipeThreads; }
 
 // grid Hkv * splits * (tiles of all requests, at most T G / tile_query_rows + B), the latest rows of a request first: they see most
-template <typename TK, typename TV, typename TQ>
-__global__ __launch_bounds__(kTileThreads, sizeof(TK) == 4 ? 1 : 2) void k_prompt_tiles(PromptArgs<TQ> a, int tiles) {
+template <int kKind, typename TK, typename TV, typename TQ>
+__global__ __launch_bounds__(tile_threads<TK>(), sizeof(TK) == 4 ? 1 : 2) void k_prompt_tiles(PromptArgs<TQ> a, int tiles) {
   constexpr int kRows = tile_query_rows<TK>();
-  __shared__ __attribute__((aligned(16))) char lds[sizeof(TK) != 4 ? kPipeLds : tile_lds<TK, TV, 1>()];
   const int G = a.s.G, per = kRows / G;
   const int g = blockIdx.x % a.s.Hkv, x0 = blockIdx.x / a.s.Hkv, split = x0 % a.splits, x = tiles - 1 - x0 / a.splits;
   // tile x is among those of the last request b with cu[b] / per + b <= x: a request has no more tiles than lie between
@@ -158,8 +159,14 @@ __global__ __launch_bounds__(kTileThreads, sizeof(TK) == 4 ? 1 : 2) void k_promp
   const int row0 = (x - first_tile(b)) * kRows;
   if (row0 < 0 || row0 >= (c1 - c0) * G) return;
   if (a.few_splits && (c1 - c0) * G <= few_most<TK>()) return;
-  if constexpr (sizeof(TK) != 4) prompt_pipe<TK, TV, TQ>(lds, a, b, g, c0, c1, row0, split);
-  else prompt_tile<TK, TV, TQ, 1>(lds, a, b, g, c0, c1, row0, split);
+  if constexpr (sizeof(TK) == 4) {
+    __shared__ __attribute__((aligned(16))) char lds[tile_lds<TK, TV, 1>()];
+    prompt_tile<TK, TV, TQ, 1>(lds, a, b, g, c0, c1, row0, split);
+  } else {
+    __shared__ __attribute__((aligned(16))) char k0[kPipeStage], k1[kPipeStage], v0[kPipeStage], v1[kPipeStage];
+    const PipeLds lds = {{(lds_char*)k0, (lds_char*)k1}, {(lds_char*)v0, (lds_char*)v1}};
+    prompt_pipe<kKind, TK, TV, TQ>(lds, a, b, g, c0, c1, row0, split);
+  }
 }
 
 // grid Hkv * few_splits * B
@@ -231,8 +238,15 @@ hipError_t prompt_t(const Shape& s, const KvView& kv, const void* q, int64_t q_s
     a.few_by_token = n_tokens <= room;
     a.few_splits = parts((int64_t)(s.B < n_tokens ? s.B : n_tokens) * s.Hkv, (a.few_by_token ? n_tokens : room) * s.Hq, part_rows - a.few_part);
   }
-  if (!all_few)
-    hipLaunchKernelGGL((k_prompt_tiles<TK, TV, TQ>), dim3((unsigned)(s.Hkv * a.splits * tiles)), dim3(kTileThreads), 0, st, a, tiles);
+  const dim3 grid((unsigned)(s.Hkv * a.splits * tiles));
+  if (!all_few) {
+    const int kind = sizeof(TK) == 4 ? kAnyRows : rows_kind(kv);
+    if (kind == kAnyRows) hipLaunchKernelGGL((k_prompt_tiles<kAnyRows, TK, TV, TQ>), grid, dim3(tile_threads<TK>()), 0, st, a, tiles);
+    if constexpr (sizeof(TK) != 4) {
+      if (kind == kSlab) hipLaunchKernelGGL((k_prompt_tiles<kSlab, TK, TV, TQ>), grid, dim3(tile_threads<TK>()), 0, st, a, tiles);
+      if (kind == kPages) hipLaunchKernelGGL((k_prompt_tiles<kPages, TK, TV, TQ>), grid, dim3(tile_threads<TK>()), 0, st, a, tiles);
+    }
+  }
   if (!none_few)
     hipLaunchKernelGGL((k_prompt_few<TK, TV, TQ>), dim3((unsigned)(s.Hkv * a.few_splits * s.B)), dim3(kTileThreads), 0, st, a);
   auto merge = [&](int few, int64_t rows) {

@@ -44,9 +44,14 @@ struct CacheRows {
 };
 
 // ---- the elements in LDS and in the matrix instructions ------------------------------------------------------
-// A row in LDS is kRowBytes long, in chunks of 16 bytes; chunk c of row r lies at place c ^ 2 (r & 7) of the row, so that eight
-// consecutive rows read at one chunk (scores), and four rows read at two neighbouring chunks (values), touch all banks evenly.
-__device__ __forceinline__ int chunk_place(int r, int c) { return c ^ (2 * (r & 7)); }
+// A row in LDS is kRowBytes long, in chunks of 16 bytes; chunk c of row r lies at place c ^ mix(r) of the row.  The LDS has 64 banks of
+// four bytes, which is 16 chunks: sixteen consecutive rows read at one chunk (scores), and four rows at four neighbouring chunks (16-bit
+// values), come from different ones.  (With c ^ 2 (r & 7), whose eight places serve half of that, the LDS took twice as long.)
+__device__ __forceinline__ int mix(int r) { return ((r & 3) << 2) | ((r >> 2) & 3); }
+// fp32 values are read along a row, in two rows four apart at once.
+__device__ __forceinline__ int mix_f32(int r) { return (r & 3) | ((r & 4) << 1) | ((r & 8) >> 1); }
+__device__ __forceinline__ int chunk_place(int r, int c) { return c ^ mix(r); }
+__device__ __forceinline__ int chunk_place_f32(int r, int c) { return c ^ mix_f32(r); }
 
 template <typename T>
 struct InLds { typedef bf16x8 Op; static constexpr int kRowBytes = 256; };       // bf16, and FP8 (every value is a bf16 value)
@@ -98,7 +103,7 @@ struct Staged {
         *reinterpret_cast<bf16x8*>(at + 16 * chunk_place(r, 2 * c)) = fp8x8_to_bf16x8(w[0], w[1]);
         *reinterpret_cast<bf16x8*>(at + 16 * chunk_place(r, 2 * c + 1)) = fp8x8_to_bf16x8(w[2], w[3]);
       } else {
-        *reinterpret_cast<u32x4*>(at + 16 * chunk_place(r, c)) = w;
+        *reinterpret_cast<u32x4*>(at + 16 * (sizeof(T) == 4 ? chunk_place_f32(r, c) : chunk_place(r, c))) = w;
       }
     }
   }
@@ -211,7 +216,7 @@ struct RowState {
     if constexpr (kF32) {
 #pragma unroll
       for (int c = 0; c < 16; ++c) {
-        const f32x4 a = *reinterpret_cast<const f32x4*>(k + n * 512 + 16 * chunk_place(n, 2 * c + h));
+        const f32x4 a = *reinterpret_cast<const f32x4*>(k + n * 512 + 16 * chunk_place_f32(n, 2 * c + h));
 #pragma unroll
         for (int i = 0; i < 4; ++i) s = mfma32(a[i], q.x[c][i], s);
       }
@@ -283,7 +288,7 @@ struct RowState {
 #pragma unroll
         for (int d = 0; d < 4; ++d) {
           const int c = 32 * d + n;
-          o[d] = mfma32(*reinterpret_cast<const float*>(v + key * 512 + 16 * chunk_place(key, c >> 2) + 4 * (c & 3)), p[r], o[d]);
+          o[d] = mfma32(*reinterpret_cast<const float*>(v + key * 512 + 16 * chunk_place_f32(key, c >> 2) + 4 * (c & 3)), p[r], o[d]);
         }
       }
     } else {
