@@ -90,7 +90,7 @@ __device__ __forceinline__ void prompt_tile(char* lds, const PromptArgs<TQ>& a, 
 
 // The same with the loop of tile_pipe.h.
 template <int kKind, typename TK, typename TV, typename TQ>
-__device__ __forceinline__ void prompt_pipe(const PipeLds& lds, const PromptArgs<TQ>& a, int b, int g, int c0, int c1, int row0, int split) {
+__device__ __forceinline__ void prompt_pipe(char* lds, const PromptArgs<TQ>& a, int b, int g, int c0, int c1, int row0, int split) {
   typedef typename InLds<TK>::Op Op;
   const Shape& s = a.s;
   const int G = s.G, shift = G == 4 ? 2 : G - 1;
@@ -163,8 +163,7 @@ __global__ __launch_bounds__(tile_threads<TK>(), sizeof(TK) == 4 ? 1 : 2) void k
     __shared__ __attribute__((aligned(16))) char lds[tile_lds<TK, TV, 1>()];
     prompt_tile<TK, TV, TQ, 1>(lds, a, b, g, c0, c1, row0, split);
   } else {
-    __shared__ __attribute__((aligned(16))) char k0[kPipeStage], k1[kPipeStage], v0[kPipeStage], v1[kPipeStage];
-    const PipeLds lds = {{(lds_char*)k0, (lds_char*)k1}, {(lds_char*)v0, (lds_char*)v1}};
+    __shared__ __attribute__((aligned(16))) char lds[kPipeLds];
     prompt_pipe<kKind, TK, TV, TQ>(lds, a, b, g, c0, c1, row0, split);
   }
 }

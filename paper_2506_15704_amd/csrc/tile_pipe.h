@@ -24,71 +24,46 @@ __device__ __forceinline__ int wave_of() { return __builtin_amdgcn_readfirstlane
 
 // The rows of a stage that a wave brings, eight, of K or V.  16-bit elements go from memory to LDS without
 // registers, four rows an instruction: lane l fills place l % 16 of row l / 16, so it asks for the chunk that belongs there.
-// Rows from `end` on are the last one again: they are read by nobody's weights but 0.  The block table's entries are asked for a
-// stage ahead.
+// Rows from `end` on are the last one again, also whole stages of them: they are read by nobody's weights but 0.
+// aim works out where a stage's rows lie, ask asks for them: the one is scalar work for when there is time, the other a few instructions.
 template <typename T, int kKind>
 struct Feed {
   static constexpr bool kDirect = sizeof(T) == 2;
   static constexpr int kLoads = kFeedRows / (kDirect ? 4 : 8);     // FP8: eight rows a load, through registers
-  static constexpr int kEntries = kKind == kAnyRows ? kLoads : 1;
   u32x4 x[kDirect ? 1 : kLoads];
-  int entry[kEntries];
-  uint32_t whole[kLoads];                            // my pieces' places where all of the rows are there
-
-  __device__ __forceinline__ void begin(const CacheRows<T>& c, int lane) {
-#pragma unroll
-    for (int i = 0; i < kLoads; ++i) whole[i] = place(c, row(i, lane), i, lane);
-  }
-  __device__ __forceinline__ static uint32_t place(const CacheRows<T>& c, int r, int i, int lane) {
-    return __umul24((uint32_t)r, (uint32_t)c.stride_n * (uint32_t)sizeof(T)) + (uint32_t)piece(i, lane);    // (a pitch below 2^24)
-  }
+  const char* base;                                  // the wave's first row
+  uint32_t off[kLoads];                              // my pieces from there
+  const char* from[kKind == kAnyRows ? kLoads : 1];  // kAnyRows: my pieces
 
   __device__ __forceinline__ static int row(int i, int lane) { return kFeedRows / kLoads * i + (kDirect ? lane >> 4 : lane >> 3); }
   __device__ __forceinline__ static int piece(int i, int lane) {                  // of a row of the cache, in bytes
-    return kDirect ? 16 * ((lane & 15) ^ mix((kFeedRows * wave_of()) + row(i, lane))) : 16 * (lane & 7);
+    return kDirect ? 16 * ((lane & 15) ^ mix(kFeedRows * wave_of() + row(i, lane))) : 16 * (lane & 7);
   }
-  // The wave's first row of the stage, one that exists.
-  __device__ __forceinline__ static int first_row(int k0, int end, int wave) {
-    const int w0 = k0 + kFeedRows * wave;
-    return __builtin_amdgcn_readfirstlane(w0 < end ? w0 : (end - 1) & ~(kFeedRows - 1));
-  }
-  __device__ __forceinline__ void look_up(const CacheRows<T>& c, int k0, int end, int lane, int wave) {
-    if (kKind == kSlab || !c.pg.table) return;
-    const int w0 = first_row(k0, end, wave), last = end - 1 - w0;
-#pragma unroll
-    for (int i = 0; i < kEntries; ++i) {
-      const int r = kKind == kPages ? 0 : row(i, lane);
-      entry[i] = RowMap<true>::block(c.pg, c.b, w0 + (r < last ? r : last));
-    }
-  }
-  __device__ __forceinline__ void one(const char* from, lds_char* stage, int i, int wave) {
-    if constexpr (kDirect)
-      __builtin_amdgcn_global_load_lds((global_char*)from, (__attribute__((address_space(3))) void*)(stage + (kFeedRows * wave + 4 * i) * 256), 16, 0, 0);
-    else
-      x[i] = *reinterpret_cast<const u32x4*>(from);
-  }
-  __device__ __forceinline__ void ask(const CacheRows<T>& c, lds_char* stage, int k0, int end, int lane, int wave) {
-    const int w0 = first_row(k0, end, wave), last = end - 1 - w0;
+  // entry: of the block table, for the wave's first row (first_row; kAnyRows looks its own up)
+  __device__ __forceinline__ void aim(const CacheRows<T>& c, int w0, int end, int entry, int lane) {
+    const int last = end - 1 - w0;
     if constexpr (kKind == kAnyRows) {
 #pragma unroll
       for (int i = 0; i < kLoads; ++i) {
-        const int r = row(i, lane);
-        one(reinterpret_cast<const char*>(c.at(w0 + (r < last ? r : last), entry[i])) + piece(i, lane), stage, i, wave);
+        const int r = w0 + min(row(i, lane), last);
+        from[i] = reinterpret_cast<const char*>(c.at(r, c.entry(r))) + piece(i, lane);
       }
     } else {
-      const int64_t first = kKind == kPages ? RowMap<true>::offset_in(c.pg, __builtin_amdgcn_readfirstlane(entry[0]), w0, c.stride_b, c.stride_n)
-                                            : w0 * c.stride_n;
-      const char* base = reinterpret_cast<const char*>(c.base + first);
-      if (last >= kFeedRows - 1) {
+      const int64_t first = kKind == kPages ? RowMap<true>::offset_in(c.pg, entry, w0, c.stride_b, c.stride_n) : w0 * c.stride_n;
+      base = reinterpret_cast<const char*>(c.base + first);
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i) one(base + whole[i], stage, i, wave);
-      } else {
+      for (int i = 0; i < kLoads; ++i)
+        off[i] = __umul24((uint32_t)min(row(i, lane), last), (uint32_t)c.stride_n * (uint32_t)sizeof(T)) + (uint32_t)piece(i, lane);
+    }
+  }
+  __device__ __forceinline__ void ask(lds_char* stage, int wave) {
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-          const int r = row(i, lane);
-          one(base + place(c, r < last ? r : last, i, lane), stage, i, wave);
-        }
-      }
+    for (int i = 0; i < kLoads; ++i) {
+      const char* p = kKind == kAnyRows ? from[i] : base + off[i];
+      if constexpr (kDirect)
+        __builtin_amdgcn_global_load_lds((global_char*)p, (__attribute__((address_space(3))) void*)(stage + (kFeedRows * wave + 4 * i) * 256), 16, 0, 0);
+      else
+        x[i] = *reinterpret_cast<const u32x4*>(p);
     }
   }
   // FP8: what has arrived becomes bf16 in the stage
@@ -104,6 +79,11 @@ struct Feed {
     }
   }
 };
+// The first row that a wave brings of the stage at k0: one that exists.
+__device__ __forceinline__ int first_row(int k0, int end, int wave) {
+  const int w0 = k0 + kFeedRows * wave;
+  return __builtin_amdgcn_readfirstlane(w0 < end ? w0 : (end - 1) & ~(kFeedRows - 1));
+}
 
 // 32 query rows of a wave.
 template <typename Op>
@@ -216,125 +196,106 @@ struct PipeState {
   }
 };
 
-// The loop.  Stage j: scores of j + 1 beside the weights of j, then the values of j.  In LDS are K of two stages and V of two; what
-// a stage has read is asked for again at its end, K three stages ahead and V one, and has arrived behind the first half of the next:
-// one barrier a stage, between its weights and its values.  (Transposed reads from LDS wait for everything that is on its way there, so
-// nothing may be asked for between a barrier and the values' reads.)
-// The order inside a stage is written down in groups of four products: the operands of the next group are read first, and every
-// product has its share of the vector work beside it; left to itself the compiler reads an operand just before its product.
-constexpr int kPipeStage = kPipeKeys * 256;
-struct PipeLds {
-  lds_char* k[2];
-  lds_char* v[2];
-};
-// Four products, each followed by kVector vector instructions, and kReads reads from LDS ahead of them.
-template <int kReads, int kVector>
-__device__ __forceinline__ void group_order() {
-  __builtin_amdgcn_sched_group_barrier(0x100, kReads, 0);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
-    __builtin_amdgcn_sched_group_barrier(0x2, kVector, 0);
-  }
-  __builtin_amdgcn_sched_barrier(0);
-}
+// The loop.  A stage has a half for the vector units (its scores become weights) and a half for the matrix units (its values, then the
+// scores of the next stage).  Waves 0-3 are half a stage ahead of waves 4-7, with which they share the SIMDs: while one of a SIMD's
+// two waves keeps the matrix unit, the other has the vector unit.  A barrier ends every half.
+//
+// While a wave keeps the matrix unit full, the other one of the SIMD hardly gets a request to memory out (280 cycles each, against 22
+// beside a wave that does anything else): all requests are made in matrix halves, between the products.  They are for K two stages ahead and V one
+// (of j: K of j + 3 and V of j + 2, counted from the weights that are in use), so in LDS are three stages of either; the places were last
+// read at least a half before, and what was asked for has arrived at the end of the wave's next vector half, a half before anyone
+// reads it.  (Transposed reads from LDS wait for everything that is on its way there: requests come behind a matrix half's last.)
+//
+// A matrix half is eight groups of four products; the operands of the group after the next are read before a group's products,
+// those of the first two before the barrier.
+constexpr int kPipeStage = kPipeKeys * 256, kPipeStages = 3, kPipeLds = 2 * kPipeStages * kPipeStage;
 template <int kKind, typename TK, typename TV, typename Op>
-__device__ __forceinline__ void pipe_loop(const PipeLds lds, const CacheRows<TK>& K, const CacheRows<TV>& V, int first, int end,
+__device__ __forceinline__ void pipe_loop(char* lds_, const CacheRows<TK>& K, const CacheRows<TV>& V, int first, int end,
                                           PipeState<Op>& st) {
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 31, h = lane >> 5;
+  lds_char* const lds = (lds_char*)lds_;
+  const int lane = threadIdx.x & 63, wave = wave_of(), n = lane & 31, h = lane >> 5;
   int least = st.limit;
 #pragma unroll
   for (int d = 1; d < 32; d <<= 1) least = min(least, __shfl_xor(least, d));
   least = __builtin_amdgcn_readfirstlane(least);
+  const bool late = wave >= kPipeWaves / 2;
   Feed<TK, kKind> fk;
   Feed<TV, kKind> fv;
-  auto arrived = [&] {
-    __builtin_amdgcn_s_waitcnt(0x0f70);       // vmcnt(0): what I asked for is in LDS
-    __syncthreads();                          // and what all did
-  };
-  auto ask_k = [&](lds_char* to, int k) {     // and the table's entries for the stage after it
-    if (k < end) fk.ask(K, to, k, end, lane, wave);
-    fk.look_up(K, k + kPipeKeys, end, lane, wave);
-  };
-  auto ask_v = [&](lds_char* to, int k) {
-    if (k < end) fv.ask(V, to, k, end, lane, wave);
-    fv.look_up(V, k + kPipeKeys, end, lane, wave);
-  };
-  fk.begin(K, lane);
-  fv.begin(V, lane);
-  fk.look_up(K, first, end, lane, wave);
-  fv.look_up(V, first, end, lane, wave);
-  ask_k(lds.k[0], first);
-  fk.put(lds.k[0], lane, wave);
-  ask_k(lds.k[1], first + kPipeKeys);
-  if (first + kPipeKeys < end) fk.put(lds.k[1], lane, wave);
-  ask_v(lds.v[0], first);
-  arrived();
-  f32x16 s[2][2];                             // scores of this stage and the next, by parity
-  {
-    Op a[4];
+  constexpr int kV = kPipeStages * kPipeStage;
+  auto row_of = [&](int k) { return first_row(k, end, wave); };
+  auto look_up = [&](int k) { return kKind == kPages ? RowMap<true>::block(K.pg, K.b, row_of(k)) : 0; };
+  auto uniform = [](int e) { return __builtin_amdgcn_readfirstlane(e); };
+  auto landed = [] { __builtin_amdgcn_s_waitcnt(0x0f70); };     // vmcnt(0): what I asked for is in LDS
 #pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      st.load_keys(a, lds.k[0], g, n, h);
-      st.add_scores(s[0], a, g);
+  for (int i = 0; i < 3; ++i) {                                  // K of the first three stages, V of two
+    const int k = first + i * kPipeKeys, e = uniform(look_up(k));
+    fk.aim(K, row_of(k), end, e, lane);
+    fk.ask(lds + i * kPipeStage, wave);
+    fk.put(lds + i * kPipeStage, lane, wave);
+    if (i < 2) {
+      fv.aim(V, row_of(k), end, e, lane);
+      fv.ask(lds + kV + i * kPipeStage, wave);
+      fv.put(lds + kV + i * kPipeStage, lane, wave);
     }
   }
+  int e_v = look_up(first + 2 * kPipeKeys), e_k = look_up(first + 3 * kPipeKeys), e_new = 0;      // of the next to be asked for
+  landed();
   __syncthreads();
-  ask_k(lds.k[0], first + 2 * kPipeKeys);
-  float mx = st.largest(s[0][1], st.largest(s[0][0], -INFINITY));     // of my scores of the stage (where nothing is hidden)
-  int k0 = first;
-  auto stage = [&](auto parity, auto masked) {
-    constexpr int P = decltype(parity)::value;
+  f32x16 s[2];                                // scores of a stage
+  Op w[4], a[3][4];                           // its weights; operands
+#pragma unroll
+  for (int g = 0; g < 4; ++g) {
+    st.load_keys(a[0], lds, g, n, h);
+    st.add_scores(s, a[0], g);
+  }
+  __syncthreads();                            // (K of the first stage has been read)
+  if (late) __syncthreads();
+  int k0 = first, now = 0, next = kPipeStage, last = 2 * kPipeStage;      // places of this stage, the next, the one after
+  auto stage = [&](auto masked) {
     constexpr bool kMasked = decltype(masked)::value;
-    Op w[4], a[2][4];
-    st.load_keys(a[0], lds.k[1 - P], 0, n, h);                   // (of the last stage: what lies there, unused)
-    if (kMasked) {
-      st.hide(s[P], k0, h);
-      mx = st.largest(s[P][1], st.largest(s[P][0], -INFINITY));
-    }
-    st.follow(mx);
+    // vector half
+    if (kMasked) st.hide(s, k0, h);
+    st.follow(st.largest(s[1], st.largest(s[0], -INFINITY)));
     const float at = st.m == -INFINITY ? 0.f : st.m - PipeState<Op>::Tile::kLift;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) st.weights(s, w, u, at);
+    if (k0 > first) {                                            // (the first stages' rows are there)
+      fk.put(lds + last, lane, wave);
+      fv.put(lds + kV + next, lane, wave);
+      e_v = e_k;
+      e_k = e_new;
+    }
+    fk.aim(K, row_of(k0 + 3 * kPipeKeys), end, uniform(e_k), lane);
+    fv.aim(V, row_of(k0 + 2 * kPipeKeys), end, uniform(e_v), lane);
+    landed();
+    const lds_char* const v = lds + kV + now;
+    const lds_char* const k = lds + next;                        // (of the last stage: what lies there, unused)
+    st.load_values(a[0], v, 0, lane);
+    st.load_values(a[1], v, 1, lane);
+    __syncthreads();
+    // matrix half
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      __builtin_amdgcn_sched_barrier(0);
+      if (i < 2) st.load_values(a[(i + 2) % 3], v, i + 2, lane);
+      else if (i < 6) st.load_keys(a[(i + 2) % 3], k, i - 2, n, h);
+      if (i < 4) st.add_values(a[i % 3], w[i]);
+      else st.add_scores(s, a[i % 3], i - 4);
+      if (i == 2) e_new = look_up(k0 + 4 * kPipeKeys);
+      if (i == 3) fk.ask(lds + now, wave);
+      if (i == 4) fv.ask(lds + kV + last, wave);
+    }
     __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      if (g < 3) st.load_keys(a[(g + 1) & 1], lds.k[1 - P], g + 1, n, h);
-      st.add_scores(s[1 - P], a[g & 1], g);
-      st.weights(s[P], w, g, at);
-      if (g < 3) group_order<4, 3>();
-      else group_order<0, 3>();
-    }
-    if (k0 + 2 * kPipeKeys < end) fk.put(lds.k[P], lane, wave);
-    fv.put(lds.v[P], lane, wave);
-    arrived();
-    st.load_values(a[0], lds.v[P], 0, lane);
-#pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      if (t < 3) st.load_values(a[(t + 1) & 1], lds.v[P], t + 1, lane);
-      st.add_values(a[t & 1], w[t]);
-      if (t < 2) {
-        st.weights(s[P], w, 4 + 2 * t, at);
-        st.weights(s[P], w, 5 + 2 * t, at);
-      } else if (!kMasked) {
-        mx = st.largest(s[1 - P][t - 2], t == 2 ? -INFINITY : mx);
-      }
-      if (t < 2) group_order<8, 6>();
-      else if (t == 2) group_order<8, 2>();
-      else group_order<0, 2>();
-    }
-    ask_k(lds.k[1 - P], k0 + 3 * kPipeKeys);
-    ask_v(lds.v[1 - P], k0 + kPipeKeys);
+    __syncthreads();
     k0 += kPipeKeys;
+    const int free = now;
+    now = next;
+    next = last;
+    last = free;
   };
-  const std::integral_constant<int, 0> even;
-  const std::integral_constant<int, 1> odd;
-  while (k0 + 2 * kPipeKeys <= least && k0 + kPipeKeys < end) {
-    stage(even, std::false_type{});
-    stage(odd, std::false_type{});
-  }
-  while (k0 < end) {
-    stage(even, std::true_type{});
-    if (k0 < end) stage(odd, std::true_type{});
-  }
+  while (k0 + kPipeKeys <= least && k0 < end) stage(std::false_type{});
+  while (k0 < end) stage(std::true_type{});
+  if (!late) __syncthreads();
 }
 
 }  // namespace lfps
