@@ -114,12 +114,12 @@ __device__ __forceinline__ void prompt_pipe(char* lds, const PromptArgs<TQ>& a, 
     st.q.load(a.q + (int64_t)(c0 + token) * a.q_stride + head * kD, h);
     const CacheRows<TK> K(a.kv.k, a.kv, b, g);
     const CacheRows<TV> V(a.kv.v, a.kv, b, g);
-    pipe_loop<kKind, TK, TV, Op>(lds, K, V, lo, hi, st);
+    pipe_loop<kKind, TK, TV, Op>(lds, K, V, lo, hi, seen(row0 >> shift), st);
   }
   if (!valid) return;
   TQ* const out = a.out + ((int64_t)(c0 + token) * s.Hq + head) * kD;
   float* const part = a.part + (part_row(a, false, 0, b, c0, token, head) + split) * kPartFloats;
-  const float l = st.l + __shfl_xor(st.l, 32), inv = l == 0.f ? 0.f : 1.f / l;
+  const float half = (st.l[0] + st.l[1]) + (st.l[2] + st.l[3]), l = half + __shfl_xor(half, 32), inv = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
   for (int d = 0; d < 4; ++d)
 #pragma unroll

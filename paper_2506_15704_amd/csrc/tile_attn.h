@@ -26,6 +26,7 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x2t __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2t __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x2t __attribute__((ext_vector_type(2)));
+typedef __attribute__((address_space(3))) char lds_char;
 
 // The rows [.., end) of one request and KV head as a kernel reads them.
 template <typename T>
@@ -184,6 +185,62 @@ struct QueryTile<float, kTerms> {
   }
 };
 
+// ---- values that are not finite ------------------------------------------------------------------------------
+// A row that does not see a key gives it the weight 0, and 0 times an infinity or NaN among that key's values is not 0.  Where some
+// row of a wave does not see all keys of a step, the step's values are looked through; if any is not finite, they are taken in key
+// by key, by the rows that see the key.
+template <typename Op>
+__device__ __forceinline__ bool any_not_finite(const lds_char* rows, int bytes) {
+  constexpr uint32_t kExp = std::is_same<Op, float>::value ? 0x7F800000u : (std::is_same<Op, f16x8>::value ? 0x7C00u : 0x7F80u);
+  bool found = false;
+  for (int at = 16 * (threadIdx.x & 63); at < bytes; at += 1024) {
+    const u32x4 x = *(const __attribute__((address_space(3))) u32x4*)(rows + at);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      found |= (x[i] & kExp) == kExp;
+      if constexpr (!std::is_same<Op, float>::value) found |= ((x[i] >> 16) & kExp) == kExp;
+    }
+  }
+  return __ballot(found) != 0;
+}
+// o += weights of `keys` keys (a multiple of 32) times their values at v, key by key on the vector units, of keys below `seen`.
+// weight(i, half): my weight of the i-th of the keys that that half of the wave holds.  Slow, and small: almost no call comes here.
+template <typename Op, typename Weight>
+__device__ __forceinline__ void add_apart(f32x16 (&o)[4], Weight weight, const lds_char* v, int keys, int seen, int lane) {
+  const int h = lane >> 5;
+#pragma unroll 1
+  for (int key = 0; key < keys; ++key) {
+    const float mine = weight((key >> 3) * 4 + (key & 3)), other = __shfl_xor(mine, 32);
+    const float w = h == ((key >> 2) & 1) ? mine : other;
+    if (key >= seen) continue;
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; r += 4) {
+        float x[4];
+        if constexpr (std::is_same<Op, float>::value) {
+          const f32x4 y = *(const __attribute__((address_space(3))) f32x4*)(v + key * 512 + 16 * chunk_place_f32(key, 8 * d + r / 2 + h));
+#pragma unroll
+          for (int i = 0; i < 4; ++i) x[i] = y[i];
+        } else {
+          typedef typename std::conditional<std::is_same<Op, bf16x8>::value, __bf16, _Float16>::type Elem;
+          typedef Elem Elem4 __attribute__((ext_vector_type(4)));
+          const Elem4 y = *(const __attribute__((address_space(3))) Elem4*)(v + key * 256 + 16 * chunk_place(key, 4 * d + r / 4) + 8 * h);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) x[i] = (float)y[i];
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[d][r + i] = fmaf(w, x[i], o[d][r + i]);
+      }
+  }
+}
+__device__ __forceinline__ f32x16 zeros16() {
+  f32x16 z;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) z[r] = 0.f;
+  return z;
+}
+
 // ---- the state of a wave's 32 rows ----------------------------------------------------------------------------
 // kTerms: 16-bit terms of the weights (1: rounded to 16 bits, as the output will be; 2: fp32 results).  An fp32 query is the sum of
 // query_terms of them: three of bf16, which hold it whole (two leave 2^-18 of every element, and the error of a score grows with it:
@@ -194,6 +251,7 @@ template <typename Op, int kTerms>
 struct RowState {
   typedef QueryTile<Op, query_terms<Op, kTerms>()> Query;
   static constexpr bool kF32 = std::is_same<Op, float>::value;
+  static constexpr int kRowBytes = kF32 ? 512 : 256;
   // Weights of fp16 values are held 2^14 (2^8 with one term) times as large, or those below 2^-24 of the row's largest would be lost.
   static constexpr float kLift = std::is_same<Op, f16x8>::value ? (kTerms == 1 ? 8.f : 14.f) : 0.f;
   f32x16 o[4];                               // channels 32 d + 8 (r / 4) + 4 h + r % 4 of row n
@@ -275,7 +333,20 @@ struct RowState {
         l += s[b][r];
       }
 #pragma unroll
-    for (int b = 0; b < kBlocks; ++b) add_values(s[b], v + 32 * b * InLds<typename std::conditional<kF32, float, uint16_t>::type>::kRowBytes, lane);
+    for (int b = 0; b < kBlocks; ++b) {
+      const char* const vb = v + 32 * b * kRowBytes;
+      if (masked && any_not_finite<Op>((const lds_char*)vb, 32 * kRowBytes)) {
+        auto weight = [&](int i) {
+          float x = 0.f;
+#pragma unroll
+          for (int r = 0; r < 16; ++r) x = r == i ? s[b][r] : x;
+          return x;
+        };
+        add_apart<Op>(o, weight, (const lds_char*)vb, 32, limit - first - 32 * b, lane);
+      } else {
+        add_values(s[b], vb, lane);
+      }
+    }
   }
 
   // o += weights of 32 keys times their values

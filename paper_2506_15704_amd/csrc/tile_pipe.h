@@ -9,7 +9,6 @@ constexpr int kPipeWaves = 8, kPipeKeys = 64, kPipeRows = 32 * kPipeWaves;      
 constexpr int kPipeThreads = 64 * kPipeWaves, kFeedRows = kPipeKeys / kPipeWaves;   // rows of a stage that a wave brings
 constexpr float kLazy = 6.f;                         // growth of a maximum, in powers of two, that is let pass
 
-typedef __attribute__((address_space(3))) char lds_char;
 typedef const __attribute__((address_space(1))) char global_char;
 
 // How the rows of a cache lie: a slab; pages of eight rows and more; anything (smaller pages, rows very far apart).  In the first two
@@ -90,13 +89,14 @@ template <typename Op>
 struct PipeState {
   typedef RowState<Op, 1> Tile;
   f32x16 o[4];
-  float m, l;
+  float m, l[4];                             // four sums, so that none waits for the one before
   typename Tile::Query q;
   int limit;
 
   __device__ __forceinline__ void clear() {
     m = -INFINITY;
-    l = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) l[i] = 0.f;
 #pragma unroll
     for (int d = 0; d < 4; ++d)
 #pragma unroll
@@ -114,10 +114,7 @@ struct PipeState {
     for (int i = 0; i < 4; ++i) {
       const int c = 2 * g + (i >> 1);
       if (c == 0) {
-        f32x16 zero;
-#pragma unroll
-        for (int r = 0; r < 16; ++r) zero[r] = 0.f;
-        s[i & 1] = mfma32(a[i], q.x[0][c], zero);
+        s[i & 1] = mfma32(a[i], q.x[0][c], zeros16());
       } else {
         s[i & 1] = mfma32(a[i], q.x[0][c], s[i & 1]);
       }
@@ -144,6 +141,17 @@ struct PipeState {
     for (int d = 0; d < 4; ++d) o[d] = mfma32(a[d], w, o[d]);
   }
 
+  // The values of a stage key by key, of those below `seen` (see any_not_finite).
+  __device__ __forceinline__ void add_values_apart(const Op (&w)[4], const lds_char* v, int lane, int seen) {
+    auto weight = [&](int i) {                                   // of the 32 that I hold
+      float x = 0.f;
+#pragma unroll
+      for (int e = 0; e < 32; ++e) x = e == i ? (float)w[e / 8][e % 8] : x;
+      return x;
+    };
+    add_apart<Op>(o, weight, v, kPipeKeys, seen, lane);
+  }
+
   // Scores of keys that the row does not see.
   __device__ __forceinline__ void hide(f32x16 (&s)[2], int first, int h) const {
 #pragma unroll
@@ -152,10 +160,15 @@ struct PipeState {
       for (int r = 0; r < 16; ++r)
         if (first + 32 * b + 8 * (r / 4) + 4 * h + r % 4 >= limit) s[b][r] = -INFINITY;
   }
-  __device__ __forceinline__ static float largest(const f32x16& s, float mx) {
+  __device__ __forceinline__ static float largest(const f32x16 (&s)[2]) {
+    float mx[4];
 #pragma unroll
-    for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[r]);
-    return mx;
+    for (int i = 0; i < 4; ++i) mx[i] = fmaxf(s[i / 2][8 * (i % 2)], s[i / 2][8 * (i % 2) + 1]);
+#pragma unroll
+    for (int r = 2; r < 8; r += 2)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) mx[i] = fmaxf(fmaxf(mx[i], s[i / 2][8 * (i % 2) + r]), s[i / 2][8 * (i % 2) + r + 1]);
+    return fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
   }
   // mx: the largest of my scores of a stage.  Follows the row's maximum, and brings the sums so far in line with it.
   __device__ __forceinline__ void follow(float mx) {
@@ -166,7 +179,8 @@ struct PipeState {
     if (__ballot(now != before)) {
       const float shrink = now == before ? 1.f : __builtin_amdgcn_exp2f(before - now);
       m = now;
-      l *= shrink;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) l[i] *= shrink;
 #pragma unroll
       for (int d = 0; d < 4; ++d)
 #pragma unroll
@@ -185,12 +199,12 @@ struct PipeState {
         const bf16x2t z = __builtin_convertvector(p, bf16x2t);
         w[e / 8][e % 8] = z[0];
         w[e / 8][e % 8 + 1] = z[1];
-        l = __builtin_amdgcn_fdot2_f32_bf16(z, bf16x2t{(__bf16)1.f, (__bf16)1.f}, l, false);
+        l[e / 2 % 4] = __builtin_amdgcn_fdot2_f32_bf16(z, bf16x2t{(__bf16)1.f, (__bf16)1.f}, l[e / 2 % 4], false);
       } else {
         const f16x2t z = {(_Float16)p[0], (_Float16)p[1]};
         w[e / 8][e % 8] = z[0];
         w[e / 8][e % 8 + 1] = z[1];
-        l = __builtin_amdgcn_fdot2(z, f16x2t{(_Float16)1.f, (_Float16)1.f}, l, false);
+        l[e / 2 % 4] = __builtin_amdgcn_fdot2(z, f16x2t{(_Float16)1.f, (_Float16)1.f}, l[e / 2 % 4], false);
       }
     }
   }
@@ -208,16 +222,13 @@ struct PipeState {
 //
 // A matrix half is eight groups of four products; the operands of the group after the next are read before a group's products,
 // those of the first two before the barrier.
-constexpr int kPipeStage = kPipeKeys * 256, kPipeStages = 3, kPipeLds = 2 * kPipeStages * kPipeStage;
+constexpr int kPipeStage = kPipeKeys * 256, kPipeStages = 3, kPipeLds = 2 * kPipeStages * kPipeStage + 16;
+// least: keys that all rows of the workgroup see.
 template <int kKind, typename TK, typename TV, typename Op>
-__device__ __forceinline__ void pipe_loop(char* lds_, const CacheRows<TK>& K, const CacheRows<TV>& V, int first, int end,
+__device__ __forceinline__ void pipe_loop(char* lds_, const CacheRows<TK>& K, const CacheRows<TV>& V, int first, int end, int least,
                                           PipeState<Op>& st) {
   lds_char* const lds = (lds_char*)lds_;
   const int lane = threadIdx.x & 63, wave = wave_of(), n = lane & 31, h = lane >> 5;
-  int least = st.limit;
-#pragma unroll
-  for (int d = 1; d < 32; d <<= 1) least = min(least, __shfl_xor(least, d));
-  least = __builtin_amdgcn_readfirstlane(least);
   const bool late = wave >= kPipeWaves / 2;
   Feed<TK, kKind> fk;
   Feed<TV, kKind> fv;
@@ -225,6 +236,8 @@ __device__ __forceinline__ void pipe_loop(char* lds_, const CacheRows<TK>& K, co
   auto row_of = [&](int k) { return first_row(k, end, wave); };
   auto look_up = [&](int k) { return kKind == kPages ? RowMap<true>::block(K.pg, K.b, row_of(k)) : 0; };
   auto uniform = [](int e) { return __builtin_amdgcn_readfirstlane(e); };
+  int* const found = (int*)(lds_ + 2 * kPipeStages * kPipeStage) + (late ? 1 : 0);      // stage (its end) with a value that is not finite
+  if ((threadIdx.x & (64 * kPipeWaves / 2 - 1)) == 0) *found = 0;
   auto landed = [] { __builtin_amdgcn_s_waitcnt(0x0f70); };     // vmcnt(0): what I asked for is in LDS
 #pragma unroll
   for (int i = 0; i < 3; ++i) {                                  // K of the first three stages, V of two
@@ -255,7 +268,7 @@ __device__ __forceinline__ void pipe_loop(char* lds_, const CacheRows<TK>& K, co
     constexpr bool kMasked = decltype(masked)::value;
     // vector half
     if (kMasked) st.hide(s, k0, h);
-    st.follow(st.largest(s[1], st.largest(s[0], -INFINITY)));
+    st.follow(st.largest(s));
     const float at = st.m == -INFINITY ? 0.f : st.m - PipeState<Op>::Tile::kLift;
 #pragma unroll
     for (int u = 0; u < 8; ++u) st.weights(s, w, u, at);
@@ -270,17 +283,24 @@ __device__ __forceinline__ void pipe_loop(char* lds_, const CacheRows<TK>& K, co
     landed();
     const lds_char* const v = lds + kV + now;
     const lds_char* const k = lds + next;                        // (of the last stage: what lies there, unused)
+    if (kMasked) {                                               // values that a row must not meet?  Four waves share the rows out
+      constexpr int kShare = kPipeStage / (kPipeWaves / 2);
+      if (any_not_finite<Op>(v + (wave % (kPipeWaves / 2)) * kShare, kShare)) *found = k0 + kPipeKeys;
+    }
     st.load_values(a[0], v, 0, lane);
     st.load_values(a[1], v, 1, lane);
     __syncthreads();
+    const bool apart = kMasked && *(volatile int*)found == k0 + kPipeKeys;
+    if (apart) st.add_values_apart(w, v, lane, st.limit - k0);
     // matrix half
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       __builtin_amdgcn_sched_barrier(0);
       if (i < 2) st.load_values(a[(i + 2) % 3], v, i + 2, lane);
       else if (i < 6) st.load_keys(a[(i + 2) % 3], k, i - 2, n, h);
-      if (i < 4) st.add_values(a[i % 3], w[i]);
-      else st.add_scores(s, a[i % 3], i - 4);
+      if (i < 4) {
+        if (!apart) st.add_values(a[i % 3], w[i]);
+      } else st.add_scores(s, a[i % 3], i - 4);
       if (i == 2) e_new = look_up(k0 + 4 * kPipeKeys);
       if (i == 3) fk.ask(lds + now, wave);
       if (i == 4) fv.ask(lds + kV + last, wave);

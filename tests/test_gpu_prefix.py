@@ -113,3 +113,29 @@ def test_prefix_refusals():
         c.ctx.lfps_prefix_attn_decode(q, c.kv, ints(starts), ints([70, 3]), out)
     torch.cuda.synchronize()
     c.ctx.close()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32", "fp8kv"])
+@pytest.mark.parametrize("members", [3, 12, 40])
+def test_prefix_values_that_are_not_finite_stay_out_of_requests_that_end_before_them(dtype, members):
+    """Members shorter than the shared prefix: rows behind their own length are the others'."""
+    Hq = 2
+    lens = [300] + [300 if i % 2 else 120 + i for i in range(1, members)]
+    c = CacheCase(dtype, Hq, 1, lens, seed=9)
+    v = c.V[0, 0].to(torch.float32)
+    v[200, 5] = float("nan")
+    v[190, 9] = float("nan") if c.vd.itemsize == 1 else float("inf")
+    c.V.view(torch.uint8)[0, 0] = v.to(c.vd).view(torch.uint8) if c.vd.itemsize == 1 else v.to(c.vd).view(torch.uint8)
+    q = c.randn(c.B, Hq, D)
+    out = torch.zeros((c.B, Hq, D), device=DEV)
+    c.ctx.lfps_prefix_attn_decode(q, c.kv, ints([0, members]), ints([300]), out)
+    K, V = c.values(c.K, 0, 0, 300)[0], v.to(c.vd).to(torch.float32).double()
+    for b, n in enumerate(lens):
+        for h in range(Hq):
+            clean = V[:n].nan_to_num(0, 0, 0)
+            ref, weighted, dots = attend64(q[b, h:h + 1].double(), K[:n], clean)
+            broken = ~V[:n].isfinite().all(0)
+            assert torch.equal(~out[b, h].isfinite(), broken), (b, h)
+            err = (out[b, h].double() - ref[0]).abs()[~broken]
+            assert bool((err <= _tolerance(dtype, ref, weighted, dots, n)[0][~broken]).all())
+    c.ctx.close()

@@ -226,3 +226,40 @@ def test_prompt_with_arrays_that_make_no_sense():
         c.ctx.lfps_prompt_attn(q, ints(cu), c.kv, guard[2:42])
         assert bool((guard[:2] == 7).all()) and bool((guard[42:] == 7).all())
     c.ctx.close()
+
+
+def _same_where_not_finite(got, ref, tol):
+    assert torch.equal(got.isnan(), ref.isnan()) and torch.equal(got.isinf(), ref.isinf())
+    assert torch.equal(got[ref.isinf()].sign(), ref[ref.isinf()].sign())
+    fine = ref.isfinite()
+    assert bool(((got - ref).abs()[fine] <= tol.expand_as(ref)[fine]).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32", "fp8v", "fp8kv"])
+@pytest.mark.parametrize("Hq,news,lens", [(1, [200], [200]), (4, [300], [333]), (4, [5], [70]), (2, [1, 70], [64, 129])])
+def test_prompt_values_that_are_not_finite_reach_only_the_tokens_that_see_them(dtype, Hq, news, lens):
+    """Infinities and NaN in single channels of single rows, a row apart from tokens that do not see them."""
+    c = CacheCase(dtype, Hq, 1, lens, seed=8)
+    bad = float("nan") if c.vd.itemsize == 1 else float("inf")
+    marks = []
+    for b, n in enumerate(lens):
+        for row, ch, x in ((n - 1, 3, bad), (n - 2, 77, float("nan")), (n // 2, 64, bad), (n // 2 + 1, 127, -bad)):
+            v = c.V[b, 0].to(torch.float32)
+            v[row, ch] = x
+            raw(c.V)[b, 0] = raw(to_cache(v, c.vd) if x == x or c.vd.itemsize > 1 else v.to(c.vd))
+            marks.append((b, row, ch))
+    at, q, out = _prompt(c, news)
+    for b, t in enumerate(news):
+        n = lens[b]
+        K, V = c.values(c.K, b, 0, n)[0], c.V[b, 0].to(torch.float32).double()
+        for h in range(Hq):
+            for i in range(max(0, t - 40), t):
+                end = n - t + i + 1
+                s = K[:end] @ q[at[b] + i, h].double() / D ** 0.5
+                p = torch.softmax(s, 0)
+                clean = V[:end].nan_to_num(0, 0, 0)
+                ref, weighted = p @ clean, p @ clean.abs()
+                dots = (K[:end].abs() @ q[at[b] + i, h].double().abs()).max() / D ** 0.5
+                ref = torch.where(V[:end].isfinite().all(0), ref, V[:end].masked_fill(V[:end].isfinite(), 0).sum(0))
+                _same_where_not_finite(out[at[b] + i, h].double(), ref, _tolerance(dtype, ref.nan_to_num(0, 0, 0), weighted, dots, n))
+    c.ctx.close()
