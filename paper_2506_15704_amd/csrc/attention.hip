@@ -11,6 +11,7 @@
 // Full: split-K over contiguous row ranges with the G heads of a group sharing every K and V row; a wave keeps the running
 // (max, sum, acc) of its heads, without grouping a lane group of 16 that of its rows, merged with the online-softmax rule.
 #include "attend.h"
+#include "prefix_groups.h"
 
 namespace lfps {
 
@@ -87,7 +88,12 @@ int full_attn_splits(const Shape& s) {
   return ns < 1 ? 1 : ns;
 }
 
-__device__ __forceinline__ int rows_per_split(int n, int n_split) { return (((n + n_split - 1) / n_split) + 15) & ~15; }
+// The rows that a pass is over: all of a request's, or with Own = PrefixGroups those that it does not share (none: it is in no group).
+__device__ __forceinline__ int first_row_of(const Shape&, const int32_t*, int, int) { return 0; }
+__device__ __forceinline__ int first_row_of(const Shape& s, const int32_t* seq_lens, int b, int n, const PrefixGroups& groups) {
+  const int first = first_own_row(s, seq_lens, groups, b);
+  return first < 0 || first > n ? n : first;
+}
 
 // x[u] = the elements at at(u), past the caches or not.  (A choice at run time between the two forms of one load is merged by the
 // compiler, into the ordinary one: the kernels hold their loops twice.)
@@ -170,12 +176,12 @@ __device__ __forceinline__ float row16_shared_sums(float (&a)[G], int j) {
 // kMayOnce: rows past the caches where the rows that the requests hold outgrow the memory-side cache (kKeptStreamBytes; 8 x 32K rows 195 against
 // 207 us with the kernel as it was); fewer are found there by the next call, whatever the context has room for (8 x 8192 of
 // 131072 rows in bf16 52.9 -> 48.8 us, 8 x 16384 in FP8 62.3 -> 57.3, against that capacity deciding).
-template <typename TK, typename T, int G, bool kPaged, bool kMayOnce>
+template <typename TK, typename T, int G, bool kPaged, bool kMayOnce, typename... Own>
 __global__ __launch_bounds__(kAttnThreads) void k_full_attn(Shape s, const float* __restrict__ q,
                                                             const TK* __restrict__ K, const T* __restrict__ V,
                                                             int64_t stride_b, int64_t stride_h, int64_t stride_n,
                                                             KvPage pg, const int32_t* __restrict__ seq_lens,
-                                                            float* __restrict__ part, int n_split, float scale) {
+                                                            float* __restrict__ part, int n_split, float scale, Own... own) {
   constexpr int U = sizeof(TK) == 4 ? 4 : 8, kRows = 4 * U;
   constexpr int kShare = 16 / G;                            // lanes of a row that hold the same head's sum
   constexpr int NV = U > kShare ? U / kShare : 1;           // (row, head) pairs of a lane
@@ -188,8 +194,9 @@ __global__ __launch_bounds__(kAttnThreads) void k_full_attn(Shape s, const float
   const int j = lane & 15, rs = lane >> 4;
   int n = seq_lens[b];
   n = n < 0 ? 0 : (n > s.Lcap ? s.Lcap : n);
-  const int rps = rows_per_split(n, n_split);
-  const int r_begin = split * rps;
+  const int r_first = first_row_of(s, seq_lens, b, n, own...);
+  const int rps = rows_per_split(n - r_first, n_split);
+  const int r_begin = r_first + split * rps;
   const int r_end = (r_begin + rps < n) ? r_begin + rps : n;
   if (r_begin >= n) return;
   const bool once_here = kMayOnce && outgrow_cache(s, held_rows(s, seq_lens), kD * (int)(sizeof(TK) + sizeof(T)), kKeptStreamBytes);
@@ -338,12 +345,12 @@ __global__ __launch_bounds__(kAttnThreads) void k_full_attn(Shape s, const float
 // in FP8 10.6 -> 9.7, 1 x 16384 in fp32 29.4 -> 28.6, 1 x 32768 in FP8 21.2 -> 19.7; 32 x 30000 in bf16 571 -> 567.
 // Paged, one look-up serves both tiles: with one each, its wait came twice as often and the compiler kept fewer loads in flight (FP8
 // 16 x 32768 169.2 -> 166.5 us, bf16 325.9 -> 323.2, 1 x 8192 11.7 -> 11.3).
-template <typename TK, typename T, bool kPaged, bool kMayOnce>
+template <typename TK, typename T, bool kPaged, bool kMayOnce, typename... Own>
 __global__ __launch_bounds__(kAttnThreads) void k_full_attn_single(Shape s, const float* __restrict__ q,
                                                                    const TK* __restrict__ K, const T* __restrict__ V,
                                                                    int64_t stride_b, int64_t stride_h, int64_t stride_n,
                                                                    KvPage pg, const int32_t* __restrict__ seq_lens,
-                                                                   float* __restrict__ part, int n_split, float) {
+                                                                   float* __restrict__ part, int n_split, float, Own... own) {
   constexpr double kLog2Scale = 0.08838834764831845 * 1.4426950408889634;
   constexpr float kHi = (float)kLog2Scale, kLo = (float)(kLog2Scale - (double)kHi);
   constexpr int U = 4, kRows = 4 * U;
@@ -355,8 +362,9 @@ __global__ __launch_bounds__(kAttnThreads) void k_full_attn_single(Shape s, cons
   const int j = lane & 15, rs = lane >> 4;
   int n = seq_lens[b];
   n = n < 0 ? 0 : (n > s.Lcap ? s.Lcap : n);
-  const int rps = rows_per_split(n, n_split);
-  const int r_begin = split * rps;
+  const int r_first = first_row_of(s, seq_lens, b, n, own...);
+  const int rps = rows_per_split(n - r_first, n_split);
+  const int r_begin = r_first + split * rps;
   const int r_end = (r_begin + rps < n) ? r_begin + rps : n;
   if (r_begin >= n) return;
   const bool once_here = kMayOnce && outgrow_cache(s, held_rows(s, seq_lens), kD * (int)(sizeof(TK) + sizeof(T)), kKeptStreamBytes);
@@ -561,6 +569,38 @@ hipError_t launch_full_attn(const Shape& s, int dtype, const float* q, const KvV
   if (dtype == LFPS_F16) return launch_full_t<_Float16, _Float16>(s, q, kv, part, n_split, st);
   return dtype == LFPS_BF16 ? launch_full_t<uint16_t, uint16_t>(s, q, kv, part, n_split, st)
                             : launch_full_t<float, float>(s, q, kv, part, n_split, st);
+}
+
+template <typename TK, typename T>
+static hipError_t launch_full_own_t(const Shape& s, const float* q, const KvView& kv, const PrefixGroups& groups, float* part, int n_split,
+                                    hipStream_t st) {
+  const dim3 grid(n_split, s.B * s.Hkv), block(kAttnThreads);
+  const float scale = 0.08838834764831845f;
+#define LFPS_LAUNCH_OWN_P(KERNEL, PAGED, ...)                                                                             \
+  hipLaunchKernelGGL((KERNEL<TK, T, ##__VA_ARGS__, PAGED, false, PrefixGroups>), grid, block, 0, st, s, q, (const TK*)kv.k, \
+                     (const T*)kv.v, kv.stride_b, kv.stride_h, kv.stride_n, kv.page, kv.seq_lens, part, n_split, scale, groups)
+#define LFPS_LAUNCH_OWN(KERNEL, ...)                              \
+  if (kv.page.table) LFPS_LAUNCH_OWN_P(KERNEL, true, ##__VA_ARGS__); \
+  else LFPS_LAUNCH_OWN_P(KERNEL, false, ##__VA_ARGS__);
+  switch (s.G) {
+    case 1: LFPS_LAUNCH_OWN(k_full_attn_single) break;
+    case 2: LFPS_LAUNCH_OWN(k_full_attn, 2) break;
+    case 4: LFPS_LAUNCH_OWN(k_full_attn, 4) break;
+    default: return hipErrorInvalidValue;
+  }
+#undef LFPS_LAUNCH_OWN
+#undef LFPS_LAUNCH_OWN_P
+  return hipGetLastError();
+}
+
+hipError_t launch_full_attn_own(const Shape& s, int dtype, const float* q, const KvView& kv, const PrefixGroups& groups, float* part,
+                                int n_split, hipStream_t st) {
+  if (dtype == LFPS_F32) return launch_full_own_t<float, float>(s, q, kv, groups, part, n_split, st);
+  if (dtype == LFPS_F16) return launch_full_own_t<_Float16, _Float16>(s, q, kv, groups, part, n_split, st);
+  if (kv.k_fp8 && kv.v_fp8) return launch_full_own_t<uint8_t, uint8_t>(s, q, kv, groups, part, n_split, st);
+  if (kv.k_fp8) return launch_full_own_t<uint8_t, uint16_t>(s, q, kv, groups, part, n_split, st);
+  if (kv.v_fp8) return launch_full_own_t<uint16_t, uint8_t>(s, q, kv, groups, part, n_split, st);
+  return launch_full_own_t<uint16_t, uint16_t>(s, q, kv, groups, part, n_split, st);
 }
 
 hipError_t launch_full_merge(const Shape& s, const int32_t* seq_lens, const float* part, int n_split, float* out,

@@ -34,10 +34,6 @@ __device__ __forceinline__ void tokens_of(const A& a, int b, int* c0, int* c1) {
   *c0 = x < 0 ? 0 : (x > a.n_tokens ? a.n_tokens : x);
   *c1 = y < *c0 ? *c0 : (y > a.n_tokens ? a.n_tokens : y);
 }
-__device__ __forceinline__ int length_of(const Shape& s, const int32_t* seq_lens, int b) {
-  const int n = seq_lens[b];
-  return n < 0 ? 0 : (n > s.Lcap ? s.Lcap : n);
-}
 template <typename TK>
 constexpr int few_most() { return 32 * (4 / few_key_waves<TK>()); }      // query rows of a request that k_prompt_few takes
 // The partial results of token i (of those from c0 on of request b), a row of `splits` of them.
@@ -114,25 +110,11 @@ __device__ __forceinline__ void prompt_pipe(char* lds, const PromptArgs<TQ>& a, 
     st.q.load(a.q + (int64_t)(c0 + token) * a.q_stride + head * kD, h);
     const CacheRows<TK> K(a.kv.k, a.kv, b, g);
     const CacheRows<TV> V(a.kv.v, a.kv, b, g);
-    pipe_loop<kKind, TK, TV, Op>(lds, K, V, lo, hi, seen(row0 >> shift), st);
+    pipe_loop<kKind, TK, TV>(lds, K, V, lo, hi, seen(row0 >> shift), row0 + 32 * wave < rows, st);
   }
   if (!valid) return;
-  TQ* const out = a.out + ((int64_t)(c0 + token) * s.Hq + head) * kD;
-  float* const part = a.part + (part_row(a, false, 0, b, c0, token, head) + split) * kPartFloats;
-  const float half = (st.l[0] + st.l[1]) + (st.l[2] + st.l[3]), l = half + __shfl_xor(half, 32), inv = l == 0.f ? 0.f : 1.f / l;
-#pragma unroll
-  for (int d = 0; d < 4; ++d)
-#pragma unroll
-    for (int r = 0; r < 16; r += 4) {
-      const f32x4 y = {st.o[d][r], st.o[d][r + 1], st.o[d][r + 2], st.o[d][r + 3]};
-      const int c = 32 * d + 2 * r + 4 * h;
-      if (a.splits > 1) put4(part + c, y);
-      else put4(out + c, f32x4{y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv});
-    }
-  if (a.splits > 1 && h == 0) {
-    part[kD] = st.m;
-    part[kD + 1] = l;
-  }
+  if (a.splits > 1) st.finish((TQ*)nullptr, a.part + (part_row(a, false, 0, b, c0, token, head) + split) * kPartFloats, h);
+  else st.finish(a.out + ((int64_t)(c0 + token) * s.Hq + head) * kD, nullptr, h);
 }
 
 }  // namespace
@@ -180,13 +162,11 @@ __global__ __launch_bounds__(kTileThreads) void k_prompt_few(PromptArgs<TQ> a) {
   prompt_tile<TK, TV, TQ, kKeyWaves>(lds, a, b, g, c0, c1, 0, split);
 }
 
-// The parts of a row -> its output row: 32 lanes a (token, head).  few: of every request's first most / G tokens, if it has no more; else
+// The parts of a row -> its output row, a wave a (token, head).  few: of every request's first most / G tokens, if it has no more; else
 // of every token of the other requests.
 template <typename TQ>
 __global__ __launch_bounds__(kTileThreads) void k_prompt_merge(PromptArgs<TQ> a, int few, int most) {
-  const int lane32 = threadIdx.x & 31, Hq = a.s.Hq;
-  const int64_t x = (int64_t)blockIdx.x * (kTileThreads / 32) + threadIdx.x / 32;
-  const int head = (int)(x % Hq), y = (int)(x / Hq);
+  const int Hq = a.s.Hq, x = blockIdx.x * (kTileThreads / 64) + wave_of(), head = x % Hq, y = x / Hq;
   int b, i, c0, c1;
   if (few) {
     b = y / (most / a.s.G);
@@ -195,20 +175,16 @@ __global__ __launch_bounds__(kTileThreads) void k_prompt_merge(PromptArgs<TQ> a,
     tokens_of(a, b, &c0, &c1);
   } else {
     if (y >= a.n_tokens) return;
-    int lo = 0, hi = a.s.B - 1;                                // the last request whose tokens do not begin behind y
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) / 2;
-      if (a.cu[mid] <= y) lo = mid;
-      else hi = mid - 1;
-    }
-    b = lo;
+    b = last_not_above(a.s.B - 1, y, [&](int j) { return a.cu[j]; });
     tokens_of(a, b, &c0, &c1);
     i = y - c0;
   }
   const int t = c1 - c0;
   if (i < 0 || i >= t || (few != 0) != (a.few_splits && (int64_t)t * a.s.G <= most)) return;
-  put4(a.out + ((int64_t)(c0 + i) * Hq + head) * kD + 4 * lane32,
-       merge_parts(a.part + part_row(a, few != 0, most, b, c0, i, head) * kPartFloats, few ? a.few_splits : a.splits, lane32));
+  const float* const part = a.part + part_row(a, few != 0, most, b, c0, i, head) * kPartFloats;
+  auto at = [&](int j) { return part + (int64_t)j * kPartFloats; };
+  put2(a.out + ((int64_t)(c0 + i) * Hq + head) * kD + 2 * (threadIdx.x & 63),
+       join_parts(few ? a.few_splits : a.splits, at, [&](int j) { return at(j)[kD]; }, [&](int j) { return at(j)[kD + 1]; }));
 }
 
 namespace {
@@ -249,7 +225,7 @@ hipError_t prompt_t(const Shape& s, const KvView& kv, const void* q, int64_t q_s
   if (!none_few)
     hipLaunchKernelGGL((k_prompt_few<TK, TV, TQ>), dim3((unsigned)(s.Hkv * a.few_splits * s.B)), dim3(kTileThreads), 0, st, a);
   auto merge = [&](int few, int64_t rows) {
-    hipLaunchKernelGGL((k_prompt_merge<TQ>), dim3((unsigned)((rows + 7) / 8)), dim3(kTileThreads), 0, st, a, few, kMost);
+    hipLaunchKernelGGL((k_prompt_merge<TQ>), dim3((unsigned)((rows + 3) / 4)), dim3(kTileThreads), 0, st, a, few, kMost);
   };
   if (a.splits > 1) merge(0, (int64_t)n_tokens * s.Hq);
   if (a.few_splits > 1) merge(1, (int64_t)s.B * (kMost / s.G) * s.Hq);

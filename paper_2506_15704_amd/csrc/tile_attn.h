@@ -12,7 +12,7 @@
 // product are taken in the order in which the first one leaves them: V is read from LDS transposed, four keys a lane
 // (ds_read_b64_tr), with each half of the wave reading the keys it holds weights for.
 #pragma once
-#include "lfps_internal.h"
+#include "prefix_groups.h"
 
 #include <type_traits>
 
@@ -65,46 +65,47 @@ __device__ __forceinline__ f32x16 mfma32(bf16x8 a, bf16x8 b, f32x16 c) { return 
 __device__ __forceinline__ f32x16 mfma32(f16x8 a, f16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
 __device__ __forceinline__ f32x16 mfma32(float a, float b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x2f32(a, b, c, 0, 0, 0); }
 
-// Rows [k0, k0 + kRows) of K or V on their way from the cache to LDS, in the registers of the workgroup's threads.
-template <typename T, int kRows>
-struct Staged {
-  static constexpr int kChunks = kD * (int)sizeof(T) / 16;                // 16-byte loads a row
-  static constexpr int kLoads = kRows * kChunks / kTileThreads;
-  u32x4 x[kLoads];
-  int e[kLoads];                                                          // the block table's entries of the rows of the tile after
+__device__ __forceinline__ int wave_of() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
 
-  __device__ __forceinline__ static int row(int i, int tid) { return (tid + kTileThreads * i) / kChunks; }
-  __device__ __forceinline__ void look_up(const CacheRows<T>& c, int k0, int end, int tid) {
+// The kRows rows of a stage, of K or V, that a wave brings.  16- and 32-bit elements go from memory to LDS without registers, 1 KB an
+// instruction: lane l fills the l-th 16 bytes of it, so it asks for the chunk that belongs there.  FP8 goes through registers and
+// becomes bf16.  Rows from `end` on are the last one again: they are read by nobody's weights but 0.
+template <typename T, int kRows>
+struct StageFeed {
+  static constexpr bool kDirect = sizeof(T) > 1;
+  static constexpr int kPieces = kD * (int)sizeof(T) / 16, kRowsOfLoad = 64 / kPieces, kLoads = kRows / kRowsOfLoad;
+  u32x4 x[kDirect ? 1 : kLoads];
+  int e[kLoads];                                                          // the block table's entries of the stage that is asked for next
+
+  __device__ __forceinline__ static int row(int i, int lane) { return kRows * wave_of() + kRowsOfLoad * i + lane / kPieces; }
+  __device__ __forceinline__ static int piece(int i, int lane) {          // of a row of the cache, in bytes
+    const int place = lane % kPieces, r = row(i, lane);
+    return 16 * (!kDirect ? place : (sizeof(T) == 4 ? chunk_place_f32(r, place) : chunk_place(r, place)));
+  }
+  __device__ __forceinline__ void look_up(const CacheRows<T>& c, int k0, int end, int lane) {
+    if (!c.pg.table) return;
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) e[i] = c.entry(min(k0 + row(i, lane), end - 1));
+  }
+  __device__ __forceinline__ void ask(const CacheRows<T>& c, lds_char* stage, int k0, int end, int lane) {
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
-      const int r = k0 + row(i, tid);
-      e[i] = c.entry(r < end ? r : end - 1);
+      const char* p = reinterpret_cast<const char*>(c.at(min(k0 + row(i, lane), end - 1), e[i])) + piece(i, lane);
+      if constexpr (kDirect)
+        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) char*)p,
+                                         (__attribute__((address_space(3))) void*)(stage + (kRows * wave_of() + kRowsOfLoad * i) * InLds<T>::kRowBytes), 16, 0, 0);
+      else
+        x[i] = *reinterpret_cast<const u32x4*>(p);
     }
   }
-  // Rows from `end` on are loaded from the last row (a caller's rows beyond it may be anything, also unmapped) and stored as zeros:
-  // their weights are 0, and 0 times what they hold need not be.
-  __device__ __forceinline__ void load(const CacheRows<T>& c, int k0, int end, int tid) {
+  __device__ __forceinline__ void put(lds_char* stage, int lane) const {
+    if constexpr (!kDirect) {
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-      const int r = k0 + row(i, tid);
-      x[i] = *reinterpret_cast<const u32x4*>(reinterpret_cast<const char*>(c.at(r < end ? r : end - 1, e[i])) + 16 * (tid % kChunks));
-    }
-  }
-  __device__ __forceinline__ void store(char* lds, int k0, int end, int tid) const {
-    const int c = tid % kChunks;
-#pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-      const int r = row(i, tid);
-      const bool in = k0 + r < end;
-      u32x4 w = x[i];
-#pragma unroll
-      for (int u = 0; u < 4; ++u) w[u] = in ? w[u] : 0u;
-      char* at = lds + r * InLds<T>::kRowBytes;
-      if constexpr (sizeof(T) == 1) {
-        *reinterpret_cast<bf16x8*>(at + 16 * chunk_place(r, 2 * c)) = fp8x8_to_bf16x8(w[0], w[1]);
-        *reinterpret_cast<bf16x8*>(at + 16 * chunk_place(r, 2 * c + 1)) = fp8x8_to_bf16x8(w[2], w[3]);
-      } else {
-        *reinterpret_cast<u32x4*>(at + 16 * (sizeof(T) == 4 ? chunk_place_f32(r, c) : chunk_place(r, c))) = w;
+      for (int i = 0; i < kLoads; ++i) {
+        const int r = row(i, lane), c = lane % kPieces;
+        typedef __attribute__((address_space(3))) bf16x8* Lds;
+        *(Lds)(stage + r * 256 + 16 * chunk_place(r, 2 * c)) = fp8x8_to_bf16x8(x[i][0], x[i][1]);
+        *(Lds)(stage + r * 256 + 16 * chunk_place(r, 2 * c + 1)) = fp8x8_to_bf16x8(x[i][2], x[i][3]);
       }
     }
   }
@@ -418,8 +419,7 @@ __device__ __forceinline__ void tile_loop(char* lds, const CacheRows<TK>& K, con
                                           const typename RowState<Op, kTerms>::Query& q, int limit, RowState<Op, kTerms>& st) {
   constexpr int kRows = tile_rows(kKeyWaves), kBlocks = kRows / 32 / kKeyWaves;
   constexpr int kStageK = stage_bytes<TK>(kRows), kStage = kStageK + stage_bytes<TV>(kRows);
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int n = lane & 31, h = lane >> 5, mine = (wave % kKeyWaves) * kBlocks * 32;
+  const int lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5, mine = (wave_of() % kKeyWaves) * kBlocks * 32;
   int most = limit, least = limit;
 #pragma unroll
   for (int d = 1; d < 32; d <<= 1) {
@@ -428,39 +428,45 @@ __device__ __forceinline__ void tile_loop(char* lds, const CacheRows<TK>& K, con
   }
   most = __builtin_amdgcn_readfirstlane(most);
   least = __builtin_amdgcn_readfirstlane(least);
-  Staged<TK, kRows> sk;
-  Staged<TV, kRows> sv;
-  sk.look_up(K, first, end, tid);
-  sv.look_up(V, first, end, tid);
-  sk.load(K, first, end, tid);
-  sv.load(V, first, end, tid);
-  sk.look_up(K, first + kRows, end, tid);
-  sv.look_up(V, first + kRows, end, tid);
-  sk.store(lds, first, end, tid);
-  sv.store(lds + kStageK, first, end, tid);
+  lds_char* const stages = (lds_char*)lds;
+  StageFeed<TK, kRows / 4> fk;
+  StageFeed<TV, kRows / 4> fv;
+  auto look_up = [&](int k) {
+    fk.look_up(K, k, end, lane);
+    fv.look_up(V, k, end, lane);
+  };
+  auto ask = [&](int k, int to) {
+    fk.ask(K, stages + to, k, end, lane);
+    fv.ask(V, stages + to + kStageK, k, end, lane);
+  };
+  auto put = [&](int to) {
+    fk.put(stages + to, lane);
+    fv.put(stages + to + kStageK, lane);
+  };
+  look_up(first);
+  ask(first, 0);
+  look_up(first + kRows);
+  put(0);
   int at = 0;
-  for (int k0 = first; k0 < end; k0 += kRows, at ^= 1) {
+  for (int k0 = first; k0 < end; k0 += kRows, at = kStage - at) {
     const bool more = k0 + kRows < end;
+    __builtin_amdgcn_s_waitcnt(0x0f70);       // vmcnt(0): what I asked for is in LDS
+    __syncthreads();                          // and what all did; nobody reads the other stage any more
     if (more) {
-      sk.load(K, k0 + kRows, end, tid);
-      sv.load(V, k0 + kRows, end, tid);
-      sk.look_up(K, k0 + 2 * kRows, end, tid);
-      sv.look_up(V, k0 + 2 * kRows, end, tid);
+      ask(k0 + kRows, kStage - at);
+      look_up(k0 + 2 * kRows);
     }
-    __syncthreads();                          // this stage is written, and nobody reads the other one any more
-    const int k_mine = k0 + mine;
-    if (k_mine < most) {
-      const char* k = lds + at * kStage + mine * InLds<TK>::kRowBytes;
-      const char* v = lds + at * kStage + kStageK + mine * InLds<TV>::kRowBytes;
-      f32x16 s[kBlocks];
+    const char* k = lds + at + mine * InLds<TK>::kRowBytes;
+    const char* v = lds + at + kStageK + mine * InLds<TV>::kRowBytes;
 #pragma unroll
-      for (int b = 0; b < kBlocks; ++b) s[b] = RowState<Op, kTerms>::scores(k + 32 * b * InLds<TK>::kRowBytes, q, n, h);
-      st.template step<kBlocks>(s, v, q.unit, k_mine, limit, k_mine + 32 * kBlocks > least, lane);
+    for (int b = 0; b < kBlocks; ++b) {
+      const int k_mine = k0 + mine + 32 * b;
+      if (k_mine < most) {
+        f32x16 s[1] = {RowState<Op, kTerms>::scores(k + 32 * b * InLds<TK>::kRowBytes, q, n, h)};
+        st.template step<1>(s, v + 32 * b * InLds<TV>::kRowBytes, q.unit, k_mine, limit, k_mine + 32 > least, lane);
+      }
     }
-    if (more) {
-      sk.store(lds + (at ^ 1) * kStage, k0 + kRows, end, tid);
-      sv.store(lds + (at ^ 1) * kStage + kStageK, k0 + kRows, end, tid);
-    }
+    if (more) put(kStage - at);
   }
 }
 
@@ -470,6 +476,9 @@ struct RowOut {
   TO* out;
   float* part;
 };
+__device__ __forceinline__ void put2(float* p, f32x2t x) { *reinterpret_cast<f32x2t*>(p) = x; }
+__device__ __forceinline__ void put2(uint16_t* p, f32x2t x) { *reinterpret_cast<bf16x2t*>(p) = __builtin_convertvector(x, bf16x2t); }
+__device__ __forceinline__ void put2(_Float16* p, f32x2t x) { *reinterpret_cast<f16x2t*>(p) = __builtin_convertvector(x, f16x2t); }
 __device__ __forceinline__ void put4(float* p, f32x4 x) { *reinterpret_cast<f32x4*>(p) = x; }
 __device__ __forceinline__ void put4(uint16_t* p, f32x4 x) {
   typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
@@ -543,29 +552,60 @@ __device__ __forceinline__ void tile_finish(char* lds, RowState<Op, kTerms>& st,
       else if (to.out) put4(to.out + c, f32x4{x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv});
     }
   if (to.part && h == 0 && d0 == 0) {
-    to.part[kD] = st.m;
+    to.part[kD] = st.m - RowState<Op, kTerms>::kLift;         // (what the weights are powers of two from)
     to.part[kD + 1] = st.l;
   }
 }
 
-// sum over n parts of a row, four channels a lane (32 lanes a row); parts whose largest score is -inf hold nothing.
-__device__ __forceinline__ f32x4 merge_parts(const float* part, int n, int lane32) {
-  float mx = -INFINITY;
-  for (int i = 0; i < n; ++i) mx = fmaxf(mx, part[(int64_t)i * kPartFloats + kD]);
-  f32x4 a = {0.f, 0.f, 0.f, 0.f};
-  float l = 0.f;
-  for (int i = 0; i < n; ++i) {
-    const float* p = part + (int64_t)i * kPartFloats;
-    const float m = p[kD];
-    if (m == -INFINITY) continue;
-    const float f = __builtin_amdgcn_exp2f(m - mx);
-    const f32x4 x = *reinterpret_cast<const f32x4*>(p + 4 * lane32);
-    l = fmaf(p[kD + 1], f, l);
+// n <= 128 parts of a row joined, by a whole wave, two channels a lane: part i is at(i), with score(i) its largest score in powers of two
+// (-inf: it holds nothing) and sum(i) the sum of its weights.  All scores come in one load, a lane a part, and the parts' rows eight at a
+// time.  (32 lanes a row that walked the parts one by one: 17.8 us for 17 parts of 160 rows.)
+template <typename At, typename Score, typename Sum>
+__device__ __forceinline__ f32x2t join_parts(int n, At at, Score score, Sum sum) {
+  const int lane = threadIdx.x & 63;
+  float m[2], f[2], l = 0.f;
+  constexpr int kU = 8;
+  f32x2t x[kU], a = {0.f, 0.f};
+  auto fetch = [&](int i0) {
 #pragma unroll
-    for (int c = 0; c < 4; ++c) a[c] = fmaf(x[c], f, a[c]);
+    for (int u = 0; u < kU; ++u) x[u] = *reinterpret_cast<const f32x2t*>(at(i0 + u < n ? i0 + u : n - 1) + 2 * lane);
+  };
+  fetch(0);
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    const int i = lane + 64 * j < n ? lane + 64 * j : n - 1;
+    m[j] = lane + 64 * j < n ? score(i) : -INFINITY;
+    f[j] = sum(i);
+  }
+  float mx = fmaxf(m[0], m[1]);
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) mx = fmaxf(mx, __shfl_xor(mx, d));
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    const float w = m[j] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[j] - mx);
+    l += w > 0.f || w != w ? w * f[j] : 0.f;
+    f[j] = w;
+  }
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) l += __shfl_xor(l, d);
+  for (int i0 = 0;;) {
+#pragma unroll
+    for (int u = 0; u < kU; ++u) {
+      const int i = i0 + u;
+      if (i < n) {
+        const float w = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(i < 64 ? f[0] : f[1]), i & 63));
+        if (w != 0.f) {
+          a[0] = fmaf(x[u][0], w, a[0]);
+          a[1] = fmaf(x[u][1], w, a[1]);
+        }
+      }
+    }
+    i0 += kU;
+    if (i0 >= n) break;
+    fetch(i0);
   }
   const float inv = l == 0.f ? 0.f : 1.f / l;
-  return f32x4{a[0] * inv, a[1] * inv, a[2] * inv, a[3] * inv};
+  return f32x2t{a[0] * inv, a[1] * inv};
 }
 
 // Part `split` of n of the rows [first, end): whole stages, and no part smaller than two of them while another has rows.
@@ -576,23 +616,6 @@ __device__ __forceinline__ void split_rows(int first, int end, int n, int split,
   const int64_t at = first + (int64_t)split * per;
   *lo = at < end ? (int)at : end;
   *hi = at + per < end ? (int)(at + per) : end;
-}
-
-// The last i in [0, n] with start(i) <= x, for a rising start with start(0) <= x: 64 places a round, by the whole wave.
-template <typename Start>
-__device__ __forceinline__ int last_not_above(int n, int x, Start start) {
-  const int lane = threadIdx.x & 63;
-  int lo = 0, span = n + 1;
-  while (span > 1) {
-    const int step = (span + 63) >> 6;
-    const int i = lo + lane * step;
-    const int last = i < lo + span ? i : lo + span - 1;
-    const int got = __popcll(__ballot(i < lo + span && start(last) <= x));
-    const int to = lo + (got > 0 ? got - 1 : 0) * step;
-    span = lo + span - to < step ? lo + span - to : step;
-    lo = to;
-  }
-  return __builtin_amdgcn_readfirstlane(lo);
 }
 
 }  // namespace lfps

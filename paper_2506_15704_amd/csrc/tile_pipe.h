@@ -19,8 +19,6 @@ __host__ inline int rows_kind(const KvView& kv) {
   return kv.page.table ? kPages : kSlab;
 }
 
-__device__ __forceinline__ int wave_of() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
-
 // The rows of a stage that a wave brings, eight, of K or V.  16-bit elements go from memory to LDS without
 // registers, four rows an instruction: lane l fills place l % 16 of row l / 16, so it asks for the chunk that belongs there.
 // Rows from `end` on are the last one again, also whole stages of them: they are read by nobody's weights but 0.
@@ -84,13 +82,14 @@ __device__ __forceinline__ int first_row(int k0, int end, int wave) {
   return __builtin_amdgcn_readfirstlane(w0 < end ? w0 : (end - 1) & ~(kFeedRows - 1));
 }
 
-// 32 query rows of a wave.
-template <typename Op>
+// 32 query rows of a wave.  kTerms: 16-bit terms of the query and of the weights (see RowState; here two of bf16 queries too: the third
+// one's registers are not to be had).
+template <typename Op, int kTerms = 1>
 struct PipeState {
-  typedef RowState<Op, 1> Tile;
+  static constexpr float kLift = std::is_same<Op, f16x8>::value ? 8.f : 0.f;       // (as there; times 2^kLazy it still is an fp16 number)
   f32x16 o[4];
   float m, l[4];                             // four sums, so that none waits for the one before
-  typename Tile::Query q;
+  QueryTile<Op, kTerms> q;
   int limit;
 
   __device__ __forceinline__ void clear() {
@@ -113,11 +112,9 @@ struct PipeState {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int c = 2 * g + (i >> 1);
-      if (c == 0) {
-        s[i & 1] = mfma32(a[i], q.x[0][c], zeros16());
-      } else {
-        s[i & 1] = mfma32(a[i], q.x[0][c], s[i & 1]);
-      }
+#pragma unroll
+      for (int t = kTerms - 1; t >= 0; --t)
+        s[i & 1] = mfma32(a[i], q.x[t][c], c == 0 && t == kTerms - 1 ? zeros16() : s[i & 1]);
     }
   }
   // Operands of the values' products of 16 keys, step t.
@@ -136,17 +133,34 @@ struct PipeState {
       a[d] = x.op;
     }
   }
-  __device__ __forceinline__ void add_values(const Op (&a)[4], const Op& w) {
+  // w: weights of step t as weights() left them, rounded (one term) or, of two, whole in s.
+  __device__ __forceinline__ void add_values(const Op (&a)[4], const Op& w, const f32x16 (&s)[2], int t) {
+    if constexpr (kTerms == 1) {
 #pragma unroll
-    for (int d = 0; d < 4; ++d) o[d] = mfma32(a[d], w, o[d]);
+      for (int d = 0; d < 4; ++d) o[d] = mfma32(a[d], w, o[d]);
+    } else {
+      Op x[2];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        typedef typename std::conditional<std::is_same<Op, bf16x8>::value, __bf16, _Float16>::type Elem;
+        const float p = s[t / 2][8 * (t % 2) + i];
+        x[0][i] = (Elem)p;
+        x[1][i] = (Elem)(p - (float)x[0][i]);
+      }
+#pragma unroll
+      for (int d = 0; d < 4; ++d) {
+        o[d] = mfma32(a[d], x[1], o[d]);
+        o[d] = mfma32(a[d], x[0], o[d]);
+      }
+    }
   }
 
   // The values of a stage key by key, of those below `seen` (see any_not_finite).
-  __device__ __forceinline__ void add_values_apart(const Op (&w)[4], const lds_char* v, int lane, int seen) {
+  __device__ __forceinline__ void add_values_apart(const Op (&w)[4], const f32x16 (&s)[2], const lds_char* v, int lane, int seen) {
     auto weight = [&](int i) {                                   // of the 32 that I hold
       float x = 0.f;
 #pragma unroll
-      for (int e = 0; e < 32; ++e) x = e == i ? (float)w[e / 8][e % 8] : x;
+      for (int e = 0; e < 32; ++e) x = e == i ? (kTerms == 1 ? (float)w[e / 8][e % 8] : s[e / 16][e % 16]) : x;
       return x;
     };
     add_apart<Op>(o, weight, v, kPipeKeys, seen, lane);
@@ -187,15 +201,20 @@ struct PipeState {
         for (int r = 0; r < 16; ++r) o[d][r] *= shrink;
     }
   }
-  // The weights of my scores 4 u .. + 3 of a stage, and the sum of them as they are rounded (two an instruction).
-  __device__ __forceinline__ void weights(const f32x16 (&s)[2], Op (&w)[4], int u, float at) {
+  // The weights of my scores 4 u .. + 3 of a stage, and the sum of them: as they are rounded, two an instruction; of two terms in place.
+  __device__ __forceinline__ void weights(f32x16 (&s)[2], Op (&w)[4], int u, float at) {
 #pragma unroll
     for (int i = 0; i < 4; i += 2) {
       const int e = 4 * u + i;
       f32x2t p;
       p[0] = __builtin_amdgcn_exp2f(fmaf(s[e / 16][e % 16], q.unit, -at));
       p[1] = __builtin_amdgcn_exp2f(fmaf(s[e / 16][e % 16 + 1], q.unit, -at));
-      if constexpr (std::is_same<Op, bf16x8>::value) {
+      if constexpr (kTerms == 2) {
+        s[e / 16][e % 16] = p[0];
+        s[e / 16][e % 16 + 1] = p[1];
+        l[e / 2 % 4] += p[0];
+        l[(e / 2 + 2) % 4] += p[1];
+      } else if constexpr (std::is_same<Op, bf16x8>::value) {
         const bf16x2t z = __builtin_convertvector(p, bf16x2t);
         w[e / 8][e % 8] = z[0];
         w[e / 8][e % 8 + 1] = z[1];
@@ -206,6 +225,24 @@ struct PipeState {
         w[e / 8][e % 8 + 1] = z[1];
         l[e / 2 % 4] = __builtin_amdgcn_fdot2(z, f16x2t{(_Float16)1.f, (_Float16)1.f}, l[e / 2 % 4], false);
       }
+    }
+  }
+  // The row's result, or with part != nullptr a part of it.  The lanes of a row's two halves call together.
+  template <typename TO>
+  __device__ __forceinline__ void finish(TO* out, float* part, int h) const {
+    const float half = (l[0] + l[1]) + (l[2] + l[3]), sum = half + __shfl_xor(half, 32), inv = sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; r += 4) {
+        const f32x4 y = {o[d][r], o[d][r + 1], o[d][r + 2], o[d][r + 3]};
+        const int c = 32 * d + 2 * r + 4 * h;
+        if (part) put4(part + c, y);
+        else put4(out + c, f32x4{y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv});
+      }
+    if (part && h == 0) {
+      part[kD] = m - kLift;              // (what the weights are powers of two from)
+      part[kD + 1] = sum;
     }
   }
 };
@@ -224,9 +261,10 @@ struct PipeState {
 // those of the first two before the barrier.
 constexpr int kPipeStage = kPipeKeys * 256, kPipeStages = 3, kPipeLds = 2 * kPipeStages * kPipeStage + 16;
 // least: keys that all rows of the workgroup see.
-template <int kKind, typename TK, typename TV, typename Op>
-__device__ __forceinline__ void pipe_loop(char* lds_, const CacheRows<TK>& K, const CacheRows<TV>& V, int first, int end, int least,
-                                          PipeState<Op>& st) {
+// active: the wave has rows of its own; one that has none only brings its share of the cache's.
+template <int kKind, typename TK, typename TV, typename Op, int kTerms>
+__device__ __forceinline__ void pipe_loop(char* lds_, const CacheRows<TK>& K, const CacheRows<TV>& V, int first, int end, int least, bool active,
+                                          PipeState<Op, kTerms>& st) {
   lds_char* const lds = (lds_char*)lds_;
   const int lane = threadIdx.x & 63, wave = wave_of(), n = lane & 31, h = lane >> 5;
   const bool late = wave >= kPipeWaves / 2;
@@ -264,14 +302,16 @@ __device__ __forceinline__ void pipe_loop(char* lds_, const CacheRows<TK>& K, co
   __syncthreads();                            // (K of the first stage has been read)
   if (late) __syncthreads();
   int k0 = first, now = 0, next = kPipeStage, last = 2 * kPipeStage;      // places of this stage, the next, the one after
-  auto stage = [&](auto masked) {
-    constexpr bool kMasked = decltype(masked)::value;
+  auto stage = [&](auto masked, auto works) {
+    constexpr bool kMasked = decltype(masked)::value, kWorks = decltype(works)::value;
     // vector half
-    if (kMasked) st.hide(s, k0, h);
-    st.follow(st.largest(s));
-    const float at = st.m == -INFINITY ? 0.f : st.m - PipeState<Op>::Tile::kLift;
+    if constexpr (kWorks) {
+      if (kMasked) st.hide(s, k0, h);
+      st.follow(st.largest(s));
+      const float at = st.m == -INFINITY ? 0.f : st.m - (PipeState<Op, kTerms>::kLift);
 #pragma unroll
-    for (int u = 0; u < 8; ++u) st.weights(s, w, u, at);
+      for (int u = 0; u < 8; ++u) st.weights(s, w, u, at);
+    }
     if (k0 > first) {                                            // (the first stages' rows are there)
       fk.put(lds + last, lane, wave);
       fv.put(lds + kV + next, lane, wave);
@@ -287,25 +327,33 @@ __device__ __forceinline__ void pipe_loop(char* lds_, const CacheRows<TK>& K, co
       constexpr int kShare = kPipeStage / (kPipeWaves / 2);
       if (any_not_finite<Op>(v + (wave % (kPipeWaves / 2)) * kShare, kShare)) *found = k0 + kPipeKeys;
     }
-    st.load_values(a[0], v, 0, lane);
-    st.load_values(a[1], v, 1, lane);
-    __syncthreads();
-    const bool apart = kMasked && *(volatile int*)found == k0 + kPipeKeys;
-    if (apart) st.add_values_apart(w, v, lane, st.limit - k0);
-    // matrix half
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      __builtin_amdgcn_sched_barrier(0);
-      if (i < 2) st.load_values(a[(i + 2) % 3], v, i + 2, lane);
-      else if (i < 6) st.load_keys(a[(i + 2) % 3], k, i - 2, n, h);
-      if (i < 4) {
-        if (!apart) st.add_values(a[i % 3], w[i]);
-      } else st.add_scores(s, a[i % 3], i - 4);
-      if (i == 2) e_new = look_up(k0 + 4 * kPipeKeys);
-      if (i == 3) fk.ask(lds + now, wave);
-      if (i == 4) fv.ask(lds + kV + last, wave);
+    if constexpr (kWorks) {
+      st.load_values(a[0], v, 0, lane);
+      st.load_values(a[1], v, 1, lane);
     }
-    __builtin_amdgcn_sched_barrier(0);
+    __syncthreads();
+    // matrix half
+    if constexpr (kWorks) {
+      const bool apart = kMasked && *(volatile int*)found == k0 + kPipeKeys;
+      if (apart) st.add_values_apart(w, s, v, lane, st.limit - k0);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        __builtin_amdgcn_sched_barrier(0);
+        if (i < 2) st.load_values(a[(i + 2) % 3], v, i + 2, lane);
+        else if (i < 6) st.load_keys(a[(i + 2) % 3], k, i - 2, n, h);
+        if (i < 4) {
+          if (!apart) st.add_values(a[i % 3], w[i], s, i);
+        } else st.add_scores(s, a[i % 3], i - 4);
+        if (i == 2) e_new = look_up(k0 + 4 * kPipeKeys);
+        if (i == 3) fk.ask(lds + now, wave);
+        if (i == 4) fv.ask(lds + kV + last, wave);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    } else {
+      e_new = look_up(k0 + 4 * kPipeKeys);
+      fk.ask(lds + now, wave);
+      fv.ask(lds + kV + last, wave);
+    }
     __syncthreads();
     k0 += kPipeKeys;
     const int free = now;
@@ -313,8 +361,15 @@ __device__ __forceinline__ void pipe_loop(char* lds_, const CacheRows<TK>& K, co
     next = last;
     last = free;
   };
-  while (k0 + kPipeKeys <= least && k0 < end) stage(std::false_type{});
-  while (k0 < end) stage(std::true_type{});
+  const std::true_type yes;
+  const std::false_type no;
+  if (active) {
+    while (k0 + kPipeKeys <= least && k0 < end) stage(no, yes);
+    while (k0 < end) stage(yes, yes);
+  } else {
+    while (k0 + kPipeKeys <= least && k0 < end) stage(no, no);
+    while (k0 < end) stage(yes, no);
+  }
   if (!late) __syncthreads();
 }
 
