@@ -39,6 +39,7 @@ struct Convert8<uint16_t, uint8_t> {
 template <typename TS, typename TK, typename TV>
 __global__ __launch_bounds__(256) void k_append(Shape s, KvView kv, const TS* __restrict__ k_new, const TS* __restrict__ v_new, int64_t stride_t,
                                                 const int32_t* __restrict__ cu, int n_tokens) {
+  request_arguments<decltype(&k_append<TS, TK, TV>)>();
   const int64_t x = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
   const int g = (int)(x % s.Hkv), c = 8 * (threadIdx.x & 15);
   const int64_t token = x / s.Hkv;

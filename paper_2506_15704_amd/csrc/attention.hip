@@ -88,11 +88,21 @@ int full_attn_splits(const Shape& s) {
   return ns < 1 ? 1 : ns;
 }
 
-// The rows that a pass is over: all of a request's, or with Own = PrefixGroups those that it does not share (none: it is in no group).
-__device__ __forceinline__ int first_row_of(const Shape&, const int32_t*, int, int) { return 0; }
-__device__ __forceinline__ int first_row_of(const Shape& s, const int32_t* seq_lens, int b, int n, const PrefixGroups& groups) {
-  const int first = first_own_row(s, seq_lens, groups, b);
-  return first < 0 || first > n ? n : first;
+// Rows [begin, end) of request b and KV head g, and which part of all they make: a split of the request, or an item of its own rows.
+__host__ __device__ __forceinline__ int rows_per_split(int n, int n_split) { return (((n + n_split - 1) / n_split) + 15) & ~15; }
+struct RowsOf { int b, g, begin, end; int64_t part; };
+__device__ __forceinline__ RowsOf rows_of_block(const Shape& s, const int32_t* seq_lens, int n_split) {
+  const int bg = blockIdx.y, b = bg / s.Hkv, split = blockIdx.x;
+  int n = seq_lens[b];
+  n = n < 0 ? 0 : (n > s.Lcap ? s.Lcap : n);
+  const int rps = rows_per_split(n, n_split), begin = split * rps;
+  return {b, bg % s.Hkv, begin, (begin + rps < n) ? begin + rps : n, (int64_t)bg * n_split + split};
+}
+__device__ __forceinline__ RowsOf rows_of_block(const Shape& s, const int32_t*, int, const OwnRows& own) {
+  const int i = blockIdx.x, g = blockIdx.y;
+  if (i >= own.item[s.B]) return {0, g, 0, 0, 0};
+  const OwnItem at = own.items[i];
+  return {at.b, g, at.begin, at.end, (int64_t)i * s.Hkv + g};
 }
 
 // x[u] = the elements at at(u), past the caches or not.  (A choice at run time between the two forms of one load is merged by the
@@ -182,23 +192,18 @@ __global__ __launch_bounds__(kAttnThreads) void k_full_attn(Shape s, const float
                                                             int64_t stride_b, int64_t stride_h, int64_t stride_n,
                                                             KvPage pg, const int32_t* __restrict__ seq_lens,
                                                             float* __restrict__ part, int n_split, float scale, Own... own) {
-  constexpr int U = sizeof(TK) == 4 ? 4 : 8, kRows = 4 * U;
+  constexpr int U = sizeof...(Own) || sizeof(TK) == 4 ? 4 : 8, kRows = 4 * U;
   constexpr int kShare = 16 / G;                            // lanes of a row that hold the same head's sum
   constexpr int NV = U > kShare ? U / kShare : 1;           // (row, head) pairs of a lane
   __shared__ float red_acc[4][G][kD];
   __shared__ float weight[4][kRows][G];
   __shared__ float red_m[4][G], red_l[4][G];
-  const int bg = blockIdx.y, b = bg / s.Hkv, g = bg % s.Hkv, split = blockIdx.x;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int j = lane & 15, rs = lane >> 4;
-  int n = seq_lens[b];
-  n = n < 0 ? 0 : (n > s.Lcap ? s.Lcap : n);
-  const int r_first = first_row_of(s, seq_lens, b, n, own...);
-  const int rps = rows_per_split(n - r_first, n_split);
-  const int r_begin = r_first + split * rps;
-  const int r_end = (r_begin + rps < n) ? r_begin + rps : n;
-  if (r_begin >= n) return;
+  const RowsOf here = rows_of_block(s, seq_lens, n_split, own...);
+  const int b = here.b, g = here.g, r_begin = here.begin, r_end = here.end;
+  if (r_begin >= r_end) return;
   const bool once_here = kMayOnce && outgrow_cache(s, held_rows(s, seq_lens), kD * (int)(sizeof(TK) + sizeof(T)), kKeptStreamBytes);
 
   float qr[G][8];
@@ -334,7 +339,7 @@ __global__ __launch_bounds__(kAttnThreads) void k_full_attn(Shape s, const float
     }
   }
   __syncthreads();
-  merge_waves<G>(red_acc, red_m, red_l, part + ((int64_t)bg * n_split + split) * G * (kD + 2));
+  merge_waves<G>(red_acc, red_m, red_l, part + here.part * G * (kD + 2));
 }
 
 // The same without grouping (G = 1), where nothing is to be shared out: the four rows that a wave instruction covers keep a state
@@ -356,23 +361,18 @@ __global__ __launch_bounds__(kAttnThreads) void k_full_attn_single(Shape s, cons
   constexpr int U = 4, kRows = 4 * U;
   __shared__ float red_acc[4][1][kD];
   __shared__ float red_m[4][1], red_l[4][1];
-  const int bg = blockIdx.y, b = bg / s.Hkv, g = bg % s.Hkv, split = blockIdx.x;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int j = lane & 15, rs = lane >> 4;
-  int n = seq_lens[b];
-  n = n < 0 ? 0 : (n > s.Lcap ? s.Lcap : n);
-  const int r_first = first_row_of(s, seq_lens, b, n, own...);
-  const int rps = rows_per_split(n - r_first, n_split);
-  const int r_begin = r_first + split * rps;
-  const int r_end = (r_begin + rps < n) ? r_begin + rps : n;
-  if (r_begin >= n) return;
+  const RowsOf here = rows_of_block(s, seq_lens, n_split, own...);
+  const int b = here.b, g = here.g, r_begin = here.begin, r_end = here.end;
+  if (r_begin >= r_end) return;
   const bool once_here = kMayOnce && outgrow_cache(s, held_rows(s, seq_lens), kD * (int)(sizeof(TK) + sizeof(T)), kKeptStreamBytes);
 
   float qr[8];
 #pragma unroll
   for (int c = 0; c < 8; ++c) {
-    const float x = q[(int64_t)bg * kD + 8 * j + c];
+    const float x = q[((int64_t)b * s.Hkv + g) * kD + 8 * j + c];
     qr[c] = fmaf(x, kHi, x * kLo);
   }
   using Rows = RowMap<kPaged>;
@@ -477,7 +477,7 @@ __global__ __launch_bounds__(kAttnThreads) void k_full_attn_single(Shape s, cons
     }
   }
   __syncthreads();
-  merge_waves<1>(red_acc, red_m, red_l, part + ((int64_t)bg * n_split + split) * (kD + 2));
+  merge_waves<1>(red_acc, red_m, red_l, part + here.part * (kD + 2));
 }
 
 // grid B*Hq, 128 threads.  Bound by latency (1 MB of partials per 256 heads and 8 splits): the maxima and sums of all
@@ -572,13 +572,12 @@ hipError_t launch_full_attn(const Shape& s, int dtype, const float* q, const KvV
 }
 
 template <typename TK, typename T>
-static hipError_t launch_full_own_t(const Shape& s, const float* q, const KvView& kv, const PrefixGroups& groups, float* part, int n_split,
-                                    hipStream_t st) {
-  const dim3 grid(n_split, s.B * s.Hkv), block(kAttnThreads);
+static hipError_t launch_full_own_t(const Shape& s, const float* q, const KvView& kv, const OwnRows& own, float* part, hipStream_t st) {
+  const dim3 grid(own_items_most(s), s.Hkv), block(kAttnThreads);
   const float scale = 0.08838834764831845f;
 #define LFPS_LAUNCH_OWN_P(KERNEL, PAGED, ...)                                                                             \
-  hipLaunchKernelGGL((KERNEL<TK, T, ##__VA_ARGS__, PAGED, false, PrefixGroups>), grid, block, 0, st, s, q, (const TK*)kv.k, \
-                     (const T*)kv.v, kv.stride_b, kv.stride_h, kv.stride_n, kv.page, kv.seq_lens, part, n_split, scale, groups)
+  hipLaunchKernelGGL((KERNEL<TK, T, ##__VA_ARGS__, PAGED, false, OwnRows>), grid, block, 0, st, s, q, (const TK*)kv.k, \
+                     (const T*)kv.v, kv.stride_b, kv.stride_h, kv.stride_n, kv.page, kv.seq_lens, part, 0, scale, own)
 #define LFPS_LAUNCH_OWN(KERNEL, ...)                              \
   if (kv.page.table) LFPS_LAUNCH_OWN_P(KERNEL, true, ##__VA_ARGS__); \
   else LFPS_LAUNCH_OWN_P(KERNEL, false, ##__VA_ARGS__);
@@ -593,14 +592,13 @@ static hipError_t launch_full_own_t(const Shape& s, const float* q, const KvView
   return hipGetLastError();
 }
 
-hipError_t launch_full_attn_own(const Shape& s, int dtype, const float* q, const KvView& kv, const PrefixGroups& groups, float* part,
-                                int n_split, hipStream_t st) {
-  if (dtype == LFPS_F32) return launch_full_own_t<float, float>(s, q, kv, groups, part, n_split, st);
-  if (dtype == LFPS_F16) return launch_full_own_t<_Float16, _Float16>(s, q, kv, groups, part, n_split, st);
-  if (kv.k_fp8 && kv.v_fp8) return launch_full_own_t<uint8_t, uint8_t>(s, q, kv, groups, part, n_split, st);
-  if (kv.k_fp8) return launch_full_own_t<uint8_t, uint16_t>(s, q, kv, groups, part, n_split, st);
-  if (kv.v_fp8) return launch_full_own_t<uint16_t, uint8_t>(s, q, kv, groups, part, n_split, st);
-  return launch_full_own_t<uint16_t, uint16_t>(s, q, kv, groups, part, n_split, st);
+hipError_t launch_full_attn_own(const Shape& s, int dtype, const float* q, const KvView& kv, const OwnRows& own, float* part, hipStream_t st) {
+  if (dtype == LFPS_F32) return launch_full_own_t<float, float>(s, q, kv, own, part, st);
+  if (dtype == LFPS_F16) return launch_full_own_t<_Float16, _Float16>(s, q, kv, own, part, st);
+  if (kv.k_fp8 && kv.v_fp8) return launch_full_own_t<uint8_t, uint8_t>(s, q, kv, own, part, st);
+  if (kv.k_fp8) return launch_full_own_t<uint8_t, uint16_t>(s, q, kv, own, part, st);
+  if (kv.v_fp8) return launch_full_own_t<uint16_t, uint8_t>(s, q, kv, own, part, st);
+  return launch_full_own_t<uint16_t, uint16_t>(s, q, kv, own, part, st);
 }
 
 hipError_t launch_full_merge(const Shape& s, const int32_t* seq_lens, const float* part, int n_split, float* out,

@@ -299,9 +299,10 @@ hipError_t launch_priors(const Shape& s, int dtype, const float* q, const KvView
 // prompt_attn.hip, prefix_attn.hip and pages.hip.  part: room for part_rows (attn_part_rows) partial results of a query row.
 constexpr int kPartFloats = kD + 4;        // weighted sum of the values, largest score (powers of two), sum of the weights
 inline int64_t attn_part_rows(const Shape& s) {
-  // Two parts at least of every (request, head); otherwise what splits a few hundred tokens of 32 heads over all CUs.
+  // Two parts at least of every (request, head); otherwise what 256 workgroups of 256 query rows make.  And what cuts the rows that
+  // requests have for themselves.
   const int64_t two = 2 * (int64_t)s.B * s.Hq;
-  return two > 65536 ? two : 65536;
+  return (two > 65536 ? two : 65536) + 8192;
 }
 hipError_t launch_append(const Shape& s, int dtype, const KvView& kv, const void* k_new, const void* v_new, int64_t stride_t,
                          const int32_t* cu, int n_tokens, hipStream_t st);

@@ -19,8 +19,9 @@ struct PrefixArgs {
   const float* q;
   PrefixGroups groups;
   float* part;                   // [B, Hq, splits] partial results over the shared rows
-  float* own_part;               // [B, Hkv, own_splits, G, D + 2] over each request's own (launch_full_attn_own)
-  int32_t splits, own_splits;
+  OwnRows own;
+  float* own_part;               // [items, Hkv, G, D + 2] over the requests' own (launch_full_attn_own)
+  int32_t splits;
 };
 
 // Query rows (member, head) from row0 on of the requests from b0 to b1, over rows [lo, hi) of request `from`; slot: of the partials.
@@ -41,11 +42,9 @@ __device__ __forceinline__ void prefix_tile(char* lds, const PrefixArgs& a, int 
   if (lo < hi) {
     const int n = length_of(s, a.kv.seq_lens, b);
     const int limit = valid ? (n < hi ? n : hi) : 0;
-    typename RowState<Op, kTerms>::Query q;
-    q.load(a.q + ((int64_t)b * s.Hq + head) * kD, h);
     const CacheRows<TK> K(a.kv.k, a.kv, from, g);
     const CacheRows<TV> V(a.kv.v, a.kv, from, g);
-    tile_loop<TK, TV, Op, kTerms, kKeyWaves>(lds, K, V, lo, hi, q, limit, st);
+    tile_loop<TK, TV, kKeyWaves>(lds, K, V, lo, hi, [&](auto& q) { q.load(a.q + ((int64_t)b * s.Hq + head) * kD, h); }, limit, st);
   }
   RowOut<float> to = {nullptr, nullptr};
   if (valid) to.part = a.part + (((int64_t)b * s.Hq + head) * a.splits + slot) * kPartFloats;
@@ -78,18 +77,96 @@ __device__ __forceinline__ void prefix_pipe(char* lds, const PrefixArgs& a, int 
   if (valid) st.finish((float*)nullptr, a.part + (((int64_t)b * s.Hq + head) * a.splits + slot) * kPartFloats, h);
 }
 
+// The items of the rows that requests have for themselves, by one workgroup: as many rows an item as make kOwnWorkgroups workgroups of
+// all, kOwnLeast at least, and no more items of a request than k_prefix_merge takes.
+__device__ __forceinline__ int own_item_rows(int64_t total, int most, int wanted) {
+  int64_t per = (total + wanted - 1) / wanted;
+  const int64_t of_longest = (most + kMaxSplits - 1) / kMaxSplits;
+  per = per > of_longest ? per : of_longest;
+  return per <= kOwnLeast ? kOwnLeast : (int)((per + 15) & ~(int64_t)15);
+}
+__device__ __forceinline__ void plan_own(char* lds, const PrefixArgs& a) {
+  const Shape& s = a.s;
+  const int lane = threadIdx.x & 63, wave = wave_of(), waves = blockDim.x >> 6;
+  int64_t* const sums = reinterpret_cast<int64_t*>(lds);           // [waves], and behind them the waves' largest
+  int* const largest = reinterpret_cast<int*>(sums + 8);
+  int64_t total = 0;
+  int most = 0;
+  for (int b = threadIdx.x; b < s.B; b += blockDim.x) {
+    int lo = 0, hi = a.groups.n - 1;                              // the last group that begins at b or before
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (a.groups.start[mid] <= b) lo = mid;
+      else hi = mid - 1;
+    }
+    int b0, b1, shared;
+    group_at(s, a.kv.seq_lens, a.groups, lo, &b0, &b1, &shared);
+    const int n = length_of(s, a.kv.seq_lens, b), first = b < b0 || b >= b1 ? -1 : min(shared, n), mine = first < 0 ? 0 : n - first;
+    a.own.first[b] = first;
+    total += mine;
+    most = max(most, mine);
+  }
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    total += __shfl_xor(total, d);
+    most = max(most, __shfl_xor(most, d));
+  }
+  if (lane == 0) {
+    sums[wave] = total;
+    largest[wave] = most;
+  }
+  __syncthreads();
+  total = 0;
+  for (int w = 0; w < waves; ++w) {
+    total += sums[w];
+    most = max(most, largest[w]);
+  }
+  const int per = own_item_rows(total, most, own_items_most(s) - s.B);
+  int* const counts = largest + 8;                                 // [2][waves]
+  int base = 0, turn = 0;
+  for (int b_first = 0; b_first < s.B; b_first += blockDim.x, turn ^= 8) {
+    const int b = b_first + threadIdx.x;
+    int first = 0, n = 0;
+    if (b < s.B) {
+      first = a.own.first[b];                                      // (my own store)
+      n = first < 0 ? first : length_of(s, a.kv.seq_lens, b);
+    }
+    const int items = (n - first + per - 1) / per;
+    int upto = items;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const int x = __shfl_up(upto, d);
+      if (lane >= d) upto += x;
+    }
+    if (lane == 63) counts[turn + wave] = upto;
+    __syncthreads();
+    int at = base + upto - items;
+    for (int w = 0; w < waves; ++w) {
+      if (w < wave) at += counts[turn + w];
+      base += counts[turn + w];
+    }
+    if (b < s.B) {
+      a.own.item[b] = at;
+      for (int r = first; r < n; r += per) a.own.items[at++] = OwnItem{b, r, min(r + per, n), 0};
+    }
+  }
+  if (threadIdx.x == 0) a.own.item[s.B] = base;
+}
+
 // Query rows of a workgroup of k_prefix_shared.
 template <typename TK, int kKeyWaves>
 constexpr int shared_rows() { return kKeyWaves == 1 && sizeof(TK) != 4 ? kPipeRows : 32 * (4 / kKeyWaves); }
 
 }  // namespace
 
-// grid Hkv * splits * tiles
+// grid 1 + Hkv * splits * tiles
 template <typename TK, typename TV, int kKeyWaves, int kKind>
 __global__ __launch_bounds__((shared_rows<TK, kKeyWaves>() == kPipeRows ? kPipeThreads : kTileThreads)) void k_prefix_shared(PrefixArgs a) {
+  request_arguments<decltype(&k_prefix_shared<TK, TV, kKeyWaves, kKind>)>();
   constexpr int kRows = shared_rows<TK, kKeyWaves>();
   __shared__ __attribute__((aligned(16))) char lds[kRows == kPipeRows ? kPipeLds : tile_lds<TK, TV, kKeyWaves>()];
-  const int g = blockIdx.x % a.s.Hkv, x0 = blockIdx.x / a.s.Hkv, split = x0 % a.splits, x = x0 / a.splits;
+  if (blockIdx.x == 0) return plan_own(lds, a);
+  const int block = blockIdx.x - 1, g = block % a.s.Hkv, x0 = block / a.s.Hkv, split = x0 % a.splits, x = x0 / a.splits;
   const int per = kRows / a.s.G;
   auto first_tile = [&](int i) {
     const int b = a.groups.start[i];
@@ -108,15 +185,15 @@ __global__ __launch_bounds__((shared_rows<TK, kKeyWaves>() == kPipeRows ? kPipeT
 
 // a wave a (request, head)
 __global__ __launch_bounds__(kTileThreads) void k_prefix_merge(PrefixArgs a, float* __restrict__ out) {
+  request_arguments<decltype(&k_prefix_merge)>();
   const Shape& s = a.s;
   const int row = blockIdx.x * (kTileThreads / 64) + wave_of();
   if (row >= s.B * s.Hq) return;
-  const int b = row / s.Hq, h = row % s.Hq, first = first_own_row(s, a.kv.seq_lens, a.groups, b);
-  if (first < 0) return;
-  const int n = length_of(s, a.kv.seq_lens, b), own = first < n ? own_parts(n - first, a.own_splits) : 0;
+  const int b = row / s.Hq, h = row % s.Hq, item = a.own.item[b], own = a.own.item[b + 1] - item;
+  if (a.own.first[b] < 0) return;
   const float* const part = a.part + (int64_t)row * a.splits * kPartFloats;
-  const int64_t step = (int64_t)s.G * (kD + 2);
-  const float* const mine = a.own_part + ((int64_t)(b * s.Hkv + h / s.G) * a.own_splits) * step + (int64_t)(h % s.G) * (kD + 2);
+  const int64_t step = (int64_t)s.Hkv * s.G * (kD + 2);
+  const float* const mine = a.own_part + item * step + (int64_t)h * (kD + 2);
   const float unit = s.G == 1 ? 1.f : kLog2e;                 // (with grouping those parts' scores are natural ones)
   auto at = [&](int i) { return i < a.splits ? part + (int64_t)i * kPartFloats : mine + (i - a.splits) * step; };
   put2(out + (int64_t)row * kD + 2 * (threadIdx.x & 63),
@@ -130,22 +207,22 @@ hipError_t prefix_t(PrefixArgs a, int dtype, float* out, int64_t part_rows, hipS
   const Shape& s = a.s;
   const int64_t heads = (int64_t)s.B * s.Hq;
   // The rows of a group of ordinary size decide how many a workgroup takes: more share a row of the cache, fewer leave no wave idle.
-  const int rows = (s.B + a.groups.n - 1) / a.groups.n * s.G;
+  const int size = (s.B + a.groups.n - 1) / a.groups.n, rows = size * s.G;
   const int key_waves = rows > 64 ? 1 : (rows > 32 || sizeof(TK) == 4 ? 2 : 4);
   const int per = key_waves == 1 ? shared_rows<TK, 1>() : 32 * (4 / key_waves);
-  const int tiles = s.B / (per / s.G) + a.groups.n;
-  auto parts = [&](int64_t wanted, int64_t groups, int64_t most) {
-    int64_t n = (wanted + groups - 1) / groups;
-    const int64_t by_len = (s.Lcap + 255) / 256;
-    if (n > by_len) n = by_len;
-    if (n > most) n = most;
-    return (int)(n < 1 ? 1 : n);
-  };
-  const int64_t room = part_rows / heads;                   // at least 2
-  a.own_splits = parts(2048, (int64_t)s.B * s.Hkv, room / 2 < kMaxSplits ? room / 2 : kMaxSplits);
-  a.splits = parts(per == kPipeRows ? 256 : 512, (int64_t)tiles * s.Hkv, room - a.own_splits < kMaxSplits ? room - a.own_splits : kMaxSplits);
+  const int tiles = s.B / (per / s.G) + a.groups.n;          // room for any groups; of groups of one size there are `usual`
+  const int64_t usual = (int64_t)a.groups.n * ((size * s.G + per - 1) / per);
+  // The workspace: parts of the shared rows; the plan of the own ones, and their parts.
+  const int64_t own_rows = (int64_t)own_items_most(s) * s.Hq, plan_rows = (own_plan_ints(s) + kPartFloats - 1) / kPartFloats;
+  const int64_t room = (part_rows - own_rows - plan_rows) / heads, by_len = (s.Lcap + 127) / 128;          // room: at least 1
+  int64_t splits = (256 + usual * s.Hkv - 1) / (usual * s.Hkv);
+  for (const int64_t most : {room, by_len, (int64_t)kMaxSplits}) splits = splits < most ? splits : most;
+  a.splits = (int)splits;
   a.own_part = a.part + heads * a.splits * kPartFloats;
-  const unsigned grid = (unsigned)(s.Hkv * a.splits * tiles);
+  a.own.items = reinterpret_cast<OwnItem*>(a.own_part + own_rows * kPartFloats);
+  a.own.first = reinterpret_cast<int32_t*>(a.own.items + own_items_most(s));
+  a.own.item = a.own.first + s.B;
+  const unsigned grid = 1 + (unsigned)(s.Hkv * a.splits * tiles);
 #define LFPS_SHARED(KW, KIND) \
   hipLaunchKernelGGL((k_prefix_shared<TK, TV, KW, KIND>), dim3(grid), dim3(per == kPipeRows ? kPipeThreads : kTileThreads), 0, st, a)
   const int kind = sizeof(TK) == 4 ? kAnyRows : rows_kind(a.kv);
@@ -157,7 +234,7 @@ hipError_t prefix_t(PrefixArgs a, int dtype, float* out, int64_t part_rows, hipS
     else LFPS_SHARED(1, kPages);
   }
 #undef LFPS_SHARED
-  const hipError_t e = launch_full_attn_own(s, dtype, a.q, a.kv, a.groups, a.own_part, a.own_splits, st);
+  const hipError_t e = launch_full_attn_own(s, dtype, a.q, a.kv, a.own, a.own_part, st);
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL(k_prefix_merge, dim3((unsigned)((heads + 3) / 4)), dim3(kTileThreads), 0, st, a, out);
   return hipGetLastError();
@@ -167,7 +244,7 @@ hipError_t prefix_t(PrefixArgs a, int dtype, float* out, int64_t part_rows, hipS
 
 hipError_t launch_prefix_attn(const Shape& s, int dtype, const KvView& kv, const float* q, const int32_t* group_start,
                               const int32_t* prefix_len, int n_groups, float* out, float* part, int64_t part_rows, hipStream_t st) {
-  const PrefixArgs a = {s, kv, q, {group_start, prefix_len, n_groups}, part, nullptr, 1, 1};
+  const PrefixArgs a = {s, kv, q, {group_start, prefix_len, n_groups}, part, {}, nullptr, 1};
   if (dtype == LFPS_F32) return prefix_t<float, float>(a, dtype, out, part_rows, st);
   if (dtype == LFPS_F16) return prefix_t<_Float16, _Float16>(a, dtype, out, part_rows, st);
   if (kv.k_fp8 && kv.v_fp8) return prefix_t<uint8_t, uint8_t>(a, dtype, out, part_rows, st);

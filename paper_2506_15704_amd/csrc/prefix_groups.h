@@ -41,22 +41,20 @@ __device__ __forceinline__ void group_at(const Shape& s, const int32_t* seq_lens
   const int n = *b0 < s.B ? length_of(s, seq_lens, *b0) : 0;
   *shared = m < 0 ? 0 : (m > n ? n : m);
 }
-// The first row that request b has for itself; below 0: it is in no group.  The whole wave calls.
-__device__ __forceinline__ int first_own_row(const Shape& s, const int32_t* seq_lens, const PrefixGroups& p, int b) {
-  const int i = last_not_above(p.n - 1, b, [&](int j) { return p.start[j]; });
-  int b0, b1, shared;
-  group_at(s, seq_lens, p, i, &b0, &b1, &shared);
-  return b >= b0 && b < b1 ? shared : -1;
-}
 
-// Full attention of every request over the rows that it has for itself: part [B, Hkv, n_split, G, D + 2], of which a request over n
-// such rows has own_parts(n, n_split), each as in the full-attention baseline.
-__host__ __device__ __forceinline__ int rows_per_split(int n, int n_split) { return (((n + n_split - 1) / n_split) + 15) & ~15; }
-__host__ __device__ __forceinline__ int own_parts(int n, int n_split) {
-  const int per = rows_per_split(n, n_split);
-  return (n + per - 1) / per;
-}
-hipError_t launch_full_attn_own(const Shape& s, int dtype, const float* q, const KvView& kv, const PrefixGroups& groups, float* part,
-                                int n_split, hipStream_t st);
+// The rows that the requests have for themselves, cut into items of no more than some number of rows, the same for all: what their lengths
+// ask for, so that a long request is cut into many and a short one into one.  Made by plan_own, once a call, on the device.
+struct OwnItem { int32_t b, begin, end, unused; };
+struct OwnRows {
+  int32_t* first;            // [B] a request's first row of its own; below 0: it is in no group
+  int32_t* item;             // [B + 1] its first item; of B: the number of all
+  OwnItem* items;            // [own_items_most]
+};
+constexpr int kOwnWorkgroups = 1024, kOwnLeast = 64;         // wanted of the kernel over the items; rows that one has at least
+__host__ __device__ inline int own_items_most(const Shape& s) { return (s.Hkv < kOwnWorkgroups ? kOwnWorkgroups / s.Hkv : 1) + s.B; }
+inline int64_t own_plan_ints(const Shape& s) { return 4 * (int64_t)own_items_most(s) + 2 * s.B + 1; }
+
+// Full attention over the items' rows: part [items, Hkv, G, D + 2], each as of a part in the full-attention baseline.
+hipError_t launch_full_attn_own(const Shape& s, int dtype, const float* q, const KvView& kv, const OwnRows& own, float* part, hipStream_t st);
 
 }  // namespace lfps

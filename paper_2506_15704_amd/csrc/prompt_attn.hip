@@ -70,11 +70,9 @@ __device__ __forceinline__ void prompt_tile(char* lds, const PromptArgs<TQ>& a, 
   RowState<Op, 1> st;
   st.clear();
   if (lo < hi) {
-    typename RowState<Op, 1>::Query q;
-    q.load(a.q + (int64_t)(c0 + token) * a.q_stride + head * kD, h);
     const CacheRows<TK> K(a.kv.k, a.kv, b, g);
     const CacheRows<TV> V(a.kv.v, a.kv, b, g);
-    tile_loop<TK, TV, Op, 1, kKeyWaves>(lds, K, V, lo, hi, q, limit, st);
+    tile_loop<TK, TV, kKeyWaves>(lds, K, V, lo, hi, [&](auto& q) { q.load(a.q + (int64_t)(c0 + token) * a.q_stride + head * kD, h); }, limit, st);
   }
   RowOut<TQ> to = {nullptr, nullptr};
   if (valid) {
@@ -153,6 +151,7 @@ __global__ __launch_bounds__(tile_threads<TK>(), sizeof(TK) == 4 ? 1 : 2) void k
 // grid Hkv * few_splits * B
 template <typename TK, typename TV, typename TQ>
 __global__ __launch_bounds__(kTileThreads) void k_prompt_few(PromptArgs<TQ> a) {
+  request_arguments<decltype(&k_prompt_few<TK, TV, TQ>)>();
   constexpr int kKeyWaves = few_key_waves<TK>();
   __shared__ __attribute__((aligned(16))) char lds[tile_lds<TK, TV, kKeyWaves>()];
   const int g = blockIdx.x % a.s.Hkv, x0 = blockIdx.x / a.s.Hkv, split = x0 % a.few_splits, b = x0 / a.few_splits;
@@ -166,6 +165,7 @@ __global__ __launch_bounds__(kTileThreads) void k_prompt_few(PromptArgs<TQ> a) {
 // of every token of the other requests.
 template <typename TQ>
 __global__ __launch_bounds__(kTileThreads) void k_prompt_merge(PromptArgs<TQ> a, int few, int most) {
+  request_arguments<decltype(&k_prompt_merge<TQ>)>();
   const int Hq = a.s.Hq, x = blockIdx.x * (kTileThreads / 64) + wave_of(), head = x % Hq, y = x / Hq;
   int b, i, c0, c1;
   if (few) {
@@ -195,11 +195,11 @@ hipError_t prompt_t(const Shape& s, const KvView& kv, const void* q, int64_t q_s
   constexpr int kMost = few_most<TK>();
   PromptArgs<TQ> a = {s, kv, (const TQ*)q, q_stride, cu, n_tokens, (TQ*)out, part, 1, 0, 0, 0};
   const int per = tile_query_rows<TK>() / s.G;
-  // As many parts as give every CU two workgroups, where the rows' partial results have room.
+  // As many parts as give every CU a workgroup (either kernel's LDS has room for one), where the rows' partial results have room.
   auto parts = [&](int64_t groups, int64_t rows, int64_t room) {
-    int64_t n = (512 + groups - 1) / groups;
+    int64_t n = (256 + groups - 1) / groups;
     if (n * rows > room) n = room / rows;
-    const int64_t by_len = (s.Lcap + 255) / 256;
+    const int64_t by_len = (s.Lcap + 127) / 128;
     if (n > by_len) n = by_len;
     if (n > kMaxSplits) n = kMaxSplits;
     return (int)(n < 1 ? 1 : n);

@@ -75,22 +75,37 @@ struct StageFeed {
   static constexpr bool kDirect = sizeof(T) > 1;
   static constexpr int kPieces = kD * (int)sizeof(T) / 16, kRowsOfLoad = 64 / kPieces, kLoads = kRows / kRowsOfLoad;
   u32x4 x[kDirect ? 1 : kLoads];
-  int e[kLoads];                                                          // the block table's entries of the stage that is asked for next
 
   __device__ __forceinline__ static int row(int i, int lane) { return kRows * wave_of() + kRowsOfLoad * i + lane / kPieces; }
   __device__ __forceinline__ static int piece(int i, int lane) {          // of a row of the cache, in bytes
     const int place = lane % kPieces, r = row(i, lane);
     return 16 * (!kDirect ? place : (sizeof(T) == 4 ? chunk_place_f32(r, place) : chunk_place(r, place)));
   }
-  __device__ __forceinline__ void look_up(const CacheRows<T>& c, int k0, int end, int lane) {
-    if (!c.pg.table) return;
+  // Where the rows of a stage lie.  The block table's entries are read a stage before they are used, and all places are made before
+  // any row is asked for: waits for an entry are waits for every row that is on its way to LDS (16 of them, one after the other, were
+  // 4.8 us of the 15 of a workgroup over 128 rows).  K and V of one element size lie at the same offsets.
+  struct Places {
+    int e[kLoads];
+    int64_t off[kLoads];
+    __device__ __forceinline__ void look_up(const CacheRows<T>& c, int k0, int end, int lane) {
+      if (!c.pg.table) return;
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) e[i] = c.entry(min(k0 + row(i, lane), end - 1));
-  }
-  __device__ __forceinline__ void ask(const CacheRows<T>& c, lds_char* stage, int k0, int end, int lane) {
+      for (int i = 0; i < kLoads; ++i) e[i] = c.entry(min(k0 + row(i, lane), end - 1));
+    }
+    __device__ __forceinline__ void aim(const CacheRows<T>& c, int k0, int end, int lane) {
+      if (c.pg.table) {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) off[i] = RowMap<true>::offset_in(c.pg, e[i], min(k0 + row(i, lane), end - 1), c.stride_b, c.stride_n);
+      } else {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) off[i] = (int64_t)min(k0 + row(i, lane), end - 1) * c.stride_n;
+      }
+    }
+  };
+  __device__ __forceinline__ void ask(const CacheRows<T>& c, const int64_t (&off)[kLoads], lds_char* stage, int lane) {
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
-      const char* p = reinterpret_cast<const char*>(c.at(min(k0 + row(i, lane), end - 1), e[i])) + piece(i, lane);
+      const char* p = reinterpret_cast<const char*>(c.base + off[i]) + piece(i, lane);
       if constexpr (kDirect)
         __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) char*)p,
                                          (__attribute__((address_space(3))) void*)(stage + (kRows * wave_of() + kRowsOfLoad * i) * InLds<T>::kRowBytes), 16, 0, 0);
@@ -412,11 +427,12 @@ constexpr int tile_lds() {
 template <typename T>
 constexpr int few_key_waves() { return sizeof(T) == 4 ? 2 : 4; }
 
+// load_q: brings the query operand, which nothing waits for until the first rows have been asked for.
 // The loop of a workgroup whose four waves are kRowWaves rows of waves (32 query rows each) by kKeyWaves (which share a stage's
 // keys).  q, limit: my query row's operand and the keys it sees.  wave_limit: the most that a row of my wave sees, and least.
-template <typename TK, typename TV, typename Op, int kTerms, int kKeyWaves>
-__device__ __forceinline__ void tile_loop(char* lds, const CacheRows<TK>& K, const CacheRows<TV>& V, int first, int end,
-                                          const typename RowState<Op, kTerms>::Query& q, int limit, RowState<Op, kTerms>& st) {
+template <typename TK, typename TV, int kKeyWaves, typename Op, int kTerms, typename LoadQ>
+__device__ __forceinline__ void tile_loop(char* lds, const CacheRows<TK>& K, const CacheRows<TV>& V, int first, int end, LoadQ load_q,
+                                          int limit, RowState<Op, kTerms>& st) {
   constexpr int kRows = tile_rows(kKeyWaves), kBlocks = kRows / 32 / kKeyWaves;
   constexpr int kStageK = stage_bytes<TK>(kRows), kStage = kStageK + stage_bytes<TV>(kRows);
   const int lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5, mine = (wave_of() % kKeyWaves) * kBlocks * 32;
@@ -431,13 +447,20 @@ __device__ __forceinline__ void tile_loop(char* lds, const CacheRows<TK>& K, con
   lds_char* const stages = (lds_char*)lds;
   StageFeed<TK, kRows / 4> fk;
   StageFeed<TV, kRows / 4> fv;
+  typename decltype(fk)::Places pk;
+  typename decltype(fv)::Places pv;
+  constexpr bool kAlike = sizeof(TK) == sizeof(TV);
   auto look_up = [&](int k) {
-    fk.look_up(K, k, end, lane);
-    fv.look_up(V, k, end, lane);
+    pk.look_up(K, k, end, lane);
+    if constexpr (!kAlike) pv.look_up(V, k, end, lane);
   };
   auto ask = [&](int k, int to) {
-    fk.ask(K, stages + to, k, end, lane);
-    fv.ask(V, stages + to + kStageK, k, end, lane);
+    pk.aim(K, k, end, lane);
+    if constexpr (!kAlike) pv.aim(V, k, end, lane);
+    __builtin_amdgcn_sched_barrier(0);
+    fk.ask(K, pk.off, stages + to, lane);
+    if constexpr (kAlike) fv.ask(V, pk.off, stages + to + kStageK, lane);
+    else fv.ask(V, pv.off, stages + to + kStageK, lane);
   };
   auto put = [&](int to) {
     fk.put(stages + to, lane);
@@ -445,7 +468,9 @@ __device__ __forceinline__ void tile_loop(char* lds, const CacheRows<TK>& K, con
   };
   look_up(first);
   ask(first, 0);
-  look_up(first + kRows);
+  if (first + kRows < end) look_up(first + kRows);
+  typename RowState<Op, kTerms>::Query q;
+  load_q(q);
   put(0);
   int at = 0;
   for (int k0 = first; k0 < end; k0 += kRows, at = kStage - at) {
@@ -454,7 +479,7 @@ __device__ __forceinline__ void tile_loop(char* lds, const CacheRows<TK>& K, con
     __syncthreads();                          // and what all did; nobody reads the other stage any more
     if (more) {
       ask(k0 + kRows, kStage - at);
-      look_up(k0 + 2 * kRows);
+      if (k0 + 2 * kRows < end) look_up(k0 + 2 * kRows);
     }
     const char* k = lds + at + mine * InLds<TK>::kRowBytes;
     const char* v = lds + at + kStageK + mine * InLds<TV>::kRowBytes;
@@ -608,11 +633,11 @@ __device__ __forceinline__ f32x2t join_parts(int n, At at, Score score, Sum sum)
   return f32x2t{a[0] * inv, a[1] * inv};
 }
 
-// Part `split` of n of the rows [first, end): whole stages, and no part smaller than two of them while another has rows.
+// Part `split` of n of the rows [first, end): whole stages.
 __device__ __forceinline__ void split_rows(int first, int end, int n, int split, int stage, int* lo, int* hi) {
   int per = (end - first + n - 1) / n;
   per = (per + stage - 1) / stage * stage;
-  per = per < 2 * stage ? 2 * stage : per;
+  per = per < stage ? stage : per;
   const int64_t at = first + (int64_t)split * per;
   *lo = at < end ? (int)at : end;
   *hi = at + per < end ? (int)(at + per) : end;

@@ -277,9 +277,11 @@ __device__ __forceinline__ void pipe_loop(char* lds_, const CacheRows<TK>& K, co
   int* const found = (int*)(lds_ + 2 * kPipeStages * kPipeStage) + (late ? 1 : 0);      // stage (its end) with a value that is not finite
   if ((threadIdx.x & (64 * kPipeWaves / 2 - 1)) == 0) *found = 0;
   auto landed = [] { __builtin_amdgcn_s_waitcnt(0x0f70); };     // vmcnt(0): what I asked for is in LDS
+  int e_v = look_up(first + 2 * kPipeKeys), e_k = look_up(first + 3 * kPipeKeys), e_new = 0;      // of the next to be asked for
+  const int e_first[3] = {look_up(first), look_up(first + kPipeKeys), e_v};
 #pragma unroll
   for (int i = 0; i < 3; ++i) {                                  // K of the first three stages, V of two
-    const int k = first + i * kPipeKeys, e = uniform(look_up(k));
+    const int k = first + i * kPipeKeys, e = uniform(e_first[i]);
     fk.aim(K, row_of(k), end, e, lane);
     fk.ask(lds + i * kPipeStage, wave);
     fk.put(lds + i * kPipeStage, lane, wave);
@@ -289,11 +291,11 @@ __device__ __forceinline__ void pipe_loop(char* lds_, const CacheRows<TK>& K, co
       fv.put(lds + kV + i * kPipeStage, lane, wave);
     }
   }
-  int e_v = look_up(first + 2 * kPipeKeys), e_k = look_up(first + 3 * kPipeKeys), e_new = 0;      // of the next to be asked for
   landed();
   __syncthreads();
   f32x16 s[2];                                // scores of a stage
-  Op w[4], a[3][4];                           // its weights; operands
+  constexpr int kAhead = kTerms == 1 ? 2 : 1, kOperands = kAhead + 1;      // groups read ahead (of two terms a group is twice as long)
+  Op w[4], a[kOperands][4];                   // its weights; operands
 #pragma unroll
   for (int g = 0; g < 4; ++g) {
     st.load_keys(a[0], lds, g, n, h);
@@ -328,8 +330,8 @@ __device__ __forceinline__ void pipe_loop(char* lds_, const CacheRows<TK>& K, co
       if (any_not_finite<Op>(v + (wave % (kPipeWaves / 2)) * kShare, kShare)) *found = k0 + kPipeKeys;
     }
     if constexpr (kWorks) {
-      st.load_values(a[0], v, 0, lane);
-      st.load_values(a[1], v, 1, lane);
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) st.load_values(a[i], v, i, lane);
     }
     __syncthreads();
     // matrix half
@@ -339,11 +341,12 @@ __device__ __forceinline__ void pipe_loop(char* lds_, const CacheRows<TK>& K, co
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         __builtin_amdgcn_sched_barrier(0);
-        if (i < 2) st.load_values(a[(i + 2) % 3], v, i + 2, lane);
-        else if (i < 6) st.load_keys(a[(i + 2) % 3], k, i - 2, n, h);
+        const int to = i + kAhead;
+        if (to < 4) st.load_values(a[to % kOperands], v, to, lane);
+        else if (to < 8) st.load_keys(a[to % kOperands], k, to - 4, n, h);
         if (i < 4) {
-          if (!apart) st.add_values(a[i % 3], w[i], s, i);
-        } else st.add_scores(s, a[i % 3], i - 4);
+          if (!apart) st.add_values(a[i % kOperands], w[i], s, i);
+        } else st.add_scores(s, a[i % kOperands], i - 4);
         if (i == 2) e_new = look_up(k0 + 4 * kPipeKeys);
         if (i == 3) fk.ask(lds + now, wave);
         if (i == 4) fv.ask(lds + kV + last, wave);
