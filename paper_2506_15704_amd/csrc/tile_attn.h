@@ -235,9 +235,9 @@ __device__ __forceinline__ void add_apart(f32x16 (&o)[4], Weight weight, const l
       for (int r = 0; r < 16; r += 4) {
         float x[4];
         if constexpr (std::is_same<Op, float>::value) {
-          const f32x4 y = *(const __attribute__((address_space(3))) f32x4*)(v + key * 512 + 16 * chunk_place_f32(key, 8 * d + r / 2 + h));
 #pragma unroll
-          for (int i = 0; i < 4; ++i) x[i] = y[i];
+          for (int i = 0; i < 4; ++i)
+            x[i] = *(const __attribute__((address_space(3))) float*)(v + key * 512 + 16 * chunk_place_f32(key, 2 * r + 4 * h + i) + 4 * d);
         } else {
           typedef typename std::conditional<std::is_same<Op, bf16x8>::value, __bf16, _Float16>::type Elem;
           typedef Elem Elem4 __attribute__((ext_vector_type(4)));
@@ -270,7 +270,7 @@ struct RowState {
   static constexpr int kRowBytes = kF32 ? 512 : 256;
   // Weights of fp16 values are held 2^14 (2^8 with one term) times as large, or those below 2^-24 of the row's largest would be lost.
   static constexpr float kLift = std::is_same<Op, f16x8>::value ? (kTerms == 1 ? 8.f : 14.f) : 0.f;
-  f32x16 o[4];                               // channels 32 d + 8 (r / 4) + 4 h + r % 4 of row n
+  f32x16 o[4];                               // of row n: with i = 8 (r / 4) + 4 h + r % 4, channel 32 d + i, of fp32 operands 4 i + d
   float m, l;                                // largest score so far, in powers of two; the sum of the weights of my half's keys
 
   __device__ __forceinline__ void clear() {
@@ -370,13 +370,11 @@ struct RowState {
     if constexpr (kF32) {
       const int h = lane >> 5, n = lane & 31;
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
+      for (int r = 0; r < 16; ++r) {                             // (a lane's four channels are one read)
         const int key = 8 * (r / 4) + 4 * h + r % 4;
+        const f32x4 x = *reinterpret_cast<const f32x4*>(v + key * 512 + 16 * chunk_place_f32(key, n));
 #pragma unroll
-        for (int d = 0; d < 4; ++d) {
-          const int c = 32 * d + n;
-          o[d] = mfma32(*reinterpret_cast<const float*>(v + key * 512 + 16 * chunk_place_f32(key, c >> 2) + 4 * (c & 3)), p[r], o[d]);
-        }
+        for (int d = 0; d < 4; ++d) o[d] = mfma32(x[d], p[r], o[d]);
       }
     } else {
 #pragma unroll
@@ -475,8 +473,14 @@ __device__ __forceinline__ void tile_loop(char* lds, const CacheRows<TK>& K, con
   int at = 0;
   for (int k0 = first; k0 < end; k0 += kRows, at = kStage - at) {
     const bool more = k0 + kRows < end;
-    __builtin_amdgcn_s_waitcnt(0x0f70);       // vmcnt(0): what I asked for is in LDS
-    __syncthreads();                          // and what all did; nobody reads the other stage any more
+    if constexpr (kKeyWaves == 4) {           // a wave reads the rows that it brings, and no others
+      wave_lds_order();
+      __builtin_amdgcn_s_waitcnt(0x0070);     // vmcnt(0) lgkmcnt(0): they are in LDS, and the other stage has been read
+      wave_lds_order();
+    } else {
+      __builtin_amdgcn_s_waitcnt(0x0f70);     // vmcnt(0)
+      __syncthreads();                        // what all asked for is there; nobody reads the other stage any more
+    }
     if (more) {
       ask(k0 + kRows, kStage - at);
       if (k0 + 2 * kRows < end) look_up(k0 + 2 * kRows);
@@ -493,6 +497,15 @@ __device__ __forceinline__ void tile_loop(char* lds, const CacheRows<TK>& K, con
     }
     if (more) put(kStage - at);
   }
+}
+
+// My four channels from the returned one on, of o[d][r .. r + 3] (fp32 operands: of o[0 .. 3][r + d]).
+template <typename Op>
+__device__ __forceinline__ int four_channels(const f32x16 (&o)[4], int d, int r, int h, f32x4* x) {
+  constexpr bool kF32 = std::is_same<Op, float>::value;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) (*x)[i] = kF32 ? o[i][r + d] : o[d][r + i];
+  return kF32 ? 4 * (2 * r + 4 * h + d) : 32 * d + 2 * r + 4 * h;
 }
 
 // Where a row's result goes: the output row, or a partial.  Both null: nowhere.
@@ -526,8 +539,11 @@ __device__ __forceinline__ void tile_finish(char* lds, RowState<Op, kTerms>& st,
 #pragma unroll
     for (int d = 0; d < 4; ++d)
 #pragma unroll
-      for (int r = 0; r < 16; r += 4)
-        *reinterpret_cast<f32x4*>(mine + 32 * d + 2 * r + 4 * h) = f32x4{st.o[d][r], st.o[d][r + 1], st.o[d][r + 2], st.o[d][r + 3]};
+      for (int r = 0; r < 16; r += 4) {
+        f32x4 x;
+        const int c = four_channels<Op>(st.o, d, r, h, &x);
+        *reinterpret_cast<f32x4*>(mine + c) = x;
+      }
     if (h == 0) {
       mine[kD] = st.m;
       mine[kD + 1] = st.l;
@@ -571,8 +587,9 @@ __device__ __forceinline__ void tile_finish(char* lds, RowState<Op, kTerms>& st,
   for (int j = 0; j < kMine; ++j)
 #pragma unroll
     for (int r = 0; r < 16; r += 4) {
-      const int c = 32 * (d0 + j) + 2 * r + 4 * h;
-      const f32x4 x = {st.o[j][r], st.o[j][r + 1], st.o[j][r + 2], st.o[j][r + 3]};
+      f32x4 x = {st.o[j][r], st.o[j][r + 1], st.o[j][r + 2], st.o[j][r + 3]};
+      int c = 32 * (d0 + j) + 2 * r + 4 * h;
+      if constexpr (kKeyWaves == 1) c = four_channels<Op>(st.o, j, r, h, &x);
       if (to.part) put4(to.part + c, x);
       else if (to.out) put4(to.out + c, f32x4{x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv});
     }
