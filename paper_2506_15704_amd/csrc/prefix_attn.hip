@@ -24,10 +24,14 @@ struct PrefixArgs {
   int32_t splits;
 };
 
+// FP8 keys and values are fp16 operands here: two fp16 terms hold a query or a weight to 22 bits, of bf16 ones it takes three.
+template <typename TK, typename TV>
+using PrefixOp = typename std::conditional<sizeof(TK) == 1 && sizeof(TV) == 1, f16x8, typename InLds<TK>::Op>::type;
+
 // Query rows (member, head) from row0 on of the requests from b0 to b1, over rows [lo, hi) of request `from`; slot: of the partials.
 template <typename TK, typename TV, int kKeyWaves>
 __device__ __forceinline__ void prefix_tile(char* lds, const PrefixArgs& a, int b0, int b1, int row0, int g, int from, int lo, int hi, int slot) {
-  typedef typename InLds<TK>::Op Op;
+  typedef PrefixOp<TK, TV> Op;
   constexpr int kTerms = std::is_same<Op, float>::value ? 1 : 2;
   const Shape& s = a.s;
   const int G = s.G, shift = G == 4 ? 2 : G - 1;
@@ -54,7 +58,7 @@ __device__ __forceinline__ void prefix_tile(char* lds, const PrefixArgs& a, int 
 // The same for 256 rows of 16-bit operands, with the loop of tile_pipe.h.
 template <int kKind, typename TK, typename TV>
 __device__ __forceinline__ void prefix_pipe(char* lds, const PrefixArgs& a, int b0, int b1, int row0, int g, int lo, int hi, int slot) {
-  typedef typename InLds<TK>::Op Op;
+  typedef PrefixOp<TK, TV> Op;
   const Shape& s = a.s;
   const int G = s.G, shift = G == 4 ? 2 : G - 1, lane = threadIdx.x & 63, h = lane >> 5, rows = (b1 - b0) << shift;
   int m = row0 + 32 * wave_of() + (lane & 31);
@@ -69,7 +73,7 @@ __device__ __forceinline__ void prefix_pipe(char* lds, const PrefixArgs& a, int 
     for (int i = b0 + row0 / G + lane; i < b1 && i < b0 + (row0 + kPipeRows) / G; i += 64) least = min(least, length_of(s, a.kv.seq_lens, i));
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) least = min(least, __shfl_xor(least, d));
-    st.q.load(a.q + ((int64_t)b * s.Hq + head) * kD, h);
+    st.q.load(a.q + ((int64_t)b * s.Hq + head) * kD, h, PipeState<Op, 2>::kRest ? (lds_char*)lds + kRestAt + wave_of() * kRestWave : nullptr);
     const CacheRows<TK> K(a.kv.k, a.kv, b0, g);
     const CacheRows<TV> V(a.kv.v, a.kv, b0, g);
     pipe_loop<kKind, TK, TV>(lds, K, V, lo, hi, __builtin_amdgcn_readfirstlane(least), row0 + 32 * wave_of() < rows, st);
@@ -164,7 +168,7 @@ template <typename TK, typename TV, int kKeyWaves, int kKind>
 __global__ __launch_bounds__((shared_rows<TK, kKeyWaves>() == kPipeRows ? kPipeThreads : kTileThreads)) void k_prefix_shared(PrefixArgs a) {
   request_arguments<decltype(&k_prefix_shared<TK, TV, kKeyWaves, kKind>)>();
   constexpr int kRows = shared_rows<TK, kKeyWaves>();
-  __shared__ __attribute__((aligned(16))) char lds[kRows == kPipeRows ? kPipeLds : tile_lds<TK, TV, kKeyWaves>()];
+  __shared__ __attribute__((aligned(16))) char lds[kRows == kPipeRows ? pipe_lds<PrefixOp<TK, TV>, 2>() : tile_lds<TK, TV, kKeyWaves>()];
   if (blockIdx.x == 0) return plan_own(lds, a);
   const int block = blockIdx.x - 1, g = block % a.s.Hkv, x0 = block / a.s.Hkv, split = x0 % a.splits, x = x0 / a.splits;
   const int per = kRows / a.s.G;

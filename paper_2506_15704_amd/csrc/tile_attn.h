@@ -55,7 +55,7 @@ __device__ __forceinline__ int chunk_place(int r, int c) { return c ^ mix(r); }
 __device__ __forceinline__ int chunk_place_f32(int r, int c) { return c ^ mix_f32(r); }
 
 template <typename T>
-struct InLds { typedef bf16x8 Op; static constexpr int kRowBytes = 256; };       // bf16, and FP8 (every value is a bf16 value)
+struct InLds { typedef bf16x8 Op; static constexpr int kRowBytes = 256; };       // bf16, and FP8 (every value is a bf16 and an fp16 value)
 template <>
 struct InLds<_Float16> { typedef f16x8 Op; static constexpr int kRowBytes = 256; };
 template <>
@@ -67,10 +67,30 @@ __device__ __forceinline__ f32x16 mfma32(float a, float b, f32x16 c) { return __
 
 __device__ __forceinline__ int wave_of() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
 
+// Eight FP8 values as eight of Op (exact).
+template <typename Op>
+__device__ __forceinline__ Op fp8x8_to(uint32_t w0, uint32_t w1) {
+  Op x;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t w = i < 2 ? w0 : w1;
+    if constexpr (std::is_same<Op, bf16x8>::value) {
+      const bf16x2t y = i % 2 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.f, true) : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.f, false);
+      x[2 * i] = y[0];
+      x[2 * i + 1] = y[1];
+    } else {
+      const f16x2t y = i % 2 ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.f, true) : __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.f, false);
+      x[2 * i] = y[0];
+      x[2 * i + 1] = y[1];
+    }
+  }
+  return x;
+}
+
 // The kRows rows of a stage, of K or V, that a wave brings.  16- and 32-bit elements go from memory to LDS without registers, 1 KB an
 // instruction: lane l fills the l-th 16 bytes of it, so it asks for the chunk that belongs there.  FP8 goes through registers and
-// becomes bf16.  Rows from `end` on are the last one again: they are read by nobody's weights but 0.
-template <typename T, int kRows>
+// becomes Op's type.  Rows from `end` on are the last one again: they are read by nobody's weights but 0.
+template <typename T, int kRows, typename Op>
 struct StageFeed {
   static constexpr bool kDirect = sizeof(T) > 1;
   static constexpr int kPieces = kD * (int)sizeof(T) / 16, kRowsOfLoad = 64 / kPieces, kLoads = kRows / kRowsOfLoad;
@@ -118,9 +138,9 @@ struct StageFeed {
 #pragma unroll
       for (int i = 0; i < kLoads; ++i) {
         const int r = row(i, lane), c = lane % kPieces;
-        typedef __attribute__((address_space(3))) bf16x8* Lds;
-        *(Lds)(stage + r * 256 + 16 * chunk_place(r, 2 * c)) = fp8x8_to_bf16x8(x[i][0], x[i][1]);
-        *(Lds)(stage + r * 256 + 16 * chunk_place(r, 2 * c + 1)) = fp8x8_to_bf16x8(x[i][2], x[i][3]);
+        typedef __attribute__((address_space(3))) Op* Lds;
+        *(Lds)(stage + r * 256 + 16 * chunk_place(r, 2 * c)) = fp8x8_to<Op>(x[i][0], x[i][1]);
+        *(Lds)(stage + r * 256 + 16 * chunk_place(r, 2 * c + 1)) = fp8x8_to<Op>(x[i][2], x[i][3]);
       }
     }
   }
@@ -142,7 +162,8 @@ struct QueryTile {
   }
   // An fp32 row.  fp16 terms are taken of the row scaled by a power of two that
   // puts its largest element just below 2^14, so that any fp32 query fits and the second term keeps its bits.
-  __device__ __forceinline__ void load(const float* q, int h) {
+  // rest: what the terms leave, as one term more, chunk after chunk (each 64 lanes' 16 bytes).
+  __device__ __forceinline__ void load(const float* q, int h, lds_char* rest = nullptr) {
     float f[8][8];
     float big = 0.f;
 #pragma unroll
@@ -167,27 +188,24 @@ struct QueryTile {
       unit *= __int_as_float((127 - e) << 23);
     }
 #pragma unroll
-    for (int s = 0; s < 8; ++s)
+    for (int s = 0; s < 8; ++s) {
+      Op left;
 #pragma unroll
       for (int c = 0; c < 8; c += 2) {
         f32x2t y = {f[s][c] * up, f[s][c + 1] * up};
+        typedef typename std::conditional<std::is_same<Op, bf16x8>::value, __bf16, _Float16>::type Elem;
 #pragma unroll
-        for (int t = 0; t < kTerms; ++t) {
-          if constexpr (std::is_same<Op, bf16x8>::value) {
-            const bf16x2t z = __builtin_convertvector(y, bf16x2t);
-            x[t][s][c] = z[0];
-            x[t][s][c + 1] = z[1];
-            y[0] -= (float)z[0];
-            y[1] -= (float)z[1];
-          } else {
-            const _Float16 z0 = (_Float16)y[0], z1 = (_Float16)y[1];
-            x[t][s][c] = z0;
-            x[t][s][c + 1] = z1;
-            y[0] -= (float)z0;
-            y[1] -= (float)z1;
+        for (int t = 0; t < kTerms; ++t)
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            x[t][s][c + i] = (Elem)y[i];
+            y[i] -= (float)x[t][s][c + i];
           }
-        }
+        left[c] = (Elem)y[0];
+        left[c + 1] = (Elem)y[1];
       }
+      if (rest) *(__attribute__((address_space(3))) Op*)(rest + 1024 * s + 16 * (threadIdx.x & 63)) = left;
+    }
   }
 };
 template <int kTerms>
@@ -265,6 +283,7 @@ template <typename Op, int kTerms>
 constexpr int query_terms() { return kTerms == 1 ? 1 : (std::is_same<Op, bf16x8>::value ? 3 : 2); }
 template <typename Op, int kTerms>
 struct RowState {
+  static constexpr int kWeightTerms = query_terms<Op, kTerms>();
   typedef QueryTile<Op, query_terms<Op, kTerms>()> Query;
   static constexpr bool kF32 = std::is_same<Op, float>::value;
   static constexpr int kRowBytes = kF32 ? 512 : 256;
@@ -379,12 +398,12 @@ struct RowState {
     } else {
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
-        Op w[kTerms];
+        Op w[kWeightTerms];
 #pragma unroll
         for (int i = 0; i < 8; i += 2) {
           f32x2t y = {p[8 * t + i], p[8 * t + i + 1]};
 #pragma unroll
-          for (int u = 0; u < kTerms; ++u) {
+          for (int u = 0; u < kWeightTerms; ++u) {
             if constexpr (std::is_same<Op, bf16x8>::value) {
               const bf16x2t z = __builtin_convertvector(y, bf16x2t);
               w[u][i] = z[0];
@@ -404,7 +423,7 @@ struct RowState {
         for (int d = 0; d < 4; ++d) {
           const Op a = values(v, t, d, lane);
 #pragma unroll
-          for (int u = kTerms - 1; u >= 0; --u) o[d] = mfma32(a, w[u], o[d]);
+          for (int u = kWeightTerms - 1; u >= 0; --u) o[d] = mfma32(a, w[u], o[d]);
         }
       }
     }
@@ -443,8 +462,8 @@ __device__ __forceinline__ void tile_loop(char* lds, const CacheRows<TK>& K, con
   most = __builtin_amdgcn_readfirstlane(most);
   least = __builtin_amdgcn_readfirstlane(least);
   lds_char* const stages = (lds_char*)lds;
-  StageFeed<TK, kRows / 4> fk;
-  StageFeed<TV, kRows / 4> fv;
+  StageFeed<TK, kRows / 4, Op> fk;
+  StageFeed<TV, kRows / 4, Op> fv;
   typename decltype(fk)::Places pk;
   typename decltype(fv)::Places pv;
   constexpr bool kAlike = sizeof(TK) == sizeof(TV);

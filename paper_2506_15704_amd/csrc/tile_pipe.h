@@ -23,7 +23,7 @@ __host__ inline int rows_kind(const KvView& kv) {
 // registers, four rows an instruction: lane l fills place l % 16 of row l / 16, so it asks for the chunk that belongs there.
 // Rows from `end` on are the last one again, also whole stages of them: they are read by nobody's weights but 0.
 // aim works out where a stage's rows lie, ask asks for them: the one is scalar work for when there is time, the other a few instructions.
-template <typename T, int kKind>
+template <typename T, int kKind, typename Op>
 struct Feed {
   static constexpr bool kDirect = sizeof(T) == 2;
   static constexpr int kLoads = kFeedRows / (kDirect ? 4 : 8);     // FP8: eight rows a load, through registers
@@ -63,15 +63,15 @@ struct Feed {
         x[i] = *reinterpret_cast<const u32x4*>(p);
     }
   }
-  // FP8: what has arrived becomes bf16 in the stage
+  // FP8: what has arrived becomes Op's type in the stage
   __device__ __forceinline__ void put(lds_char* stage, int lane, int wave) const {
     if constexpr (!kDirect) {
 #pragma unroll
       for (int i = 0; i < kLoads; ++i) {
         const int r = kFeedRows * wave + row(i, lane), c = lane & 7;
-        typedef __attribute__((address_space(3))) bf16x8* Lds;
-        *(Lds)(stage + r * 256 + 16 * chunk_place(r, 2 * c)) = fp8x8_to_bf16x8(x[i][0], x[i][1]);
-        *(Lds)(stage + r * 256 + 16 * chunk_place(r, 2 * c + 1)) = fp8x8_to_bf16x8(x[i][2], x[i][3]);
+        typedef __attribute__((address_space(3))) Op* Lds;
+        *(Lds)(stage + r * 256 + 16 * chunk_place(r, 2 * c)) = fp8x8_to<Op>(x[i][0], x[i][1]);
+        *(Lds)(stage + r * 256 + 16 * chunk_place(r, 2 * c + 1)) = fp8x8_to<Op>(x[i][2], x[i][3]);
       }
     }
   }
@@ -82,10 +82,13 @@ __device__ __forceinline__ int first_row(int k0, int end, int wave) {
   return __builtin_amdgcn_readfirstlane(w0 < end ? w0 : (end - 1) & ~(kFeedRows - 1));
 }
 
-// 32 query rows of a wave.  kTerms: 16-bit terms of the query and of the weights (see RowState; here two of bf16 queries too: the third
-// one's registers are not to be had).
+// 32 query rows of a wave.  kTerms: 16-bit terms of the query and of the weights (see RowState).  The third one of a query in bf16 terms
+// is in LDS (kRest), for want of registers: its products come last of a chunk's.  Two terms of the weights leave 2^-18 of each, which
+// is 1e-6 of the output, as much as fp32 sums of a few thousand products have; a third costs an eighth of the time (64 requests over
+// 32768 shared rows).
 template <typename Op, int kTerms = 1>
 struct PipeState {
+  static constexpr bool kRest = query_terms<Op, kTerms>() > kTerms;
   static constexpr float kLift = std::is_same<Op, f16x8>::value ? 8.f : 0.f;       // (as there; times 2^kLazy it still is an fp16 number)
   f32x16 o[4];
   float m, l[4];                             // four sums, so that none waits for the one before
@@ -108,13 +111,22 @@ struct PipeState {
     for (int i = 0; i < 4; ++i)
       a[i] = *(const __attribute__((address_space(3))) Op*)(k + (32 * (i & 1) + n) * 256 + 16 * chunk_place(n, 2 * (2 * g + (i >> 1)) + h));
   }
-  __device__ __forceinline__ void add_scores(f32x16 (&s)[2], const Op (&a)[4], int g) const {
+  __device__ __forceinline__ void add_scores(f32x16 (&s)[2], const Op (&a)[4], int g, const lds_char* rest) const {
+    Op x[2];
+    if constexpr (kRest) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) x[i] = *(const __attribute__((address_space(3))) Op*)(rest + 1024 * (2 * g + i) + 16 * (threadIdx.x & 63));
+    }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int c = 2 * g + (i >> 1);
 #pragma unroll
       for (int t = kTerms - 1; t >= 0; --t)
         s[i & 1] = mfma32(a[i], q.x[t][c], c == 0 && t == kTerms - 1 ? zeros16() : s[i & 1]);
+    }
+    if constexpr (kRest) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s[i & 1] = mfma32(a[i], x[i >> 1], s[i & 1]);
     }
   }
   // Operands of the values' products of 16 keys, step t.
@@ -139,19 +151,21 @@ struct PipeState {
 #pragma unroll
       for (int d = 0; d < 4; ++d) o[d] = mfma32(a[d], w, o[d]);
     } else {
-      Op x[2];
+      Op x[kTerms];
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         typedef typename std::conditional<std::is_same<Op, bf16x8>::value, __bf16, _Float16>::type Elem;
-        const float p = s[t / 2][8 * (t % 2) + i];
-        x[0][i] = (Elem)p;
-        x[1][i] = (Elem)(p - (float)x[0][i]);
+        float p = s[t / 2][8 * (t % 2) + i];
+#pragma unroll
+        for (int u = 0; u < kTerms; ++u) {
+          x[u][i] = (Elem)p;
+          p -= (float)x[u][i];
+        }
       }
 #pragma unroll
-      for (int d = 0; d < 4; ++d) {
-        o[d] = mfma32(a[d], x[1], o[d]);
-        o[d] = mfma32(a[d], x[0], o[d]);
-      }
+      for (int u = kTerms - 1; u >= 0; --u)
+#pragma unroll
+        for (int d = 0; d < 4; ++d) o[d] = mfma32(a[d], x[u], o[d]);
     }
   }
 
@@ -260,6 +274,9 @@ struct PipeState {
 // A matrix half is eight groups of four products; the operands of the group after the next are read before a group's products,
 // those of the first two before the barrier.
 constexpr int kPipeStage = kPipeKeys * 256, kPipeStages = 3, kPipeLds = 2 * kPipeStages * kPipeStage + 16;
+constexpr int kRestAt = 2 * kPipeStages * kPipeStage, kRestWave = 8 * 1024;       // third terms of the query rows, instead of those 16 bytes
+template <typename Op, int kTerms>
+constexpr int pipe_lds() { return PipeState<Op, kTerms>::kRest ? kRestAt + kPipeWaves * kRestWave : kPipeLds; }
 // least: keys that all rows of the workgroup see.
 // active: the wave has rows of its own; one that has none only brings its share of the cache's.
 template <int kKind, typename TK, typename TV, typename Op, int kTerms>
@@ -268,14 +285,16 @@ __device__ __forceinline__ void pipe_loop(char* lds_, const CacheRows<TK>& K, co
   lds_char* const lds = (lds_char*)lds_;
   const int lane = threadIdx.x & 63, wave = wave_of(), n = lane & 31, h = lane >> 5;
   const bool late = wave >= kPipeWaves / 2;
-  Feed<TK, kKind> fk;
-  Feed<TV, kKind> fv;
+  Feed<TK, kKind, Op> fk;
+  Feed<TV, kKind, Op> fv;
   constexpr int kV = kPipeStages * kPipeStage;
   auto row_of = [&](int k) { return first_row(k, end, wave); };
   auto look_up = [&](int k) { return kKind == kPages ? RowMap<true>::block(K.pg, K.b, row_of(k)) : 0; };
   auto uniform = [](int e) { return __builtin_amdgcn_readfirstlane(e); };
+  constexpr bool kRest = PipeState<Op, kTerms>::kRest;
+  const lds_char* const rest = lds + kRestAt + wave * kRestWave;
   int* const found = (int*)(lds_ + 2 * kPipeStages * kPipeStage) + (late ? 1 : 0);      // stage (its end) with a value that is not finite
-  if ((threadIdx.x & (64 * kPipeWaves / 2 - 1)) == 0) *found = 0;
+  if (!kRest && (threadIdx.x & (64 * kPipeWaves / 2 - 1)) == 0) *found = 0;
   auto landed = [] { __builtin_amdgcn_s_waitcnt(0x0f70); };     // vmcnt(0): what I asked for is in LDS
   int e_v = look_up(first + 2 * kPipeKeys), e_k = look_up(first + 3 * kPipeKeys), e_new = 0;      // of the next to be asked for
   const int e_first[3] = {look_up(first), look_up(first + kPipeKeys), e_v};
@@ -299,7 +318,7 @@ __device__ __forceinline__ void pipe_loop(char* lds_, const CacheRows<TK>& K, co
 #pragma unroll
   for (int g = 0; g < 4; ++g) {
     st.load_keys(a[0], lds, g, n, h);
-    st.add_scores(s, a[0], g);
+    st.add_scores(s, a[0], g, rest);
   }
   __syncthreads();                            // (K of the first stage has been read)
   if (late) __syncthreads();
@@ -325,7 +344,10 @@ __device__ __forceinline__ void pipe_loop(char* lds_, const CacheRows<TK>& K, co
     landed();
     const lds_char* const v = lds + kV + now;
     const lds_char* const k = lds + next;                        // (of the last stage: what lies there, unused)
-    if (kMasked) {                                               // values that a row must not meet?  Four waves share the rows out
+    bool apart = false;
+    if (kMasked && kRest) {                                      // values that a row must not meet?
+      apart = any_not_finite<Op>(v, kPipeStage);
+    } else if (kMasked) {                                        // four waves share the rows out
       constexpr int kShare = kPipeStage / (kPipeWaves / 2);
       if (any_not_finite<Op>(v + (wave % (kPipeWaves / 2)) * kShare, kShare)) *found = k0 + kPipeKeys;
     }
@@ -336,7 +358,7 @@ __device__ __forceinline__ void pipe_loop(char* lds_, const CacheRows<TK>& K, co
     __syncthreads();
     // matrix half
     if constexpr (kWorks) {
-      const bool apart = kMasked && *(volatile int*)found == k0 + kPipeKeys;
+      if (kMasked && !kRest) apart = *(volatile int*)found == k0 + kPipeKeys;
       if (apart) st.add_values_apart(w, s, v, lane, st.limit - k0);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
@@ -346,7 +368,7 @@ __device__ __forceinline__ void pipe_loop(char* lds_, const CacheRows<TK>& K, co
         else if (to < 8) st.load_keys(a[to % kOperands], k, to - 4, n, h);
         if (i < 4) {
           if (!apart) st.add_values(a[i % kOperands], w[i], s, i);
-        } else st.add_scores(s, a[i % kOperands], i - 4);
+        } else st.add_scores(s, a[i % kOperands], i - 4, rest);
         if (i == 2) e_new = look_up(k0 + 4 * kPipeKeys);
         if (i == 3) fk.ask(lds + now, wave);
         if (i == 4) fv.ask(lds + kV + last, wave);
