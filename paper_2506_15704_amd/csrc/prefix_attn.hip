@@ -86,7 +86,7 @@ __device__ __forceinline__ void prefix_pipe(char* lds, const PrefixArgs& a, int 
 __device__ __forceinline__ int own_item_rows(int64_t total, int most, int wanted) {
   int64_t per = (total + wanted - 1) / wanted;
   const int64_t of_longest = (most + kMaxSplits - 1) / kMaxSplits;
-  per = per > of_longest ? per : of_longest;
+  per = per > of_longest ? (per < most ? per : most) : of_longest;
   return per <= kOwnLeast ? kOwnLeast : (int)((per + 15) & ~(int64_t)15);
 }
 __device__ __forceinline__ void plan_own(char* lds, const PrefixArgs& a) {

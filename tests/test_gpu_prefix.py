@@ -139,3 +139,64 @@ def test_prefix_values_that_are_not_finite_stay_out_of_requests_that_end_before_
             err = (out[b, h].double() - ref[0]).abs()[~broken]
             assert bool((err <= _tolerance(dtype, ref, weighted, dots, n)[0][~broken]).all())
     c.ctx.close()
+
+
+@pytest.mark.parametrize("Hq,Hkv", [(1, 1), (4, 1)])
+def test_prefix_many_requests_of_unlike_lengths_in_groups_of_unlike_sizes(Hq, Hkv):
+    """More requests than a workgroup has threads; own rows from none to thousands, so that some requests are one item and one is many."""
+    lens = [20 + i * 7 % 50 for i in range(600)]
+    lens[300], lens[599] = 3000, 1
+    starts = [0, 1, 65, 67, 299, 400, 400, 599]                # (a group without members; the last request is in none)
+    c = CacheCase("bf16", Hq, Hkv, lens, 16, seed=9)
+    _check(c, starts, [5, 20, 64, 21, 9, 3, 33])
+    c.ctx.close()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp8kv"])
+def test_prefix_one_request_with_many_rows_of_its_own(dtype):
+    c = CacheCase(dtype, 2, 1, [20011], 64, seed=10)
+    _check(c, [0, 1], [3])
+    c.ctx.close()
+
+
+@pytest.mark.parametrize("members", [2, 12, 30])
+@pytest.mark.parametrize("scale", [1e-30, 30.0, 1e4])
+def test_prefix_fp8_queries_of_any_size(members, scale):
+    c = CacheCase("fp8kv", 4, 1, [200 + i for i in range(members)], 16, seed=11, scale=1.0 if scale < 100 else 1e-2)
+    _check(c, [0, members], [190], scale=scale)
+    c.ctx.close()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp8k", "fp8v"])
+def test_prefix_large_groups_hold_a_query_whole(dtype):
+    """70 members x 1 head: the 256-row form, with values of unlike size in one query: 2^-18 of each element is too much here (the
+    bound has 2^-20 of the absolute sum for the query, which three bf16 terms keep)."""
+    c = CacheCase(dtype, 2, 2, [520] * 70, 16, seed=12)
+    q = c.randn(c.B, c.Hq, D) * torch.exp2(torch.randint(-6, 3, (c.B, c.Hq, D), device=DEV, generator=c.gen).float())
+    out = torch.full((c.B, c.Hq, D), 7.0, device=DEV)
+    c.ctx.lfps_prefix_attn_decode(q, c.kv, ints([0, c.B]), ints([520]), out)
+    for b in range(0, c.B, 7):
+        for h in range(c.Hq):
+            k, v = c.values(c.K, 0, 0, 520)[h // c.G], c.values(c.V, 0, 0, 520)[h // c.G]
+            ref, weighted, dots = attend64(q[b, h:h + 1].double(), k, v)
+            # the query's terms 2^-24 of each element at most and fp32 products (260 of 2^-24), twice; two terms of a weight 2^-18; sums over 520 keys
+            bound = (2 * 262 * 2.0 ** -24 * dots + 2 * 2.0 ** -18 + 2.0 ** -21 + 600 * 2.0 ** -24) * weighted + 1e-7
+            assert bool(((out[b, h].double() - ref[0]).abs() <= bound[0]).all()), (b, h)
+    c.ctx.close()
+
+
+@pytest.mark.parametrize("members", [1, 9, 20])
+def test_prefix_every_fp8_value_is_itself(members):
+    """One row: its weight is 1, whatever its score, and the output its values (2 rows: all 256 codes, NaN among them)."""
+    c = CacheCase("fp8kv", 4, 1, [1] * members, 16, seed=13)
+    for codes in (torch.arange(128), torch.arange(128, 256)):
+        x = codes.to(torch.uint8).to(DEV).view(torch.float8_e4m3fn)
+        c.put(c.V, 0, 0, x.view(1, 1, D))
+        out = torch.zeros((members, 4, D), device=DEV)
+        c.ctx.lfps_prefix_attn_decode(c.randn(members, 4, D), c.kv, ints([0, members]), ints([1]), out)
+        # The one weight is a power of two only up to the rounding of score - maximum + a constant: as two fp16 terms it is 2^-22 off at
+        # most, its sum is not; product, join, sum and division round by 2^-24 each, ten times at most.
+        want = x.float()
+        assert torch.equal(out.isnan(), want.isnan().expand_as(out))
+        assert bool((out - want).abs().nan_to_num(0).le((2.0 ** -22 + 10 * 2.0 ** -24) * want.abs().nan_to_num(0)).all())
+    c.ctx.close()

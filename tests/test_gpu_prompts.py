@@ -263,3 +263,17 @@ def test_prompt_values_that_are_not_finite_reach_only_the_tokens_that_see_them(d
                 ref = torch.where(V[:end].isfinite().all(0), ref, V[:end].masked_fill(V[:end].isfinite(), 0).sum(0))
                 _same_where_not_finite(out[at[b] + i, h].double(), ref, _tolerance(dtype, ref.nan_to_num(0, 0, 0), weighted, dots, n))
     c.ctx.close()
+
+
+@pytest.mark.parametrize("tokens", [1, 300])
+def test_prompt_every_fp8_value_is_itself(tokens):
+    """Rows that all are the same: the output is that row's values, which bf16 holds (a few tokens; many, which take the other kernel)."""
+    c = CacheCase("fp8kv", 2, 1, [tokens], 16, seed=21)
+    for codes in (torch.arange(127), torch.arange(128, 255)):
+        x = torch.cat([codes, codes[-1:]]).to(torch.uint8).to(DEV).view(torch.float8_e4m3fn)
+        c.put(c.V, 0, 0, raw(x.view(1, 1, D)).expand(tokens, 1, D).contiguous().view(torch.float8_e4m3fn))
+        out = torch.zeros((tokens, 2, D), dtype=torch.bfloat16, device=DEV)
+        c.ctx.lfps_prompt_attn(c.randn(tokens, 2, D).to(torch.bfloat16), ints([0, tokens]), c.kv, out)
+        # sums of equal values, divided by the weights' own sum: fp32 rounding, then bf16's; the values have 4 bits
+        assert bool((out.float() - x.float()).abs().le(2.0 ** -8 * x.float().abs()).all())
+    c.ctx.close()
