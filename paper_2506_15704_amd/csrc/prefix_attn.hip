@@ -210,9 +210,13 @@ template <typename TK, typename TV>
 hipError_t prefix_t(PrefixArgs a, int dtype, float* out, int64_t part_rows, hipStream_t st) {
   const Shape& s = a.s;
   const int64_t heads = (int64_t)s.B * s.Hq;
-  // The rows of a group of ordinary size decide how many a workgroup takes: more share a row of the cache, fewer leave no wave idle.
+  // The rows of a group of ordinary size decide how many a workgroup takes.  16-bit operands: up to 64 rows, tiles of 32 with a wave a
+  // quarter of the keys; more, 256 rows with the pipelined loop.  Over 8192 rows of 8 KV heads, us of the whole call with either: bf16
+  // groups of 32 rows 27.3 / 30.5, 48 32.8 / 31.8, 64 30.4 / 32.4, 80 51.0 / 33.9, 128 39.5 / 37.9; FP8 26.1 / 29.5, 31.4 / 30.6, 29.1 / 32.5,
+  // 48.6 / 34.1, 38.0 / 38.7.  (Tiles of 64 rows with half the keys a wave: 30.3, 35.1, 32.8, 45.1, 40.3 in bf16, never the best.)
+  // fp32: tiles of 64 rows, of 128 where a group fills them.
   const int size = (s.B + a.groups.n - 1) / a.groups.n, rows = size * s.G;
-  const int key_waves = rows > 64 ? 1 : (rows > 32 || sizeof(TK) == 4 ? 2 : 4);
+  const int key_waves = rows > 64 ? 1 : (sizeof(TK) == 4 ? 2 : 4);
   const int per = key_waves == 1 ? shared_rows<TK, 1>() : 32 * (4 / key_waves);
   const int tiles = s.B / (per / s.G) + a.groups.n;          // room for any groups; of groups of one size there are `usual`
   const int64_t usual = (int64_t)a.groups.n * ((size * s.G + per - 1) / per);
@@ -230,9 +234,9 @@ hipError_t prefix_t(PrefixArgs a, int dtype, float* out, int64_t part_rows, hipS
 #define LFPS_SHARED(KW, KIND) \
   hipLaunchKernelGGL((k_prefix_shared<TK, TV, KW, KIND>), dim3(grid), dim3(per == kPipeRows ? kPipeThreads : kTileThreads), 0, st, a)
   const int kind = sizeof(TK) == 4 ? kAnyRows : rows_kind(a.kv);
-  if (key_waves == 2) LFPS_SHARED(2, kAnyRows);
-  else if (key_waves == 1 && kind == kAnyRows) LFPS_SHARED(1, kAnyRows);
-  else if constexpr (sizeof(TK) != 4) {
+  if (key_waves == 1 && kind == kAnyRows) LFPS_SHARED(1, kAnyRows);
+  else if constexpr (sizeof(TK) == 4) LFPS_SHARED(2, kAnyRows);
+  else {
     if (key_waves == 4) LFPS_SHARED(4, kAnyRows);
     else if (kind == kSlab) LFPS_SHARED(1, kSlab);
     else LFPS_SHARED(1, kPages);

@@ -204,7 +204,13 @@ hipError_t prompt_t(const Shape& s, const KvView& kv, const void* q, int64_t q_s
     if (n > kMaxSplits) n = kMaxSplits;
     return (int)(n < 1 ? 1 : n);
   };
-  const bool all_few = (int64_t)n_tokens * s.G <= kMost, none_few = !all_few && s.B == 1;
+  // k_prompt_few makes 32 rows of work for a request of one token where k_prompt_tiles makes 256, but of 16-bit operands the latter's
+  // loop asks for rows earlier and hides a stage's parts behind each other: it is the quicker one until the requests fill the chip by
+  // themselves.  us, few / tiles: one token over 4100 rows of 8 KV heads 15.5 / 13.3, over 32768 38.1 / 33.1; 16 requests of 4 tokens
+  // over 4100 rows 64.8 / 54.4 (FP8 65.0 / 49.9), of one over 8192 109 / 120 (111 / 87); 64 of one over 2048 112 / 123 (112 / 91), of
+  // seven 113 / 171 (112 / 136).  fp32: 32 / 50, 135 / 239, 270 / 464, 514 / 900.
+  const bool small = sizeof(TK) != 4 && s.B * s.Hkv <= 128;
+  const bool all_few = !small && (int64_t)n_tokens * s.G <= kMost, none_few = small || (!all_few && s.B == 1);
   const int tiles = n_tokens / per + s.B;
   if (!all_few) a.splits = parts((int64_t)tiles * s.Hkv, (int64_t)n_tokens * s.Hq, part_rows);
   if (a.splits > 1) a.few_part = (int64_t)n_tokens * s.Hq * a.splits;
