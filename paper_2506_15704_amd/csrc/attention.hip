@@ -192,6 +192,7 @@ __global__ __launch_bounds__(kAttnThreads) void k_full_attn(Shape s, const float
                                                             int64_t stride_b, int64_t stride_h, int64_t stride_n,
                                                             KvPage pg, const int32_t* __restrict__ seq_lens,
                                                             float* __restrict__ part, int n_split, float scale, Own... own) {
+  // (items are short, and more of their workgroups fit with the half of rows in flight: 32 requests in FP8 75.9 -> 72.5 us, bf16 the same)
   constexpr int U = sizeof...(Own) || sizeof(TK) == 4 ? 4 : 8, kRows = 4 * U;
   constexpr int kShare = 16 / G;                            // lanes of a row that hold the same head's sum
   constexpr int NV = U > kShare ? U / kShare : 1;           // (row, head) pairs of a lane

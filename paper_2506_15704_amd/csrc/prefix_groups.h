@@ -44,6 +44,9 @@ __device__ __forceinline__ void group_at(const Shape& s, const int32_t* seq_lens
 
 // The rows that the requests have for themselves, cut into items of no more than some number of rows, the same for all: what their lengths
 // ask for, so that a long request is cut into many and a short one into one.  Made by plan_own, once a call, on the device.
+// (With the same number of parts for each request, most workgroups of a batch of unlike lengths found nothing to do, and the chip holds
+// 768 of them at a time: 64 requests of 1 to 900 rows 35 -> 29 us, 32 of 100 to 2000 in FP8 33 -> 27.  64, 128 and 256 rows at least: 77.5, 78.3
+// and 83.2 us of the whole FP8 call.)
 struct OwnItem { int32_t b, begin, end, unused; };
 struct OwnRows {
   int32_t* first;            // [B] a request's first row of its own; below 0: it is in no group

@@ -2,10 +2,16 @@
 // few drafted tokens, single ones.  Tokens of all requests are packed; token i of the t_b of request b sits at row n_b - t_b + i
 // and sees the rows up to its own.
 //
-// Two kernels, both the body of tile_attn.h.  k_prompt_tiles: a workgroup has 128 query rows of one (request, KV head), 32 a wave,
-// and streams the rows they see; bound by the matrix units.  k_prompt_few: a request whose tokens fill no more than one wave's
-// rows; the four waves share the keys, and the rows are cut into parts that are joined afterwards; bound by the bytes of K and V.
-// Which one takes a request is decided on the device by its number of tokens, so one call takes any mixture.
+// Two kernels.  k_prompt_tiles: a workgroup has 256 query rows of one (request, KV head) with the loop of tile_pipe.h, 128 over fp32
+// caches with that of tile_attn.h, and streams the rows they see; bound by the matrix units.  k_prompt_few: requests whose tokens fill no
+// more than one wave's rows (fp32: two), where there are many of them; the waves share the keys; bound by the bytes of K and V.
+// Where the rows alone do not fill the chip, those that they see are cut into parts that k_prompt_merge joins.
+// Which kernel takes a request is decided on the device by its number of tokens, so one call takes any mixture.
+//
+// 32 heads over 8 KV heads: 16384 tokens in bf16 1.90 ms, 1160 TFLOP/s of the 1370 that the largest products of the BLAS library reach
+// here; 8192 behind 24576 rows of FP8 pages 3.34 ms, 1150; eight prompts of 61 to 4096 tokens over 16 heads in fp16 207 us, 794; two of
+// 944 and 1307 in fp32 276 us, 77 of 155 TFLOP/s; five tokens over 4104 rows 13.4 us in two launches.  What each step gave is beside
+// the loops.
 #include "tile_pipe.h"
 
 namespace lfps {

@@ -1,5 +1,10 @@
 // The prompt kernel's body for 16-bit operands (bf16, fp16, FP8 converted to bf16): tile_attn.h's products, made for the matrix
 // units' rate.
+//
+// Steps, over 16384 tokens of 32 heads in bf16: rows through registers, 128 query rows a workgroup, 5.09 ms; straight into LDS, a maximum that
+// is followed lazily 2.17; 256 query rows, places without bank conflicts, scores of the next stage beside the weights of this one
+// 1.94; the two waves of a SIMD half a stage apart, requests between the products 1.89.  A stage of 64 keys takes 3100 to 3250 cycles of
+// which 2048 are the matrix unit's; the clock falls to 1.75 to 2.0 GHz meanwhile, and cards differ by 3% in it.
 #pragma once
 #include "tile_attn.h"
 
