@@ -276,9 +276,9 @@ __device__ __forceinline__ f32x16 zeros16() {
 }
 
 // ---- the state of a wave's 32 rows ----------------------------------------------------------------------------
-// kTerms: 16-bit terms of the weights (1: rounded to 16 bits, as the output will be; 2: fp32 results).  An fp32 query is the sum of
-// query_terms of them: three of bf16, which hold it whole (two leave 2^-18 of every element, and the error of a score grows with it:
-// 3e-6 of the output instead of 1e-6 where a few rows carry most of the weight), two of fp16 (2^-22 is left).
+// kTerms: 1: the query is 16-bit and the weights are rounded to 16 bits, as the output will be; 2: fp32 query and results.  An fp32
+// query, and an fp32 weight, is then the sum of query_terms 16-bit ones: three of bf16, which hold it whole, two of fp16 (2^-22 is left).
+// Two of bf16 leave 2^-18 of each: 1.2 to 1.5e-6 from 64 bits with a few hundred rows, where these are 0.5e-6.
 template <typename Op, int kTerms>
 constexpr int query_terms() { return kTerms == 1 ? 1 : (std::is_same<Op, bf16x8>::value ? 3 : 2); }
 template <typename Op, int kTerms>
