@@ -636,14 +636,15 @@ __device__ __forceinline__ f32x2t join_parts(int n, At at, Score score, Sum sum)
   for (int j = 0; j < 2; ++j) {
     const int i = lane + 64 * j < n ? lane + 64 * j : n - 1;
     m[j] = lane + 64 * j < n ? score(i) : -INFINITY;
-    f[j] = sum(i);
+    f[j] = lane + 64 * j < n ? sum(i) : 0.f;
   }
   float mx = fmaxf(m[0], m[1]);
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) mx = fmaxf(mx, __shfl_xor(mx, d));
 #pragma unroll
   for (int j = 0; j < 2; ++j) {
-    const float w = m[j] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[j] - mx);
+    // (no score: nothing was seen, or all that was is NaN, and then so is the sum)
+    const float w = m[j] == -INFINITY ? (f[j] == 0.f ? 0.f : NAN) : __builtin_amdgcn_exp2f(m[j] - mx);
     l += w > 0.f || w != w ? w * f[j] : 0.f;
     f[j] = w;
   }

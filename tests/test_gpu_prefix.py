@@ -200,3 +200,20 @@ def test_prefix_every_fp8_value_is_itself(members):
         assert torch.equal(out.isnan(), want.isnan().expand_as(out))
         assert bool((out - want).abs().nan_to_num(0).le((2.0 ** -22 + 10 * 2.0 ** -24) * want.abs().nan_to_num(0)).all())
     c.ctx.close()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32", "fp8kv"])
+@pytest.mark.parametrize("members,prefix", [(3, 2000), (12, 40), (40, 700)])
+def test_prefix_a_query_of_nan_is_nan_and_its_own_only(dtype, members, prefix):
+    c = CacheCase(dtype, 4, 1, [prefix + i % 3 for i in range(members)], 16, seed=14)
+    q = c.randn(members, 4, D)
+    outs = []
+    for spoilt in (False, True):
+        if spoilt:
+            q[1, 2] = float("nan")
+        outs.append(torch.zeros((members, 4, D), device=DEV))
+        c.ctx.lfps_prefix_attn_decode(q, c.kv, ints([0, members]), ints([prefix]), outs[-1])
+    assert bool(outs[1][1, 2].isnan().all())
+    outs[0][1, 2] = outs[1][1, 2] = 0
+    assert torch.equal(*outs)
+    c.ctx.close()

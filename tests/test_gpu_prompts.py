@@ -277,3 +277,22 @@ def test_prompt_every_fp8_value_is_itself(tokens):
         # sums of equal values, divided by the weights' own sum: fp32 rounding, then bf16's; the values have 4 bits
         assert bool((out.float() - x.float()).abs().le(2.0 ** -8 * x.float().abs()).all())
     c.ctx.close()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32", "fp8kv"])
+@pytest.mark.parametrize("Hkv,news,lens", [(1, [5], [4000]), (1, [300], [300]), (8, [3] * 20, [90] * 20)])
+def test_prompt_a_query_of_nan_is_nan_and_its_own_only(dtype, Hkv, news, lens):
+    """In parts, in one, and many requests of few tokens."""
+    c = CacheCase(dtype, 4 * Hkv, Hkv, lens, 16, seed=22)
+    at = packed(news)
+    q = c.randn(at[-1], 4 * Hkv, D).to(c.q_dtype)
+    outs = []
+    for spoilt in (False, True):
+        if spoilt:
+            q[2, 3] = float("nan")
+        outs.append(torch.zeros_like(q))
+        c.ctx.lfps_prompt_attn(q, ints(at), c.kv, outs[-1])
+    assert bool(outs[1][2, 3].isnan().all())
+    outs[0][2, 3] = outs[1][2, 3] = 0
+    assert torch.equal(*outs)
+    c.ctx.close()
