@@ -296,3 +296,13 @@ def test_prompt_a_query_of_nan_is_nan_and_its_own_only(dtype, Hkv, news, lens):
     outs[0][2, 3] = outs[1][2, 3] = 0
     assert torch.equal(*outs)
     c.ctx.close()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp8kv", "f32"])
+def test_prompt_single_tokens_over_many_rows_beside_a_prompt(dtype):
+    """Both kernels in one call, the few tokens in parts."""
+    news = [900, 1, 7, 2]
+    c = CacheCase(dtype, 4, 1, [900, 5000, 4001, 17], 16, seed=23)
+    at, q, out = _prompt(c, news)
+    _check_prompt(c, news, at, q, out)
+    c.ctx.close()
