@@ -322,9 +322,10 @@ int lfps_pages_workspace_bytes(int32_t n_blocks, int64_t* out);
  * It keeps the parent's blocks as far as it has rows of them.  New blocks are the lowest ones that are not live before the call,
  * dealt to the requests in order, to each first the copy of its last block, then those of its growth.  That copy is made where it
  * will write behind the parent's rows in a block of which others keep rows, or which is held; where all who keep it
- * write into it, the first of them keeps the block itself.  Copy before anything is appended.
- * If the blocks do not suffice, a request gets what is left: lens_out says how many rows it has room for (never fewer than it kept)
- * and LFPS_FLAG_PAGES_FULL is raised.  Blocks that this call frees can be had from the next one on. */
+ * write into it, the one with the most rows in it (of those, the first) keeps the block itself.  Copy before anything is appended.
+ * If the blocks do not suffice, a request gets what is left: lens_out says how many rows it has room for (never fewer than it kept,
+ * and nobody's growth reaches rows that another kept) and LFPS_FLAG_PAGES_FULL is raised.  Append no more tokens than it grew by: they
+ * are the newest rows of lens_out.  Blocks that this call frees can be had from the next one on. */
 int lfps_pages_update(lfps_ctx* ctx, const lfps_kv* kv, const int32_t* parent, const int32_t* new_lens,
                       const int32_t* held, int32_t* table_out, int32_t* lens_out, int32_t* copies, void* work,
                       int64_t work_bytes, void* stream);

@@ -4,7 +4,8 @@
 // An update makes the next table from the last one: request b continues request parent[b] (itself, another: a fork, none: it
 // ends) with new_lens[b] rows.  Blocks are only taken from those that nobody used before the call, in rising order, so
 // what a copy reads is never what another copy writes.  A half-filled block that a request will write into and others keep is
-// copied for it; of several that all write into it the first keeps it.
+// copied for it; of several that all write into it the one with the most rows there (of those, the first) keeps it: whatever it appends
+// lies behind the others' rows, also of those for whose copy no block is left and who stay in this one.
 // A compaction moves the live blocks behind the front into the holes of the front, both in rising order.
 //
 // All of it is whole numbers, and none depends on the order of atomics.  A few dependent launches over 4 bytes an entry of the
@@ -31,7 +32,7 @@ struct PagesArgs {
   uint8_t* live;                           // [n_blocks] used by the table, or held
   int32_t* writers;                        // [n_blocks] requests that will write into this half-filled block
   int32_t* holders;                        // [n_blocks] entries of the new table with it, where there are writers
-  int32_t* first;                          // [n_blocks] B minus the first writer
+  uint32_t* keeper;                        // [n_blocks] the largest writer_rank of them
   int32_t* list;                           // [n_blocks] free blocks; compaction: holes, from n_blocks / 2 on movers
   int32_t* chunk;                          // [n_chunks] free (compaction: live) blocks of every chunk
 };
@@ -52,6 +53,8 @@ struct Next {
   int kept, wanted;                        // the same in blocks
   int tail;                                // the half-filled block that it will write into, or -1
 };
+// Rows of its last kept block, 0 where that is full.
+__device__ __forceinline__ int rows_in_tail(const PagesArgs& a, const Next& x) { return x.rows & ((1 << a.pg.shift) - 1); }
 __device__ __forceinline__ Next next_of(const PagesArgs& a, int b) {
   Next x;
   x.parent = a.parent ? a.parent[b] : b;
@@ -62,12 +65,14 @@ __device__ __forceinline__ Next next_of(const PagesArgs& a, int b) {
   x.rows = n < x.length ? n : x.length;
   x.kept = blocks_of(a, x.rows);
   x.wanted = blocks_of(a, x.length);
-  x.tail = x.length > x.rows && (x.rows & ((1 << a.pg.shift) - 1)) ? entry_of(a, x.parent, x.kept - 1) : -1;
+  x.tail = x.length > x.rows && rows_in_tail(a, x) ? entry_of(a, x.parent, x.kept - 1) : -1;
   return x;
 }
+// Who of a block's writers comes first: who has more rows in it, then the lower number (either below 2^16).
+__device__ __forceinline__ uint32_t writer_rank(const PagesArgs& a, int b, const Next& x) { return (uint32_t)rows_in_tail(a, x) << 16 | (uint32_t)(a.s.B - b); }
 // Does it get a copy of that block?  (After the counting.)
 __device__ __forceinline__ bool copies(const PagesArgs& a, int b, const Next& x) {
-  return x.tail >= 0 && (is_held(a, x.tail) || a.holders[x.tail] > a.writers[x.tail] || a.first[x.tail] != a.s.B - b);
+  return x.tail >= 0 && (is_held(a, x.tail) || a.holders[x.tail] > a.writers[x.tail] || a.keeper[x.tail] != writer_rank(a, b, x));
 }
 
 // Sum over the workgroup, in every thread.
@@ -126,7 +131,7 @@ __global__ __launch_bounds__(kPageThreads) void k_pages_mark(PagesArgs a) {
     const Next x = next_of(a, b);
     if (x.tail >= 0) {
       atomicAdd(a.writers + x.tail, 1);
-      atomicMax(a.first + x.tail, a.s.B - b);
+      atomicMax(a.keeper + x.tail, writer_rank(a, b, x));
     }
   }
 }
@@ -195,7 +200,7 @@ __global__ __launch_bounds__(kPageThreads) void k_pages_write(PagesArgs a, int32
     lens_out[b] = length;
     copies_out[3 * b] = copied ? x.tail : -1;
     copies_out[3 * b + 1] = copied ? mine[0] : -1;
-    copies_out[3 * b + 2] = copied ? x.rows & ((1 << a.pg.shift) - 1) : 0;
+    copies_out[3 * b + 2] = copied ? rows_in_tail(a, x) : 0;
   }
 }
 
@@ -310,7 +315,7 @@ PagesArgs pages_args(const Shape& s, const KvView& kv, const int32_t* held, void
   p += align16(4 * n);
   a.holders = (int32_t*)p;
   p += align16(4 * n);
-  a.first = (int32_t*)p;
+  a.keeper = (uint32_t*)p;
   p += align16(4 * n);
   a.list = (int32_t*)p;
   p += align16(4 * n);
