@@ -50,7 +50,8 @@ __global__ __launch_bounds__(256) void k_append(Shape s, KvView kv, const TS* __
   if (token >= n_tokens) return;
   const int t = (int)token;
   while (b + 1 < s.B && cu[b + 1] <= t) ++b;
-  const int c0 = cu[b], c1 = cu[b + 1];
+  int c0, c1;
+  request_tokens(cu, n_tokens, b, &c0, &c1);
   if (t < c0 || t >= c1) return;
   int n = kv.seq_lens[b];
   n = n < 0 ? 0 : (n > s.Lcap ? s.Lcap : n);

@@ -1,4 +1,5 @@
-// Groups of requests that share their first rows (lfps_prefix_attn_decode), as the kernels read them.
+// Packed tokens of requests (lfps_append, lfps_prompt_attn) and groups of requests that share their first rows (lfps_prefix_attn_decode),
+// as the kernels read them.
 #pragma once
 #include "lfps_internal.h"
 
@@ -13,6 +14,13 @@ struct PrefixGroups {
 __device__ __forceinline__ int length_of(const Shape& s, const int32_t* seq_lens, int b) {
   const int n = seq_lens[b];
   return n < 0 ? 0 : (n > s.Lcap ? s.Lcap : n);
+}
+
+// Tokens [c0, c1) of request b of n_tokens packed ones, whatever cu holds.
+__device__ __forceinline__ void request_tokens(const int32_t* cu, int n_tokens, int b, int* c0, int* c1) {
+  const int x = cu[b], y = cu[b + 1];
+  *c0 = x < 0 ? 0 : (x > n_tokens ? n_tokens : x);
+  *c1 = y < *c0 ? *c0 : (y > n_tokens ? n_tokens : y);
 }
 
 // The last i in [0, n] with start(i) <= x, for a rising start with start(0) <= x: 64 places a round, by the whole wave.  Of a start that

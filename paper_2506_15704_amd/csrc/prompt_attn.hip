@@ -33,12 +33,9 @@ struct PromptArgs {
   int32_t few_by_token;          // and whether they lie by token, or else in room for few_tokens of every request
 };
 
-// Tokens [c0, c1) of request b, whatever cu holds.
 template <typename A>
 __device__ __forceinline__ void tokens_of(const A& a, int b, int* c0, int* c1) {
-  const int x = a.cu[b], y = a.cu[b + 1];
-  *c0 = x < 0 ? 0 : (x > a.n_tokens ? a.n_tokens : x);
-  *c1 = y < *c0 ? *c0 : (y > a.n_tokens ? a.n_tokens : y);
+  request_tokens(a.cu, a.n_tokens, b, c0, c1);
 }
 template <typename TK>
 constexpr int few_most() { return 32 * (4 / few_key_waves<TK>()); }      // query rows of a request that k_prompt_few takes
