@@ -592,7 +592,7 @@ __device__ __forceinline__ void tile_finish(char* lds, RowState<Op, kTerms>& st,
         for (int w = 0; w < kKeyWaves; ++w) {
           const f32x4 x = *reinterpret_cast<const f32x4*>(rows + w * 32 * kRow + 32 * d + 2 * r + 4 * h);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) a[i] = f[w] == 0.f ? a[i] : fmaf(x[i], f[w], a[i]);
+          for (int i = 0; i < 4; ++i) a[i] = fmaf(x[i], f[w], a[i]);
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) st.o[j][r + i] = a[i];
@@ -620,7 +620,7 @@ __device__ __forceinline__ void tile_finish(char* lds, RowState<Op, kTerms>& st,
 
 // n <= 128 parts of a row joined, by a whole wave, two channels a lane: part i is at(i), with score(i) its largest score in powers of two
 // (-inf: it holds nothing) and sum(i) the sum of its weights.  All scores come in one load, a lane a part, and the parts' rows eight at a
-// time.  (32 lanes a row that walked the parts one by one: 17.8 us for 17 parts of 160 rows.)
+// time.  What is not finite in a part shows in the row, also where the part weighs 0, as it does in rows of one part.  (32 lanes a row that walked the parts one by one: 17.8 us for 17 parts of 160 rows.)
 template <typename At, typename Score, typename Sum>
 __device__ __forceinline__ f32x2t join_parts(int n, At at, Score score, Sum sum) {
   const int lane = threadIdx.x & 63;
@@ -644,7 +644,7 @@ __device__ __forceinline__ f32x2t join_parts(int n, At at, Score score, Sum sum)
 #pragma unroll
   for (int j = 0; j < 2; ++j) {
     // (no score: nothing was seen, or all that was is NaN, and then so is the sum)
-    const float w = m[j] == -INFINITY ? (f[j] == 0.f ? 0.f : NAN) : __builtin_amdgcn_exp2f(m[j] - mx);
+    const float w = f[j] != f[j] ? NAN : (m[j] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[j] - mx));
     l += w > 0.f || w != w ? w * f[j] : 0.f;
     f[j] = w;
   }
@@ -656,10 +656,8 @@ __device__ __forceinline__ f32x2t join_parts(int n, At at, Score score, Sum sum)
       const int i = i0 + u;
       if (i < n) {
         const float w = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(i < 64 ? f[0] : f[1]), i & 63));
-        if (w != 0.f) {
-          a[0] = fmaf(x[u][0], w, a[0]);
-          a[1] = fmaf(x[u][1], w, a[1]);
-        }
+        a[0] = fmaf(x[u][0], w, a[0]);
+        a[1] = fmaf(x[u][1], w, a[1]);
       }
     }
     i0 += kU;
