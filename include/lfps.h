@@ -307,9 +307,10 @@ int lfps_prefix_attn_decode(lfps_ctx* ctx, const float* q, const lfps_kv* kv, co
 
 /* Pages.  The state of a paged cache is its block table and lengths (the view's); a block is live if the table names it for a
  * row below some n_b, or if the caller holds it for something else (held [n_blocks] int32, not 0; or NULL).  The calls below
- * read the view's table and lengths and write new ones, which must not overlap them: swap the two, as the Top-k arrays of two
- * steps.  They compute whole numbers only and plan the copies of rows as a list [.., 3] of (from block, to block, leading rows;
- * -1, -1, 0: none), which lfps_pages_copy carries out in the pool of every layer that shares the table.
+ * read the view's table and lengths and write new ones: swap the two, as the Top-k arrays of two steps.  What a call writes
+ * (its results and work) must not overlap what it reads, nor another result.  They compute whole numbers only and plan the copies
+ * of rows as a list [.., 3] of (from block, to block, leading rows; -1, -1, 0: none), which lfps_pages_copy carries out in the pool of
+ * every layer that shares the table.
  * work: lfps_pages_workspace_bytes(n_blocks) bytes of device memory, 16-byte aligned, that no other call uses meanwhile; nothing
  * in it is kept from one call to the next.  The view must be paged; n_blocks <= 2^24. */
 int lfps_pages_workspace_bytes(int32_t n_blocks, int64_t* out);

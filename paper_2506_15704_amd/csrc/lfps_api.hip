@@ -3,6 +3,7 @@
 #include <stdio.h>
 #include <string.h>
 
+#include <initializer_list>
 #include <mutex>
 #include <new>
 
@@ -962,16 +963,32 @@ int check_kv_both(lfps_ctx* ctx, const lfps_kv* kv, KvView* v) {
   if (rc != LFPS_OK) return rc;
   return kv->v ? LFPS_OK : fail(ctx, LFPS_EINVAL, "kv->v is NULL");
 }
-int check_pages(lfps_ctx* ctx, const lfps_kv* kv, const void* table_out, const void* work, int64_t work_bytes, KvView* v) {
+// The arrays of a call on pages.  A later workgroup still reads what an earlier one has answered, so what is written overlaps nothing.
+struct Span { const void* p; int64_t bytes; };             // p NULL: not there
+bool overlap(Span a, Span b) {
+  const uintptr_t x = (uintptr_t)a.p, y = (uintptr_t)b.p;
+  return a.p && b.p && x < y + (uintptr_t)b.bytes && y < x + (uintptr_t)a.bytes;
+}
+int check_pages(lfps_ctx* ctx, const lfps_kv* kv, void* work, int64_t work_bytes, std::initializer_list<Span> in, std::initializer_list<Span> out,
+                KvView* v) {
   const int rc = check_kv(ctx, kv, false, v);
   if (rc != LFPS_OK) return rc;
   if (!kv->block_table) return fail(ctx, LFPS_EINVAL, "pages: the view has no block table");
   if (kv->n_blocks > (1 << 24)) return fail(ctx, LFPS_ECAP, "pages: n_blocks exceeds 2^24");
   if ((uintptr_t)work % 16 || work_bytes < pages_workspace_bytes(kv->n_blocks))
     return fail(ctx, LFPS_EINVAL, "pages: work must be 16-byte aligned and hold lfps_pages_workspace_bytes(n_blocks)");
-  const uintptr_t bytes = (uintptr_t)ctx->shape.B * kv->block_table_stride * 4, from = (uintptr_t)kv->block_table, to = (uintptr_t)table_out;
-  if (from < to + bytes && to < from + bytes) return fail(ctx, LFPS_EINVAL, "pages: table_out overlaps the view's block table");
-  return LFPS_OK;
+  // (of the table's last row only the entries that are read: its stride may reach beyond them)
+  const int64_t B = ctx->shape.B, entries = (ctx->shape.Lcap + (int64_t)kv->block_size - 1) / kv->block_size;
+  const Span table = {kv->block_table, 4 * ((B - 1) * kv->block_table_stride + entries)}, lens = {kv->seq_lens, 4 * B};
+  const Span room = {work, pages_workspace_bytes(kv->n_blocks)};
+  bool bad = overlap(room, table) || overlap(room, lens);
+  for (const Span& x : in) bad = bad || overlap(room, x);
+  for (const Span& x : out) {
+    bad = bad || overlap(x, room) || overlap(x, table) || overlap(x, lens);
+    for (const Span& y : in) bad = bad || overlap(x, y);
+    for (const Span& y : out) bad = bad || (&x != &y && overlap(x, y));
+  }
+  return bad ? fail(ctx, LFPS_EINVAL, "pages: an array that is written overlaps another one of the call") : LFPS_OK;
 }
 }  // namespace
 
@@ -1042,9 +1059,10 @@ int lfps_pages_update(lfps_ctx* ctx, const lfps_kv* kv, const int32_t* parent, c
   if (!ctx) return LFPS_EINVAL;
   if (!new_lens || !table_out || !lens_out || !copies || !work) return fail(ctx, LFPS_EINVAL, "lfps_pages_update: NULL argument");
   KvView v;
-  const int rc = check_pages(ctx, kv, table_out, work, work_bytes, &v);
+  const int64_t B = ctx->shape.B;
+  const int rc = check_pages(ctx, kv, work, work_bytes, {{parent, 4 * B}, {new_lens, 4 * B}, {held, kv ? 4 * (int64_t)kv->n_blocks : 0}},
+                             {{table_out, kv ? 4 * B * kv->block_table_stride : 0}, {lens_out, 4 * B}, {copies, 12 * B}}, &v);
   if (rc != LFPS_OK) return rc;
-  if (lens_out == kv->seq_lens) return fail(ctx, LFPS_EINVAL, "lfps_pages_update: lens_out is the view's seq_lens");
   const OnDevice on(ctx->cfg.device);
   hipStream_t st = (hipStream_t)stream;
   LAUNCH(ctx, LFPS_KERNEL_PAGES_PLAN, st,
@@ -1057,7 +1075,9 @@ int lfps_pages_compact(lfps_ctx* ctx, const lfps_kv* kv, const int32_t* held, in
   if (!ctx) return LFPS_EINVAL;
   if (!table_out || !block_map || !n_live || !work) return fail(ctx, LFPS_EINVAL, "lfps_pages_compact: NULL argument");
   KvView v;
-  const int rc = check_pages(ctx, kv, table_out, work, work_bytes, &v);
+  const int64_t n = kv ? kv->n_blocks : 0;
+  const int rc = check_pages(ctx, kv, work, work_bytes, {{held, 4 * n}},
+                             {{table_out, kv ? 4 * (int64_t)ctx->shape.B * kv->block_table_stride : 0}, {moves, 12 * (n / 2)}, {block_map, 4 * n}, {n_live, 4}}, &v);
   if (rc != LFPS_OK) return rc;
   if (!moves && kv->n_blocks > 1) return fail(ctx, LFPS_EINVAL, "lfps_pages_compact: moves is NULL");
   const OnDevice on(ctx->cfg.device);
