@@ -4,6 +4,7 @@
 #include <stdint.h>
 
 #include "lfps.h"
+#include "part_rooms.h"
 #include "range_rule.h"
 
 namespace lfps {
@@ -297,13 +298,8 @@ hipError_t launch_priors(const Shape& s, int dtype, const float* q, const KvView
 
 // Packed new tokens into the cache; their causal attention over it; full attention with shared first rows; pages.  See append.hip,
 // prompt_attn.hip, prefix_attn.hip and pages.hip.  part: room for part_rows (attn_part_rows) partial results of a query row.
-constexpr int kPartFloats = kD + 4;        // weighted sum of the values, largest score (powers of two), sum of the weights
-inline int64_t attn_part_rows(const Shape& s) {
-  // Two parts at least of every (request, head); otherwise what 256 workgroups of 256 query rows make.  And what cuts the rows that
-  // requests have for themselves.
-  const int64_t two = 2 * (int64_t)s.B * s.Hq;
-  return (two > 65536 ? two : 65536) + 8192;
-}
+static_assert(kPartFloats == kD + 4, "");
+inline int64_t attn_part_rows(const Shape& s) { return attn_part_rows_for(s.B, s.Hq, s.Hkv); }
 hipError_t launch_append(const Shape& s, int dtype, const KvView& kv, const void* k_new, const void* v_new, int64_t stride_t,
                          const int32_t* cu, int n_tokens, hipStream_t st);
 hipError_t launch_prompt_attn(const Shape& s, int dtype, const KvView& kv, const void* q, int64_t q_stride, const int32_t* cu,

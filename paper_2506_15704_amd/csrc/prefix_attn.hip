@@ -227,8 +227,8 @@ hipError_t prefix_t(PrefixArgs a, int dtype, float* out, int64_t part_rows, hipS
   const int tiles = s.B / (per / s.G) + a.groups.n;          // room for any groups; of groups of one size there are `usual`
   const int64_t usual = (int64_t)a.groups.n * ((size * s.G + per - 1) / per);
   // The workspace: parts of the shared rows; the plan of the own ones, and their parts.
-  const int64_t own_rows = (int64_t)own_items_most(s) * s.Hq, plan_rows = (own_plan_ints(s) + kPartFloats - 1) / kPartFloats;
-  const int64_t room = (part_rows - own_rows - plan_rows) / heads, by_len = (s.Lcap + 127) / 128;          // room: at least 1
+  const int64_t own_rows = (int64_t)own_items_most(s) * s.Hq, plan_rows = own_plan_rows_for(s.B, s.Hkv);
+  const int64_t room = (part_rows - own_rows - plan_rows) / heads, by_len = (s.Lcap + 127) / 128;          // room: at least 1 (part_rooms.h)
   int64_t splits = (256 + usual * s.Hkv - 1) / (usual * s.Hkv);
   for (const int64_t most : {room, by_len, (int64_t)kMaxSplits}) splits = splits < most ? splits : most;
   a.splits = (int)splits;

@@ -61,9 +61,7 @@ struct OwnRows {
   int32_t* item;             // [B + 1] its first item; of B: the number of all
   OwnItem* items;            // [own_items_most]
 };
-constexpr int kOwnWorkgroups = 1024, kOwnLeast = 64;         // wanted of the kernel over the items; rows that one has at least
-__host__ __device__ inline int own_items_most(const Shape& s) { return (s.Hkv < kOwnWorkgroups ? kOwnWorkgroups / s.Hkv : 1) + s.B; }
-inline int64_t own_plan_ints(const Shape& s) { return 4 * (int64_t)own_items_most(s) + 2 * s.B + 1; }
+__host__ __device__ inline int own_items_most(const Shape& s) { return own_items_for(s.B, s.Hkv); }
 
 // Full attention over the items' rows: part [items, Hkv, G, D + 2], each as of a part in the full-attention baseline.
 hipError_t launch_full_attn_own(const Shape& s, int dtype, const float* q, const KvView& kv, const OwnRows& own, float* part, hipStream_t st);
