@@ -281,7 +281,7 @@ int lfps_table_step_gated(lfps_ctx* ctx, const float* q, const lfps_kv* kv, cons
  * t*stride_t + g*D + c (slices of a fused projection; rows 16-byte aligned, stride_t >= Hkv*D).  The cache behind kv is
  * WRITTEN, at the rows named above and nowhere else; tokens at no row are dropped.  FP8 caches: rounded to nearest even,
  * values beyond +-448 and infinities become +-448, NaN stays NaN.  Two requests whose tables name the same block for a row
- * that both append leave either's (lfps_pages_update gives each its own). */
+ * that both append leave either's (lfps_pages_update gives each its own); rows whose entry names no block of the pool are dropped. */
 int lfps_append(lfps_ctx* ctx, const void* k_new, const void* v_new, int64_t stride_t, const int32_t* cu,
                 int32_t n_tokens, const lfps_kv* kv, void* stream);
 

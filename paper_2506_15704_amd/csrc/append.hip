@@ -61,6 +61,7 @@ __global__ __launch_bounds__(256) void k_append(Shape s, KvView kv, const TS* __
   const CacheRows<TK> K(kv.k, kv, b, g);
   const CacheRows<TV> V(kv.v, kv, b, g);
   const int e = K.entry((int)row);
+  if (kv.page.table && (uint32_t)e >= (uint32_t)kv.page.n_blocks) return;       // (readers clamp; a write would be into someone's block)
   Convert8<TS, TK>::move(k_new + from, const_cast<TK*>(K.at((int)row, e)) + c);
   Convert8<TS, TV>::move(v_new + from, const_cast<TV*>(V.at((int)row, e)) + c);
 }

@@ -61,3 +61,27 @@ def test_append_with_arrays_that_make_no_sense():
             used[block, at] = True
         assert bool(raw(x).transpose(1, 2)[~used].isnan().all()) and not bool(raw(x).transpose(1, 2)[used].isnan().any())
     c.ctx.close()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32", "fp8kv"])
+@pytest.mark.parametrize("page", [1, 16])
+def test_append_drops_rows_whose_table_entry_is_no_block(dtype, page):
+    """(lfps_pages_update leaves -1 for rows that a request did not get.)"""
+    c = CacheCase(dtype, 2, 2, [70, 40, 33], page, seed=6)
+    k, v = (c.randn(90, 2, D).to(c.q_dtype) for _ in range(2))
+    first = [70 - 50, 40 - 20, 33 - 20]
+    want = [raw(x).clone() for x in (c.K, c.V)]
+    for w, x, new in zip(want, (c.K, c.V), (k, v)):
+        for b, t0, t in ((0, 0, 50), (1, 50, 20), (2, 70, 20)):
+            for i in range(t):
+                j = (first[b] + i) // page
+                if not (b == 0 and j >= 48 // page or b == 2 and j == 32 // page):
+                    w[c.table[b, j], :, (first[b] + i) % page] = raw(to_cache(new[t0 + i].float(), x.dtype))
+    c.table[0, 48 // page:] = -1
+    c.table[2, 32 // page] = c.n_blocks
+    c.table[0, -1] = 2 ** 31 - 1
+    c.ctx.lfps_append(k, v, ints([0, 50, 70, 90]), c.view())
+    for x, w in zip((c.K, c.V), want):
+        bits = {1: torch.uint8, 2: torch.int16, 4: torch.int32}[x.element_size()]
+        assert torch.equal(raw(x).contiguous().view(bits), w.contiguous().view(bits))
+    c.ctx.close()
