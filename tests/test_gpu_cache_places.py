@@ -133,3 +133,40 @@ def test_fp16_prompts_keep_the_sum_of_many_small_weights():
     # 2^-15 < weight * 2^8 < 2^-14: a step of 2^-24 there, half of it 2^-10 of a weight (sum and output hold the same rounded one); output 2^-11
     assert bool(((out.double() - ref).abs() <= (2.0 ** -10 + 2.0 ** -11 + 2.0 ** -14) * ref).all())
     c.ctx.close()
+
+
+def _far_apart(x, stride_b, stride_n, dtype):
+    """[n, Hkv, rows, D] with the given strides in a buffer of its own, most of which nothing touches."""
+    n, Hkv, rows, _ = x.shape
+    size = (n - 1) * stride_b + (rows - 1) * stride_n + Hkv * D
+    y = torch.empty(size, dtype=raw(x).dtype, device=DEV).as_strided(x.shape, (stride_b, D, stride_n, 1))
+    y.copy_(raw(x))
+    return y.view(dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp8kv", "f32"])
+@pytest.mark.parametrize("layout,stride_b,stride_n", [(0, (1 << 30) + 64, 256), (0, 256, 3 << 20), (16, 80_000_000, 256), (16, 256, (9 << 24) + 32)])
+def test_rows_more_than_2_to_the_31_elements_apart(dtype, layout, stride_b, stride_n):
+    """Requests, rows, blocks, and rows of a block: the same results as close together, and the same rows appended and copied."""
+    lens, news = [700, 200, 333], [3, 150, 0]
+    c = CacheCase(dtype, 4, 2, lens, layout, cap=700, seed=6)
+    if layout == 0 and stride_n > stride_b:
+        stride_b = 2 * D                                       # (rows of the requests side by side: three of them in one stride)
+    far = [_far_apart(x, stride_b, stride_n, x.dtype) for x in (c.K, c.V)]
+    assert (far[0].shape[0] - 1) * stride_b + (far[0].shape[2] - 1) * stride_n > 1 << 31
+    q, qd = c.randn(153, 4, D).to(c.q_dtype), c.randn(3, 4, D)
+    k, v = (c.randn(153, 2, D).to(c.q_dtype) for _ in range(2))
+    cu, runs = ints([0, 3, 153, 153]), []
+    for K, V in ((c.K, c.V), far):
+        kv = c.ctx.paged_kv_view(K, V, c.table, c.seq) if layout else c.ctx.kv_view(K, V, c.seq)
+        if layout:
+            spare = sorted(set(range(c.n_blocks)) - set(c.table.flatten().tolist()))
+            c.ctx.lfps_pages_copy(kv, ints([[int(c.table[0, 2]), spare[-1], 16], [int(c.table[2, 1]), spare[0], 5]]))
+        c.ctx.lfps_append(k, v, cu, kv)
+        outs = [torch.zeros_like(q), torch.zeros_like(qd)]
+        c.ctx.lfps_prompt_attn(q, cu, kv, outs[0])
+        c.ctx.lfps_prefix_attn_decode(qd, kv, ints([0, 2, 3]), ints([150, 40]), outs[1])
+        runs.append(outs + [raw(x).contiguous().view(torch.uint8 if x.element_size() == 1 else torch.int16 if x.element_size() == 2 else torch.int32) for x in (K, V)])
+    for a, b in zip(*runs):
+        assert torch.equal(a, b)
+    c.ctx.close()
