@@ -301,7 +301,11 @@ int lfps_prompt_attn(lfps_ctx* ctx, const void* q, int64_t stride_t, const int32
  *   prefix_len  [n_groups] int32, clamped to [0, n of the group's first request]: row j < prefix_len[i] of any of them is row
  *               j of the group's first request (as far as the request has rows); what the others' own slabs or tables hold
  *               there is not read.
- *   q, out      [B, Hq, D] fp32.  Rows of out of requests in no group are left as they were.  1 <= n_groups <= B. */
+ *   q, out      [B, Hq, D] fp32.  Rows of out of requests in no group are left as they were.  1 <= n_groups <= B.
+ * Requests that share nothing are best one group with a prefix_len of 0: the call is made for few groups of like sizes and prefixes.
+ * Over shared rows, products with 16-bit and FP8 rows take the query and the softmax weights as sums of 16-bit terms: to 2^-22 of each
+ * (fp16; FP8 keys and values), else the query whole and the weights whole for groups of up to 64 query rows (requests * Hq / Hkv, by
+ * the average size), to 2^-18 for larger ones, so the last bits of a result depend on the groups.  Sums are fp32. */
 int lfps_prefix_attn_decode(lfps_ctx* ctx, const float* q, const lfps_kv* kv, const int32_t* group_start,
                             const int32_t* prefix_len, int32_t n_groups, float* out, void* stream);
 

@@ -1,8 +1,8 @@
 // The newest rows of every request into its cache: token i of the t_b packed tokens of request b becomes row n_b - t_b + i.  A
 // copy of t_b * Hkv rows of K and of V, from rows with a stride of their own (slices of a fused projection) to wherever the
 // cache has them; FP8 caches convert, to nearest even, values beyond +-448 (infinities too) to +-448, NaN to NaN.  Bound by the
-// bytes; a decode step's call by its latency: 32 tokens of 8 heads into FP8 pages 3.5 us, 25776 tokens of 8 heads in bf16 (211 MB read and
-// written) 36 us, 5.8 TB/s.
+// bytes; a decode step's call by its latency: 32 tokens of 8 heads into FP8 pages 3.7 us, 25776 tokens of 8 heads in bf16 (211 MB read and
+// written) 37 us, 5.7 TB/s.
 #include "tile_attn.h"
 
 namespace lfps {

@@ -10,7 +10,7 @@
 //
 // All of it is whole numbers, and none depends on the order of atomics.  A few dependent launches over 4 bytes an entry of the
 // table and 13 a block of the pool: bound by the launches.  The copies are bound by the bytes.  64 requests over a pool of 65536 blocks:
-// an update 3 + 5 + 5 + 3 + 5.5 us and a copy of their tails 4; a compaction's plan 23 us, its copy of 1.9 GB (read and written) 370, 5.1 TB/s.
+// an update 2 + 4 + 5 + 3.5 + 5.5 us and a copy of their tails 4; a compaction's plan 29 us in six launches, its copy of 1.9 GB (read and written) 370, 5.1 TB/s.
 #include "lfps_internal.h"
 
 namespace lfps {

@@ -9,8 +9,8 @@
 // fp32, as a sum of 16-bit terms, and so do the weights (tile_attn.h): the results are fp32 ones as everywhere in the library, 0.4 to 1.5e-6
 // from 64 bits where fp32 sums of the same rows are 0.5 to 2.6e-6.
 //
-// 32 heads over 8 KV heads: 64 requests over 32768 shared rows and 28267 own ones in bf16 119 us (part 1 86: 1000 TFLOP/s, of five products
-// where two would do in 16 bits; part 2 29, 4.0 TB/s; part 3 9), 32 requests in four groups over 40000 and 34000 rows of FP8 64 us (37,
+// 32 heads over 8 KV heads: 64 requests over 32768 shared rows and 28267 own ones in bf16 127 us (part 1 86: 1000 TFLOP/s, of five products
+// where two would do in 16 bits; part 2 29, 4.0 TB/s; part 3 9), 32 requests in four groups over 40000 and 34000 rows of FP8 69 us (37,
 // 27, 5), four over 2049 rows 20 us (10.5, 5.5, 5).
 #include "tile_pipe.h"
 
@@ -221,6 +221,9 @@ hipError_t prefix_t(PrefixArgs a, int dtype, float* out, int64_t part_rows, hipS
   // groups of 32 rows 27.3 / 30.5, 48 32.8 / 31.8, 64 30.4 / 32.4, 80 51.0 / 33.9, 128 39.5 / 37.9; FP8 26.1 / 29.5, 31.4 / 30.6, 29.1 / 32.5,
   // 48.6 / 34.1, 38.0 / 38.7.  (Tiles of 64 rows with half the keys a wave: 30.3, 35.1, 32.8, 45.1, 40.3 in bf16, never the best.)
   // fp32: tiles of 64 rows, of 128 where a group fills them.
+  // Form and parts follow from the number of groups, not from their sizes and prefixes, which are on the device.  Groups that are unlike
+  // pay for it: 32 requests over 30000 rows take 80 us with 500 rows each of their own, and 576 beside 32 groups of one request (170 where
+  // those are one group with a prefix of 0); a pair over 30000 beside 31 pairs over 100 rows takes 778, walked by a workgroup a KV head.
   const int size = (s.B + a.groups.n - 1) / a.groups.n, rows = size * s.G;
   const int key_waves = rows > 64 ? 1 : (sizeof(TK) == 4 ? 2 : 4);
   const int per = key_waves == 1 ? shared_rows<TK, 1>() : 32 * (4 / key_waves);

@@ -9,8 +9,8 @@
 // Which kernel takes a request is decided on the device by its number of tokens, so one call takes any mixture.
 //
 // 32 heads over 8 KV heads: 16384 tokens in bf16 1.90 ms, 1160 TFLOP/s of the 1370 that the largest products of the BLAS library reach
-// here; 8192 behind 24576 rows of FP8 pages 3.34 ms, 1150; eight prompts of 61 to 4096 tokens over 16 heads in fp16 214 us, 768; two of
-// 944 and 1307 in fp32 276 us, 77 of 155 TFLOP/s; five tokens over 4104 rows 13.4 us in two launches.  What each step gave is beside
+// here; 8192 behind 24576 rows of FP8 pages 3.34 ms, 1150; eight prompts of 61 to 4096 tokens over 16 heads in fp16 232 us, 710; two of
+// 944 and 1307 in fp32 279 us, 76 of 155 TFLOP/s; five tokens over 4104 rows 15.5 us in two launches (cards differ: 214 to 233, 13.4 to 15.8).  What each step gave is beside
 // the loops.
 #include "tile_pipe.h"
 
@@ -211,11 +211,14 @@ hipError_t prompt_t(const Shape& s, const KvView& kv, const void* q, int64_t q_s
   // loop asks for rows earlier and hides a stage's parts behind each other: it is the quicker one until the requests fill the chip by
   // themselves.  us, few / tiles: one token over 4100 rows of 8 KV heads 15.5 / 13.3, over 32768 38.1 / 33.1; 16 requests of 4 tokens
   // over 4100 rows 64.8 / 54.4 (FP8 65.0 / 49.9), of one over 8192 109 / 120 (111 / 87); 64 of one over 2048 112 / 123 (112 / 91), of
-  // seven 113 / 171 (112 / 136).  fp32: 32 / 50, 135 / 239, 270 / 464, 514 / 900.
+  // seven 113 / 171 (112 / 136).  fp32: 32 / 50, 135 / 239, 270 / 464, 514 / 900.  The rule looks at neither the format nor the lengths,
+  // and so takes the slower one in two of these: bf16 16 of one over 8192 (120), FP8 64 of one over 2048 (112).
   // Only where the tiles are not many more than the requests: their number decides how many parts either has, and a single token over many
   // rows needs many, beside a prompt too (2048 tokens and seven single ones over 30000 rows 247 / 689, 512 and three over 16000 83 / 118;
-  // eight ragged prompts of many tokens, where k_prompt_few finds nothing to do, 214 / 211).  What is left: 9 to 63 tokens over many rows
-  // beside a long prompt are a workgroup a KV head.
+  // eight ragged prompts of many tokens, where k_prompt_few finds nothing to do, 214 / 211).  What is left:
+  // the tiles are those that the batch and n_tokens leave room for, not those that are there.  9 to 63 tokens over many rows beside a
+  // long prompt are a workgroup a KV head (20 behind 30000 rows beside 2048: 607 us), and so are the few requests with tokens in a
+  // context of many (20 tokens of one request behind 32768 rows: 41 us in a context of one, 335 of 16, 665 of 64; 512 tokens 319, 440, 771).
   const bool small = sizeof(TK) != 4 && s.B * s.Hkv <= 128 && n_tokens <= (int64_t)per * s.B;
   const bool all_few = !small && (int64_t)n_tokens * s.G <= kMost, none_few = small || (!all_few && s.B == 1);
   const int tiles = n_tokens / per + s.B;

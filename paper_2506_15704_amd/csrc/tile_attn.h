@@ -444,9 +444,9 @@ constexpr int tile_lds() {
 template <typename T>
 constexpr int few_key_waves() { return sizeof(T) == 4 ? 2 : 4; }
 
-// load_q: brings the query operand, which nothing waits for until the first rows have been asked for.
-// The loop of a workgroup whose four waves are kRowWaves rows of waves (32 query rows each) by kKeyWaves (which share a stage's
-// keys).  q, limit: my query row's operand and the keys it sees.  wave_limit: the most that a row of my wave sees, and least.
+// The loop of a workgroup whose four waves are 4 / kKeyWaves rows of waves (32 query rows each) by kKeyWaves (which share a stage's
+// keys), over the rows [first, end).  load_q: brings my query row's operand, which nothing waits for until the first rows have been
+// asked for.  limit: the keys that my query row sees.
 template <typename TK, typename TV, int kKeyWaves, typename Op, int kTerms, typename LoadQ>
 __device__ __forceinline__ void tile_loop(char* lds, const CacheRows<TK>& K, const CacheRows<TV>& V, int first, int end, LoadQ load_q,
                                           int limit, RowState<Op, kTerms>& st) {

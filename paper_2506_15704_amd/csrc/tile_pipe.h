@@ -1,5 +1,5 @@
-// The prompt kernel's body for 16-bit operands (bf16, fp16, FP8 converted to bf16): tile_attn.h's products, made for the matrix
-// units' rate.
+// The body of the prompt kernel, and of large groups of a shared prefix, for 16-bit operands (bf16, fp16; FP8 rows as bf16 in prompts, as
+// fp16 in prefixes): tile_attn.h's products, made for the matrix units' rate.
 //
 // Steps, over 16384 tokens of 32 heads in bf16: rows through registers, 128 query rows a workgroup, 5.09 ms; straight into LDS, a maximum that
 // is followed lazily 2.17; 256 query rows, places without bank conflicts, scores of the next stage beside the weights of this one
