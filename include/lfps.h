@@ -296,6 +296,67 @@ int lfps_append(lfps_ctx* ctx, const void* k_new, const void* v_new, int64_t str
 int lfps_prompt_attn(lfps_ctx* ctx, const void* q, int64_t stride_t, const int32_t* cu, int32_t n_tokens,
                      const lfps_kv* kv, void* out, void* stream);
 
+/* What stands between the projection and the attention, in one pass: every head of q and k_new is brought to unit mean square,
+ *   y_c = x_c / sqrt(mean_c x_c^2 + eps) * weight_c       (weight NULL: y = x),
+ * its first rotary_dim channels are turned in pairs by the token's position,
+ *   (y_a, y_b) -> (y_a cos x - y_b sin x, y_b cos x + y_a sin x),   x = positions[pair_axis[i]][t] * inv_freq[i]   for pair i = (a, b),
+ * and keys and values go into the cache as in lfps_append (which takes keys that are turned already). */
+typedef struct {
+  const float* q_weight;    /* [D] fp32, 16-byte aligned, or NULL: the query heads are not normed */
+  const float* k_weight;    /* the same of the key heads */
+  const float* inv_freq;    /* [rotary_dim / 2] fp32: a pair's angle per position */
+  const int32_t* pair_axis; /* [rotary_dim / 2]: the row of positions that turns a pair (time, height, width, ...), clamped to n_axes; NULL: row 0 */
+  float eps;                /* >= 0 */
+  int32_t rotary_dim;       /* a multiple of 16 in [0, D]; channels behind them are not turned */
+  int32_t n_axes;           /* rows of positions, 1 to 8; more than one needs pair_axis and positions */
+  int32_t interleaved;      /* pair i is the channels 0: i and i + rotary_dim / 2, 1: 2 i and 2 i + 1 */
+} lfps_rotary;
+/*   q, k_new, v_new  [n_tokens, Hq or Hkv, D] of cfg.kv_dtype, element (t, h, c) at t*stride_t + h*D + c (slices of one fused projection; rows 16-byte
+ *              aligned, stride_t >= Hq*D)
+ *   positions  [n_axes, n_tokens] int32, any values; NULL: a token's cache row
+ *   q_out      [n_tokens, Hq, D], contiguous, 16-byte aligned, of q_out_dtype: LFPS_F32 (what the decode steps take: one token a request makes [B, Hq, D])
+ *              or cfg.kv_dtype (lfps_prompt_attn, lfps_window_attn).  It must not overlap the inputs.  A token at no row gets zeros, rows of
+ *              tokens of no request are left as they were.
+ * Norms, angles and turns are fp32, with angles reduced in 64 bits; every value is rounded once, to the type that it is stored in (FP8: as in lfps_append). */
+int lfps_rotate_append(lfps_ctx* ctx, const lfps_rotary* rot, const void* q, const void* k_new, const void* v_new, int64_t stride_t,
+                       const int32_t* positions, const int32_t* cu, int32_t n_tokens, const lfps_kv* kv, void* q_out, int32_t q_out_dtype,
+                       void* stream);
+
+/* lfps_prompt_attn and lfps_full_attn_decode over a sliding window and the first rows: the token at row p sees the rows j <= p with
+ * j > p - window (window >= 1: its own row is the last of them) or j < n_sink.  Arguments else as there; out must not overlap q. */
+int lfps_window_attn(lfps_ctx* ctx, const void* q, int64_t stride_t, const int32_t* cu, int32_t n_tokens, const lfps_kv* kv, int32_t window,
+                     int32_t n_sink, void* out, void* stream);
+int lfps_window_attn_decode(lfps_ctx* ctx, const float* q, const lfps_kv* kv, int32_t window, int32_t n_sink, float* out, void* stream);
+
+/* Accumulated attention weight.  For all rows j < n_b:
+ *   mass[b,g,j] = (j < held[b] ? decay * mass[b,g,j] : 0) + sum over the new tokens t of b and the heads h of g of softmax_j(q[t,h].K[b,g,j]/sqrt(D))
+ * with the rows that lfps_prompt_attn gives a token (its own and those before).  The tokens may be fewer than were appended last: the newest 32 of a
+ * prompt are packed as a call with cu of their own.
+ *   held   [B] int32: rows that have a weight already (0 after a prompt's first call, the rows before the new ones later); NULL: none, mass
+ *          is written whole.  decay in [0, 1].
+ *   mass   [B, Hkv, max_seq_len] fp32, 16-byte aligned; rows from n_b on are left as they were
+ * kv->v is not read.  Products and sums are fp32; sums come in the same order every time. */
+int lfps_attn_mass(lfps_ctx* ctx, const void* q, int64_t stride_t, const int32_t* cu, int32_t n_tokens, const lfps_kv* kv, const int32_t* held,
+                   float decay, float* mass, void* stream);
+/* lfps_full_attn_decode that adds its weights up too (q, out [B, Hq, D] fp32; mass as above, the one token of a request being its row n_b - 1).
+ * q, out and mass must not overlap. */
+int lfps_full_attn_mass_decode(lfps_ctx* ctx, const float* q, const lfps_kv* kv, const int32_t* held, float decay, float* mass, float* out,
+                               void* stream);
+
+/* Eviction: every KV head of request b keeps m_b = min(n_b, budget[b]) of its rows: the first n_sink, the n_recent newest (as far as there is room), and
+ * between them those of the largest mass (of equal ones the lower rows; NaN counts as least).  The kept rows move to the front in order: row i of the
+ * result is row kept[b,g,i] of K and V.  Keys stay as they were turned.
+ *   mass, mass_out [B, Hkv, max_seq_len] fp32; mass_out[b,g,i] = mass[b,g,kept[b,g,i]]
+ *   budget [B] int32, clamped to [0, n_b];  lens_out [B] int32: m_b
+ *   kept   [B, Hkv, max_seq_len] int32.  Entries of mass_out and kept from m_b on are left as they were.
+ *   to     NULL: in place; K and V of kv are WRITTEN, at rows below m_b that change.  No other request may then have these rows (a shared block
+ *          would change for all of them).  Else the view that receives the rows (its k, v, strides, table; its seq_lens are not read): other
+ *          slabs, or blocks that no request of kv has, of the same pool too; rows whose table entry names no block are dropped.
+ * The calls of several layers read the same lengths: swap lens_out in when all have been made (lfps_pages_update with new_lens = m_b then frees the
+ * blocks behind).  Written arrays must not overlap read ones, nor each other. */
+int lfps_evict(lfps_ctx* ctx, const lfps_kv* kv, const float* mass, const int32_t* budget, int32_t n_sink, int32_t n_recent, const lfps_kv* to,
+               float* mass_out, int32_t* kept, int32_t* lens_out, void* stream);
+
 /* lfps_full_attn_decode for a batch in which groups of requests share their first rows, which are then read once a group.
  *   group_start [n_groups + 1] int32, rising: group i is the requests group_start[i] <= b < group_start[i+1]
  *   prefix_len  [n_groups] int32, clamped to [0, n of the group's first request]: row j < prefix_len[i] of any of them is row
@@ -397,7 +458,11 @@ enum {
   LFPS_KERNEL_APPEND = 17,
   LFPS_KERNEL_PAGES_PLAN = 18,
   LFPS_KERNEL_PAGES_COPY = 19,
-  LFPS_N_KERNELS = 20
+  LFPS_KERNEL_ROTATE_APPEND = 20,
+  LFPS_KERNEL_WINDOW_ATTN = 21,
+  LFPS_KERNEL_ATTN_MASS = 22,
+  LFPS_KERNEL_EVICT = 23,
+  LFPS_N_KERNELS = 24
 };
 #define LFPS_TIMING_MAX_LAUNCHES 4096
 int lfps_timing_enable(lfps_ctx* ctx, int32_t on);

@@ -23,7 +23,7 @@ LFPS_FLAG_CAND_OVERFLOW = 1
 LFPS_FLAG_TABLE_FULL = 2
 LFPS_FLAG_Q_RANGE = 4
 LFPS_FLAG_PAGES_FULL = 8
-N_KERNELS = 20
+N_KERNELS = 24
 NOALLOC_MAX_SCORES = 2097152
 
 
@@ -47,6 +47,11 @@ class lfps_kv(ctypes.Structure):
                 ("seq_lens", ctypes.c_void_p), ("block_table", ctypes.c_void_p),
                 ("block_size", ctypes.c_int32), ("block_table_stride", ctypes.c_int32),
                 ("n_blocks", ctypes.c_int32)]
+
+
+class lfps_rotary(ctypes.Structure):
+    _fields_ = [("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p), ("inv_freq", ctypes.c_void_p), ("pair_axis", ctypes.c_void_p),
+                ("eps", ctypes.c_float), ("rotary_dim", ctypes.c_int32), ("n_axes", ctypes.c_int32), ("interleaved", ctypes.c_int32)]
 
 
 def _load() -> ctypes.CDLL:
@@ -89,6 +94,13 @@ def _load() -> ctypes.CDLL:
         "lfps_head_sparsity": (ctypes.c_int, [P, VP, ctypes.POINTER(lfps_kv), VP, VP, I32, ctypes.c_float, VP, VP, VP]),
         "lfps_append": (ctypes.c_int, [P, VP, VP, ctypes.c_int64, VP, I32, ctypes.POINTER(lfps_kv), VP]),
         "lfps_prompt_attn": (ctypes.c_int, [P, VP, ctypes.c_int64, VP, I32, ctypes.POINTER(lfps_kv), VP, VP]),
+        "lfps_rotate_append": (ctypes.c_int, [P, ctypes.POINTER(lfps_rotary), VP, VP, VP, ctypes.c_int64, VP, VP, I32, ctypes.POINTER(lfps_kv), VP,
+                                              I32, VP]),
+        "lfps_window_attn": (ctypes.c_int, [P, VP, ctypes.c_int64, VP, I32, ctypes.POINTER(lfps_kv), I32, I32, VP, VP]),
+        "lfps_window_attn_decode": (ctypes.c_int, [P, VP, ctypes.POINTER(lfps_kv), I32, I32, VP, VP]),
+        "lfps_attn_mass": (ctypes.c_int, [P, VP, ctypes.c_int64, VP, I32, ctypes.POINTER(lfps_kv), VP, ctypes.c_float, VP, VP]),
+        "lfps_full_attn_mass_decode": (ctypes.c_int, [P, VP, ctypes.POINTER(lfps_kv), VP, ctypes.c_float, VP, VP, VP]),
+        "lfps_evict": (ctypes.c_int, [P, ctypes.POINTER(lfps_kv), VP, VP, I32, I32, ctypes.POINTER(lfps_kv), VP, VP, VP, VP]),
         "lfps_prefix_attn_decode": (ctypes.c_int, [P, VP, ctypes.POINTER(lfps_kv), VP, VP, I32, VP, VP]),
         "lfps_pages_workspace_bytes": (ctypes.c_int, [I32, ctypes.POINTER(ctypes.c_int64)]),
         "lfps_pages_update": (ctypes.c_int, [P, ctypes.POINTER(lfps_kv), VP, VP, VP, VP, VP, VP, VP, ctypes.c_int64, VP]),
@@ -436,6 +448,82 @@ class Lfps:
             return
         self._check(_lib.lfps_prompt_attn(self._ctx, pq, sq, _ptr(cu, torch.int32, (self.B + 1,), "cu", d), int(q.shape[0]),
                                           ctypes.byref(kv), po, self._stream()))
+
+    # ------------------------------------------------------------------ a cache of bounded length
+    def rotary(self, inv_freq=None, q_weight=None, k_weight=None, eps: float = 0.0, pair_axis=None, n_axes: int = 1,
+               interleaved: bool = False) -> lfps_rotary:
+        """How lfps_rotate_append norms and turns heads: inv_freq [rotary_dim / 2] fp32 (None: nothing is turned), weights [D] fp32 (None: no
+        norm), pair_axis [rotary_dim / 2] int32."""
+        d, half = self.device, 0 if inv_freq is None else int(inv_freq.shape[0])
+        rot = lfps_rotary(_ptr(q_weight, torch.float32, (self.D,), "q_weight", d), _ptr(k_weight, torch.float32, (self.D,), "k_weight", d),
+                          _ptr(inv_freq, torch.float32, (half,), "inv_freq", d), _ptr(pair_axis, torch.int32, (half,), "pair_axis", d),
+                          float(eps), 2 * half, int(n_axes), int(bool(interleaved)))
+        rot._keep = (q_weight, k_weight, inv_freq, pair_axis)
+        return rot
+
+    def lfps_rotate_append(self, rot: lfps_rotary, q, k_new, v_new, positions, cu, kv: lfps_kv, q_out):
+        """q, k_new, v_new: [tokens, heads, D] of kv_dtype, packed (slices of one fused projection: equal token strides); positions: [n_axes, tokens]
+        int32, [tokens] for one axis, or None (the cache rows); q_out: [tokens, Hq, D], fp32 or kv_dtype.  The cache behind the view is
+        written."""
+        d, T = self.device, int(q.shape[0])
+        pq, sq = _token_rows(q, self.kv_torch_dtype, self.Hq, "q", d)
+        pk, sk = _token_rows(k_new, self.kv_torch_dtype, self.Hkv, "k_new", d)
+        pv, sv = _token_rows(v_new, self.kv_torch_dtype, self.Hkv, "v_new", d)
+        if k_new.shape[0] != T or v_new.shape[0] != T or (T > 1 and not sq == sk == sv):
+            raise ValueError("q, k_new and v_new must share tokens and token stride")
+        if positions is not None and positions.dim() == 1:
+            positions = positions.unsqueeze(0)
+        pp = _ptr(positions, torch.int32, (rot.n_axes, T), "positions", d)
+        if q_out.dtype not in (torch.float32, self.kv_torch_dtype):
+            raise TypeError(f"q_out: expected dtype torch.float32 or {self.kv_torch_dtype}, got {q_out.dtype}")
+        po = _ptr(q_out, q_out.dtype, tuple(q.shape), "q_out", d)
+        if T == 0:
+            return
+        self._check(_lib.lfps_rotate_append(
+            self._ctx, ctypes.byref(rot), pq, pk, pv, max(sq, sk, sv), pp, _ptr(cu, torch.int32, (self.B + 1,), "cu", d), T, ctypes.byref(kv), po,
+            LFPS_F32 if q_out.dtype == torch.float32 else self.cfg.kv_dtype, self._stream()))
+
+    def lfps_window_attn(self, q, cu, kv: lfps_kv, window: int, n_sink: int, out):
+        """Arguments as lfps_prompt_attn's; a token sees the newest `window` rows up to its own and the first n_sink."""
+        d = self.device
+        pq, sq = _token_rows(q, self.kv_torch_dtype, self.Hq, "q", d)
+        po = _ptr(out, self.kv_torch_dtype, tuple(q.shape), "out", d)
+        if q.shape[0] == 0:
+            return
+        self._check(_lib.lfps_window_attn(self._ctx, pq, sq, _ptr(cu, torch.int32, (self.B + 1,), "cu", d), int(q.shape[0]), ctypes.byref(kv),
+                                          int(window), int(n_sink), po, self._stream()))
+
+    def lfps_window_attn_decode(self, q, kv: lfps_kv, window: int, n_sink: int, out):
+        d = self.device
+        self._check(_lib.lfps_window_attn_decode(
+            self._ctx, _ptr(q, torch.float32, (self.B, self.Hq, self.D), "q", d), ctypes.byref(kv), int(window), int(n_sink),
+            _ptr(out, torch.float32, (self.B, self.Hq, self.D), "out", d), self._stream()))
+
+    def lfps_attn_mass(self, q, cu, kv: lfps_kv, mass, held=None, decay: float = 1.0):
+        """q: [tokens, Hq, D] of kv_dtype, packed: the requests' newest tokens; mass: [B, Hkv, max_seq_len] fp32; held: [B] rows that have a weight
+        already (None: mass is written whole)."""
+        d = self.device
+        pq, sq = _token_rows(q, self.kv_torch_dtype, self.Hq, "q", d)
+        self._check(_lib.lfps_attn_mass(
+            self._ctx, pq, sq, _ptr(cu, torch.int32, (self.B + 1,), "cu", d), int(q.shape[0]), ctypes.byref(kv),
+            _ptr(held, torch.int32, (self.B,), "held", d), float(decay), _ptr(mass, torch.float32, (self.B, self.Hkv, self.Lcap), "mass", d),
+            self._stream()))
+
+    def lfps_full_attn_mass_decode(self, q, kv: lfps_kv, mass, out, held=None, decay: float = 1.0):
+        d = self.device
+        self._check(_lib.lfps_full_attn_mass_decode(
+            self._ctx, _ptr(q, torch.float32, (self.B, self.Hq, self.D), "q", d), ctypes.byref(kv), _ptr(held, torch.int32, (self.B,), "held", d),
+            float(decay), _ptr(mass, torch.float32, (self.B, self.Hkv, self.Lcap), "mass", d),
+            _ptr(out, torch.float32, (self.B, self.Hq, self.D), "out", d), self._stream()))
+
+    def lfps_evict(self, kv: lfps_kv, mass, budget, n_sink: int, n_recent: int, mass_out, kept, lens_out, to: Optional[lfps_kv] = None):
+        """mass, mass_out [B, Hkv, max_seq_len] fp32, kept the same in int32, budget and lens_out [B] int32; to: the view that receives the kept rows
+        (None: in place, the cache behind kv is written)."""
+        d, shape = self.device, (self.B, self.Hkv, self.Lcap)
+        self._check(_lib.lfps_evict(
+            self._ctx, ctypes.byref(kv), _ptr(mass, torch.float32, shape, "mass", d), _ptr(budget, torch.int32, (self.B,), "budget", d), int(n_sink),
+            int(n_recent), None if to is None else ctypes.byref(to), _ptr(mass_out, torch.float32, shape, "mass_out", d),
+            _ptr(kept, torch.int32, shape, "kept", d), _ptr(lens_out, torch.int32, (self.B,), "lens_out", d), self._stream()))
 
     def lfps_prefix_attn_decode(self, q, kv: lfps_kv, group_start, prefix_len, out):
         d, n = self.device, int(prefix_len.shape[0])

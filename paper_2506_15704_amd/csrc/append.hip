@@ -3,38 +3,10 @@
 // cache has them; FP8 caches convert, to nearest even, values beyond +-448 (infinities too) to +-448, NaN to NaN.  Bound by the
 // bytes; a decode step's call by its latency: 32 tokens of 8 heads into FP8 pages 3.7 us, 25776 tokens of 8 heads in bf16 (211 MB read and
 // written) 37 us, 5.7 TB/s.
+#include "stored_rows.h"
 #include "tile_attn.h"
 
 namespace lfps {
-
-namespace {
-
-// Eight elements as they are stored: TS of the new rows, TC of the cache.
-template <typename TS, typename TC>
-struct Convert8 {
-  static_assert(sizeof(TS) == sizeof(TC), "");
-  __device__ __forceinline__ static void move(const TS* from, TC* to) {
-#pragma unroll
-    for (int u = 0; u < (int)sizeof(TS) / 2; ++u) reinterpret_cast<u32x4*>(to)[u] = reinterpret_cast<const u32x4*>(from)[u];
-  }
-};
-template <>
-struct Convert8<uint16_t, uint8_t> {
-  __device__ __forceinline__ static void move(const uint16_t* from, uint8_t* to) {
-    const u32x4 w = *reinterpret_cast<const u32x4*>(from);
-    u32x2 r;
-    auto kept = [](float x) { return x != x ? x : fminf(fmaxf(x, -448.f), 448.f); };
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      int v = __builtin_amdgcn_cvt_pk_fp8_f32(kept(bf16_lo(w[2 * u])), kept(bf16_hi(w[2 * u])), 0, false);
-      v = __builtin_amdgcn_cvt_pk_fp8_f32(kept(bf16_lo(w[2 * u + 1])), kept(bf16_hi(w[2 * u + 1])), v, true);
-      r[u] = (uint32_t)v;
-    }
-    *reinterpret_cast<u32x2*>(to) = r;
-  }
-};
-
-}  // namespace
 
 // 16 lanes a (token, KV head), 8 channels a lane
 template <typename TS, typename TK, typename TV>

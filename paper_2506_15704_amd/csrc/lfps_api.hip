@@ -1,5 +1,6 @@
 // The C ABI of liblfps: context, argument validation, workspace, per-kernel timing, and the
 // sequencing of the kernels for each entry point.  No arithmetic of the method lives here.
+#include <math.h>
 #include <stdio.h>
 #include <string.h>
 
@@ -73,7 +74,8 @@ static const char* const kKernelNames[LFPS_N_KERNELS] = {
     "candidates", "gather_score", "select", "sparse_attn",
     "dense_score", "full_attn", "full_merge", "head_score", "filter_score", "filter_select",
     "table_flags", "table_candidates", "table_update", "filter_select_attend", "select_attend",
-    "prompt_attn", "prefix_attn", "append", "pages_plan", "pages_copy"};
+    "prompt_attn", "prefix_attn", "append", "pages_plan", "pages_copy",
+    "rotate_append", "window_attn", "attn_mass", "evict"};
 
 // Margin below the previous step's k-th best score at which the filtered pass keeps a row.
 static const float kFilterMargin = 0.125f;
@@ -1026,6 +1028,157 @@ int lfps_prompt_attn(lfps_ctx* ctx, const void* q, int64_t stride_t, const int32
   hipStream_t st = (hipStream_t)stream;
   LAUNCH(ctx, LFPS_KERNEL_PROMPT_ATTN, st,
          launch_prompt_attn(ctx->shape, ctx->cfg.kv_dtype, v, q, stride_t, cu, n_tokens, out, ctx->part, attn_part_rows(ctx->shape), st));
+  return LFPS_OK;
+}
+
+int lfps_rotate_append(lfps_ctx* ctx, const lfps_rotary* rot, const void* q, const void* k_new, const void* v_new, int64_t stride_t,
+                       const int32_t* positions, const int32_t* cu, int32_t n_tokens, const lfps_kv* kv, void* q_out, int32_t q_out_dtype, void* stream) {
+  if (!ctx) return LFPS_EINVAL;
+  if (!rot || !q || !k_new || !v_new || !cu || !q_out) return fail(ctx, LFPS_EINVAL, "lfps_rotate_append: NULL argument");
+  KvView v;
+  const Shape& s = ctx->shape;
+  int rc = check_kv_both(ctx, kv, &v);
+  if (rc == LFPS_OK) rc = check_n_tokens(ctx, n_tokens);
+  const char* rows = "lfps_rotate_append: q, k_new and v_new need 16-byte aligned rows and stride_t >= their heads * head_dim";
+  if (rc == LFPS_OK) rc = check_tokens(ctx, q, stride_t, s.Hq, rows);
+  if (rc == LFPS_OK) rc = check_tokens(ctx, k_new, stride_t, s.Hkv, rows);
+  if (rc == LFPS_OK) rc = check_tokens(ctx, v_new, stride_t, s.Hkv, rows);
+  if (rc != LFPS_OK) return rc;
+  if (q_out_dtype != LFPS_F32 && q_out_dtype != ctx->cfg.kv_dtype) return fail(ctx, LFPS_EINVAL, "lfps_rotate_append: q_out_dtype must be LFPS_F32 or kv_dtype");
+  const bool q_f32 = q_out_dtype == LFPS_F32;
+  if ((uintptr_t)q_out % 16) return fail(ctx, LFPS_EINVAL, "lfps_rotate_append: q_out must be 16-byte aligned");
+  if (rot->rotary_dim < 0 || rot->rotary_dim > kD || rot->rotary_dim % 16) return fail(ctx, LFPS_EINVAL, "lfps_rotary: rotary_dim must be a multiple of 16 in [0, head_dim]");
+  if (rot->rotary_dim && !rot->inv_freq) return fail(ctx, LFPS_EINVAL, "lfps_rotary: inv_freq is NULL");
+  if (rot->n_axes < 1 || rot->n_axes > 8) return fail(ctx, LFPS_EINVAL, "lfps_rotary: n_axes must be in [1, 8]");
+  if (rot->n_axes > 1 && rot->rotary_dim && (!rot->pair_axis || !positions)) return fail(ctx, LFPS_EINVAL, "lfps_rotary: several axes need pair_axis and positions");
+  if (rot->interleaved != 0 && rot->interleaved != 1) return fail(ctx, LFPS_EINVAL, "lfps_rotary: interleaved must be 0 or 1");
+  if (!(rot->eps >= 0.f) || !(rot->eps < INFINITY)) return fail(ctx, LFPS_EINVAL, "lfps_rotary: eps must be finite and >= 0");
+  if ((uintptr_t)rot->q_weight % 16 || (uintptr_t)rot->k_weight % 16) return fail(ctx, LFPS_EINVAL, "lfps_rotary: weights must be 16-byte aligned");
+  if (n_tokens == 0) return LFPS_OK;
+  // (heads are read by other waves than write them)
+  const int64_t e = elem_bytes(ctx->cfg), before = e * (n_tokens - 1) * stride_t;
+  const Span in_q = {q, before + e * s.Hq * kD}, in_k = {k_new, before + e * s.Hkv * kD}, in_v = {v_new, before + e * s.Hkv * kD};
+  const Span out = {q_out, (int64_t)n_tokens * s.Hq * kD * (q_f32 ? 4 : e)};
+  if (overlap(out, in_q) || overlap(out, in_k) || overlap(out, in_v)) return fail(ctx, LFPS_EINVAL, "lfps_rotate_append: q_out overlaps an input");
+  const Rotary r = {rot->q_weight, rot->k_weight, rot->inv_freq, rot->pair_axis, rot->eps, rot->rotary_dim, rot->n_axes, rot->interleaved};
+  const OnDevice on(ctx->cfg.device);
+  hipStream_t st = (hipStream_t)stream;
+  LAUNCH(ctx, LFPS_KERNEL_ROTATE_APPEND, st,
+         launch_rotate_append(s, ctx->cfg.kv_dtype, v, r, q, k_new, v_new, stride_t, positions, cu, n_tokens, q_out, q_f32, st));
+  return LFPS_OK;
+}
+
+static int check_window(lfps_ctx* ctx, int32_t window, int32_t n_sink) {
+  if (window < 1) return fail(ctx, LFPS_EINVAL, "window must be >= 1");
+  return n_sink < 0 ? fail(ctx, LFPS_EINVAL, "n_sink must be >= 0") : LFPS_OK;
+}
+
+int lfps_window_attn(lfps_ctx* ctx, const void* q, int64_t stride_t, const int32_t* cu, int32_t n_tokens, const lfps_kv* kv, int32_t window,
+                     int32_t n_sink, void* out, void* stream) {
+  if (!ctx) return LFPS_EINVAL;
+  if (!q || !cu || !out) return fail(ctx, LFPS_EINVAL, "lfps_window_attn: NULL argument");
+  KvView v;
+  int rc = check_kv_both(ctx, kv, &v);
+  if (rc == LFPS_OK) rc = check_n_tokens(ctx, n_tokens);
+  if (rc == LFPS_OK)
+    rc = check_tokens(ctx, q, stride_t, ctx->shape.Hq, "lfps_window_attn: q needs 16-byte aligned rows and stride_t >= n_q_heads * head_dim");
+  if (rc == LFPS_OK) rc = check_window(ctx, window, n_sink);
+  if (rc != LFPS_OK) return rc;
+  if ((uintptr_t)out % 16) return fail(ctx, LFPS_EINVAL, "lfps_window_attn: out must be 16-byte aligned");
+  if (n_tokens == 0) return LFPS_OK;
+  const int64_t e = elem_bytes(ctx->cfg), wide = (int64_t)ctx->shape.Hq * kD;
+  if (overlap({q, e * ((n_tokens - 1) * stride_t + wide)}, {out, e * n_tokens * wide})) return fail(ctx, LFPS_EINVAL, "lfps_window_attn: out overlaps q");
+  const OnDevice on(ctx->cfg.device);
+  hipStream_t st = (hipStream_t)stream;
+  LAUNCH(ctx, LFPS_KERNEL_WINDOW_ATTN, st,
+         launch_window_attn(ctx->shape, ctx->cfg.kv_dtype, v, q, stride_t, cu, n_tokens, window, n_sink, out, ctx->part, attn_part_rows(ctx->shape), st));
+  return LFPS_OK;
+}
+
+int lfps_window_attn_decode(lfps_ctx* ctx, const float* q, const lfps_kv* kv, int32_t window, int32_t n_sink, float* out, void* stream) {
+  if (!ctx) return LFPS_EINVAL;
+  if (!q || !out) return fail(ctx, LFPS_EINVAL, "lfps_window_attn_decode: NULL argument");
+  KvView v;
+  int rc = check_kv_both(ctx, kv, &v);
+  if (rc == LFPS_OK) rc = check_window(ctx, window, n_sink);
+  if (rc != LFPS_OK) return rc;
+  if ((uintptr_t)q % 16 || (uintptr_t)out % 16) return fail(ctx, LFPS_EINVAL, "lfps_window_attn_decode: q and out must be 16-byte aligned");
+  const int64_t bytes = 4 * (int64_t)ctx->shape.B * ctx->shape.Hq * kD;
+  if (overlap({q, bytes}, {out, bytes})) return fail(ctx, LFPS_EINVAL, "lfps_window_attn_decode: out overlaps q");
+  const OnDevice on(ctx->cfg.device);
+  hipStream_t st = (hipStream_t)stream;
+  LAUNCH(ctx, LFPS_KERNEL_WINDOW_ATTN, st,
+         launch_window_attn_decode(ctx->shape, ctx->cfg.kv_dtype, v, q, window, n_sink, out, ctx->part, attn_part_rows(ctx->shape), st));
+  return LFPS_OK;
+}
+
+static Span mass_span(const lfps_ctx* ctx, const void* p) { return {p, 4 * (int64_t)ctx->shape.B * ctx->shape.Hkv * ctx->shape.Lcap}; }
+
+int lfps_attn_mass(lfps_ctx* ctx, const void* q, int64_t stride_t, const int32_t* cu, int32_t n_tokens, const lfps_kv* kv, const int32_t* held,
+                   float decay, float* mass, void* stream) {
+  if (!ctx) return LFPS_EINVAL;
+  if ((!q && n_tokens) || !cu || !mass) return fail(ctx, LFPS_EINVAL, "lfps_attn_mass: NULL argument");
+  KvView v;
+  int rc = check_kv(ctx, kv, false, &v);
+  if (rc == LFPS_OK) rc = check_n_tokens(ctx, n_tokens);
+  if (rc == LFPS_OK && n_tokens)
+    rc = check_tokens(ctx, q, stride_t, ctx->shape.Hq, "lfps_attn_mass: q needs 16-byte aligned rows and stride_t >= n_q_heads * head_dim");
+  if (rc != LFPS_OK) return rc;
+  if (!(decay >= 0.f && decay <= 1.f)) return fail(ctx, LFPS_EINVAL, "lfps_attn_mass: decay must be in [0, 1]");
+  if ((uintptr_t)mass % 16) return fail(ctx, LFPS_EINVAL, "lfps_attn_mass: mass must be 16-byte aligned");
+  const OnDevice on(ctx->cfg.device);
+  hipStream_t st = (hipStream_t)stream;
+  LAUNCH(ctx, LFPS_KERNEL_ATTN_MASS, st,
+         launch_attn_mass(ctx->shape, ctx->cfg.kv_dtype, v, q, stride_t, cu, n_tokens, held, decay, mass, ctx->part, attn_part_rows(ctx->shape), st));
+  return LFPS_OK;
+}
+
+int lfps_full_attn_mass_decode(lfps_ctx* ctx, const float* q, const lfps_kv* kv, const int32_t* held, float decay, float* mass, float* out,
+                               void* stream) {
+  if (!ctx) return LFPS_EINVAL;
+  if (!q || !mass || !out) return fail(ctx, LFPS_EINVAL, "lfps_full_attn_mass_decode: NULL argument");
+  KvView v;
+  const int rc = check_kv_both(ctx, kv, &v);
+  if (rc != LFPS_OK) return rc;
+  if (!(decay >= 0.f && decay <= 1.f)) return fail(ctx, LFPS_EINVAL, "lfps_full_attn_mass_decode: decay must be in [0, 1]");
+  if ((uintptr_t)q % 16 || (uintptr_t)out % 16 || (uintptr_t)mass % 16)
+    return fail(ctx, LFPS_EINVAL, "lfps_full_attn_mass_decode: q, out and mass must be 16-byte aligned");
+  const Shape& s = ctx->shape;
+  const Span in = {q, 4 * (int64_t)s.B * s.Hq * kD}, row = {out, in.bytes}, sums = mass_span(ctx, mass);
+  if (overlap(in, row) || overlap(in, sums) || overlap(row, sums)) return fail(ctx, LFPS_EINVAL, "lfps_full_attn_mass_decode: q, out and mass overlap");
+  const OnDevice on(ctx->cfg.device);
+  hipStream_t st = (hipStream_t)stream;
+  LAUNCH(ctx, LFPS_KERNEL_FULL_ATTN, st, launch_full_attn(s, ctx->cfg.kv_dtype, q, v, ctx->part, ctx->n_split_full, st));
+  LAUNCH(ctx, LFPS_KERNEL_FULL_MERGE, st, launch_full_merge(s, v.seq_lens, ctx->part, ctx->n_split_full, out, st));
+  LAUNCH(ctx, LFPS_KERNEL_ATTN_MASS, st, launch_attn_mass_decode(s, ctx->cfg.kv_dtype, v, q, held, decay, mass, ctx->part, attn_part_rows(s), st));
+  return LFPS_OK;
+}
+
+int lfps_evict(lfps_ctx* ctx, const lfps_kv* kv, const float* mass, const int32_t* budget, int32_t n_sink, int32_t n_recent, const lfps_kv* to,
+               float* mass_out, int32_t* kept, int32_t* lens_out, void* stream) {
+  if (!ctx) return LFPS_EINVAL;
+  if (!mass || !budget || !mass_out || !kept || !lens_out) return fail(ctx, LFPS_EINVAL, "lfps_evict: NULL argument");
+  KvView v, w;
+  int rc = check_kv_both(ctx, kv, &v);
+  if (rc == LFPS_OK && to) rc = check_kv_both(ctx, to, &w);
+  if (rc != LFPS_OK) return rc;
+  if (n_sink < 0 || n_recent < 0) return fail(ctx, LFPS_EINVAL, "lfps_evict: n_sink and n_recent must be >= 0");
+  if (to && !(v.page.table && w.page.table) && (v.k == w.k || v.v == w.v))
+    return fail(ctx, LFPS_EINVAL, "lfps_evict: rows go to the cache that they come from (in place: to = NULL)");
+  const int64_t B = ctx->shape.B;
+  const Span out[] = {mass_span(ctx, mass_out), mass_span(ctx, kept), {lens_out, 4 * B}};
+  const int64_t entries = v.page.table ? (ctx->shape.Lcap + ((int64_t)1 << v.page.shift) - 1) >> v.page.shift : 0;
+  const Span in[] = {mass_span(ctx, mass), {budget, 4 * B}, {v.seq_lens, 4 * B}, {v.page.table, 4 * ((B - 1) * v.page.table_stride + entries)}};
+  for (const Span& x : out) {
+    for (const Span& y : in)
+      if (overlap(x, y)) return fail(ctx, LFPS_EINVAL, "lfps_evict: an array that is written overlaps one that is read");
+    for (const Span& y : out)
+      if (&x != &y && overlap(x, y)) return fail(ctx, LFPS_EINVAL, "lfps_evict: two arrays that are written overlap");
+  }
+  const OnDevice on(ctx->cfg.device);
+  hipStream_t st = (hipStream_t)stream;
+  LAUNCH(ctx, LFPS_KERNEL_EVICT, st,
+         launch_evict(ctx->shape, ctx->cfg.kv_dtype, v, mass, budget, n_sink, n_recent, to ? &w : nullptr, mass_out, kept, lens_out, st));
   return LFPS_OK;
 }
 

@@ -304,6 +304,27 @@ hipError_t launch_append(const Shape& s, int dtype, const KvView& kv, const void
                          const int32_t* cu, int n_tokens, hipStream_t st);
 hipError_t launch_prompt_attn(const Shape& s, int dtype, const KvView& kv, const void* q, int64_t q_stride, const int32_t* cu,
                               int n_tokens, void* out, float* part, int64_t part_rows, hipStream_t st);
+// Heads normed and turned on their way into the cache; attention over a window and the first rows; accumulated weights, and what they leave of a
+// cache.  See rotate.hip, window_attn.hip, attn_mass.hip and evict.hip.
+struct Rotary {                   // lfps_rotary, checked
+  const float *q_weight, *k_weight;
+  const float* inv_freq;
+  const int32_t* pair_axis;
+  float eps;
+  int32_t rotary_dim, n_axes, interleaved;
+};
+hipError_t launch_rotate_append(const Shape& s, int dtype, const KvView& kv, const Rotary& rot, const void* q, const void* k_new, const void* v_new,
+                                int64_t stride_t, const int32_t* positions, const int32_t* cu, int n_tokens, void* q_out, bool q_f32, hipStream_t st);
+hipError_t launch_window_attn(const Shape& s, int dtype, const KvView& kv, const void* q, int64_t q_stride, const int32_t* cu, int n_tokens, int window,
+                              int n_sink, void* out, float* part, int64_t part_rows, hipStream_t st);
+hipError_t launch_window_attn_decode(const Shape& s, int dtype, const KvView& kv, const float* q, int window, int n_sink, float* out, float* part,
+                                     int64_t part_rows, hipStream_t st);
+hipError_t launch_attn_mass(const Shape& s, int dtype, const KvView& kv, const void* q, int64_t q_stride, const int32_t* cu, int n_tokens,
+                            const int32_t* held, float decay, float* mass, float* part, int64_t part_rows, hipStream_t st);
+hipError_t launch_attn_mass_decode(const Shape& s, int dtype, const KvView& kv, const float* q, const int32_t* held, float decay, float* mass,
+                                   float* part, int64_t part_rows, hipStream_t st);
+hipError_t launch_evict(const Shape& s, int dtype, const KvView& kv, const float* mass, const int32_t* budget, int n_sink, int n_recent, const KvView* to,
+                        float* mass_out, int32_t* kept, int32_t* lens_out, hipStream_t st);
 hipError_t launch_prefix_attn(const Shape& s, int dtype, const KvView& kv, const float* q, const int32_t* group_start,
                               const int32_t* prefix_len, int n_groups, float* out, float* part, int64_t part_rows, hipStream_t st);
 int64_t pages_workspace_bytes(int32_t n_blocks);
