@@ -44,6 +44,33 @@ struct CacheRows {
   }
 };
 
+// ---- the rows that a loop walks --------------------------------------------------------------------------------
+// All of a range, in which a query row sees those below its limit; or a range with a gap: from row `at` of the walk on, it has the cache's rows
+// `by` further up, and a query row does not see the cache's rows [sinks, from) either.  clear: row of the walk from which on no query
+// row of the workgroup misses one for its window.
+struct AllRows {
+  static constexpr bool kGap = false;
+  __device__ __forceinline__ int row(int k) const { return k; }
+  __device__ __forceinline__ int end(int e) const { return e; }
+  __device__ __forceinline__ int steps(int e) const { return e; }
+  __device__ __forceinline__ bool hides(int) const { return false; }
+  // is key `key` of those from row `base` on seen by a query row of this limit?
+  __device__ __forceinline__ auto seen_from(int base, int limit) const {
+    return [seen = limit - base](int key) { return key < seen; };
+  }
+};
+struct GapRows {
+  static constexpr bool kGap = true;
+  int at, by, clear, sinks, from;
+  __device__ __forceinline__ int row(int k) const { return k < at ? k : k + by; }
+  __device__ __forceinline__ int end(int e) const { return e > at ? e + by : e; }      // of the cache's rows, for a walk that ends at e
+  __device__ __forceinline__ int steps(int e) const { return e - by; }                 // and the other way round, e > at + by
+  __device__ __forceinline__ bool hides(int j) const { return j < from && j >= sinks; }
+  __device__ __forceinline__ auto seen_from(int base, int limit) const {
+    return [seen = limit - base, first = sinks - base, begin = from - base](int key) { return key < seen && (key >= begin || key < first); };
+  }
+};
+
 // ---- the elements in LDS and in the matrix instructions ------------------------------------------------------
 // A row in LDS is kRowBytes long, in chunks of 16 bytes; chunk c of row r lies at place c ^ mix(r) of the row.  The LDS has 64 banks of
 // four bytes, which is 16 chunks: sixteen consecutive rows read at one chunk (scores), and four rows at four neighbouring chunks (16-bit
@@ -107,18 +134,20 @@ struct StageFeed {
   struct Places {
     int e[kLoads];
     int64_t off[kLoads];
-    __device__ __forceinline__ void look_up(const CacheRows<T>& c, int k0, int end, int lane) {
+    template <typename Rows = AllRows>
+    __device__ __forceinline__ void look_up(const CacheRows<T>& c, int k0, int end, int lane, const Rows& rows = Rows()) {
       if (!c.pg.table) return;
 #pragma unroll
-      for (int i = 0; i < kLoads; ++i) e[i] = c.entry(min(k0 + row(i, lane), end - 1));
+      for (int i = 0; i < kLoads; ++i) e[i] = c.entry(rows.row(min(k0 + row(i, lane), end - 1)));
     }
-    __device__ __forceinline__ void aim(const CacheRows<T>& c, int k0, int end, int lane) {
+    template <typename Rows = AllRows>
+    __device__ __forceinline__ void aim(const CacheRows<T>& c, int k0, int end, int lane, const Rows& rows = Rows()) {
       if (c.pg.table) {
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i) off[i] = RowMap<true>::offset_in(c.pg, e[i], min(k0 + row(i, lane), end - 1), c.stride_b, c.stride_n);
+        for (int i = 0; i < kLoads; ++i) off[i] = RowMap<true>::offset_in(c.pg, e[i], rows.row(min(k0 + row(i, lane), end - 1)), c.stride_b, c.stride_n);
       } else {
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i) off[i] = (int64_t)min(k0 + row(i, lane), end - 1) * c.stride_n;
+        for (int i = 0; i < kLoads; ++i) off[i] = (int64_t)rows.row(min(k0 + row(i, lane), end - 1)) * c.stride_n;
       }
     }
   };
@@ -237,16 +266,16 @@ __device__ __forceinline__ bool any_not_finite(const lds_char* rows, int bytes) 
   }
   return __ballot(found) != 0;
 }
-// o += weights of `keys` keys (a multiple of 32) times their values at v, key by key on the vector units, of keys below `seen`.
+// o += weights of `keys` keys (a multiple of 32) times their values at v, key by key on the vector units, of keys that the row sees(key).
 // weight(i, half): my weight of the i-th of the keys that that half of the wave holds.  Slow, and small: almost no call comes here.
-template <typename Op, typename Weight>
-__device__ __forceinline__ void add_apart(f32x16 (&o)[4], Weight weight, const lds_char* v, int keys, int seen, int lane) {
+template <typename Op, typename Weight, typename Sees>
+__device__ __forceinline__ void add_apart(f32x16 (&o)[4], Weight weight, const lds_char* v, int keys, Sees sees, int lane) {
   const int h = lane >> 5;
 #pragma unroll 1
   for (int key = 0; key < keys; ++key) {
     const float mine = weight((key >> 3) * 4 + (key & 3)), other = __shfl_xor(mine, 32);
     const float w = h == ((key >> 2) & 1) ? mine : other;
-    if (key >= seen) continue;
+    if (!sees(key)) continue;
 #pragma unroll
     for (int d = 0; d < 4; ++d)
 #pragma unroll
@@ -339,8 +368,8 @@ struct RowState {
 
   // One step of kBlocks * 32 keys: scores s (products) -> weights, sums and values.  first: position of the first key; limit: the
   // keys that row n sees; masked: some row of the wave sees fewer than all of these.
-  template <int kBlocks>
-  __device__ __forceinline__ void step(f32x16 (&s)[kBlocks], const char* v, float unit, int first, int limit, bool masked, int lane) {
+  template <int kBlocks, typename Rows>
+  __device__ __forceinline__ void step(f32x16 (&s)[kBlocks], const char* v, float unit, int first, int limit, bool masked, int lane, const Rows& rows) {
     const int h = lane >> 5;
     float mx = m;
 #pragma unroll
@@ -348,7 +377,8 @@ struct RowState {
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         s[b][r] *= unit;
-        if (masked && first + 32 * b + 8 * (r / 4) + 4 * h + r % 4 >= limit) s[b][r] = -INFINITY;
+        const int j = first + 32 * b + 8 * (r / 4) + 4 * h + r % 4;
+        if (masked && (j >= limit || rows.hides(j))) s[b][r] = -INFINITY;
         mx = fmaxf(mx, s[b][r]);
       }
     mx = fmaxf(mx, __shfl_xor(mx, 32));
@@ -377,7 +407,7 @@ struct RowState {
           for (int r = 0; r < 16; ++r) x = r == i ? s[b][r] : x;
           return x;
         };
-        add_apart<Op>(o, weight, (const lds_char*)vb, 32, limit - first - 32 * b, lane);
+        add_apart<Op>(o, weight, (const lds_char*)vb, 32, rows.seen_from(first + 32 * b, limit), lane);
       } else {
         add_values(s[b], vb, lane);
       }
@@ -447,9 +477,9 @@ constexpr int few_key_waves() { return sizeof(T) == 4 ? 2 : 4; }
 // The loop of a workgroup whose four waves are 4 / kKeyWaves rows of waves (32 query rows each) by kKeyWaves (which share a stage's
 // keys), over the rows [first, end).  load_q: brings my query row's operand, which nothing waits for until the first rows have been
 // asked for.  limit: the keys that my query row sees.
-template <typename TK, typename TV, int kKeyWaves, typename Op, int kTerms, typename LoadQ>
+template <typename TK, typename TV, int kKeyWaves, typename Op, int kTerms, typename LoadQ, typename Rows = AllRows>
 __device__ __forceinline__ void tile_loop(char* lds, const CacheRows<TK>& K, const CacheRows<TV>& V, int first, int end, LoadQ load_q,
-                                          int limit, RowState<Op, kTerms>& st) {
+                                          int limit, RowState<Op, kTerms>& st, const Rows& rows = Rows()) {
   constexpr int kRows = tile_rows(kKeyWaves), kBlocks = kRows / 32 / kKeyWaves;
   constexpr int kStageK = stage_bytes<TK>(kRows), kStage = kStageK + stage_bytes<TV>(kRows);
   const int lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5, mine = (wave_of() % kKeyWaves) * kBlocks * 32;
@@ -461,6 +491,13 @@ __device__ __forceinline__ void tile_loop(char* lds, const CacheRows<TK>& K, con
   }
   most = __builtin_amdgcn_readfirstlane(most);
   least = __builtin_amdgcn_readfirstlane(least);
+  int begun = 0;                              // the row from which on none of my wave's misses one for its window
+  if constexpr (Rows::kGap) {
+    begun = rows.from;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) begun = max(begun, __shfl_xor(begun, d));
+    begun = __builtin_amdgcn_readfirstlane(begun);
+  }
   lds_char* const stages = (lds_char*)lds;
   StageFeed<TK, kRows / 4, Op> fk;
   StageFeed<TV, kRows / 4, Op> fv;
@@ -468,12 +505,12 @@ __device__ __forceinline__ void tile_loop(char* lds, const CacheRows<TK>& K, con
   typename decltype(fv)::Places pv;
   constexpr bool kAlike = sizeof(TK) == sizeof(TV);
   auto look_up = [&](int k) {
-    pk.look_up(K, k, end, lane);
-    if constexpr (!kAlike) pv.look_up(V, k, end, lane);
+    pk.look_up(K, k, end, lane, rows);
+    if constexpr (!kAlike) pv.look_up(V, k, end, lane, rows);
   };
   auto ask = [&](int k, int to) {
-    pk.aim(K, k, end, lane);
-    if constexpr (!kAlike) pv.aim(V, k, end, lane);
+    pk.aim(K, k, end, lane, rows);
+    if constexpr (!kAlike) pv.aim(V, k, end, lane, rows);
     __builtin_amdgcn_sched_barrier(0);
     fk.ask(K, pk.off, stages + to, lane);
     if constexpr (kAlike) fv.ask(V, pk.off, stages + to + kStageK, lane);
@@ -508,10 +545,10 @@ __device__ __forceinline__ void tile_loop(char* lds, const CacheRows<TK>& K, con
     const char* v = lds + at + kStageK + mine * InLds<TV>::kRowBytes;
 #pragma unroll
     for (int b = 0; b < kBlocks; ++b) {
-      const int k_mine = k0 + mine + 32 * b;
+      const int k_mine = rows.row(k0 + mine + 32 * b);
       if (k_mine < most) {
         f32x16 s[1] = {RowState<Op, kTerms>::scores(k + 32 * b * InLds<TK>::kRowBytes, q, n, h)};
-        st.template step<1>(s, v + 32 * b * InLds<TV>::kRowBytes, q.unit, k_mine, limit, k_mine + 32 > least, lane);
+        st.template step<1>(s, v + 32 * b * InLds<TV>::kRowBytes, q.unit, k_mine, limit, k_mine + 32 > least || (Rows::kGap && k_mine < begun), lane, rows);
       }
     }
     if (more) put(kStage - at);

@@ -174,24 +174,28 @@ struct PipeState {
     }
   }
 
-  // The values of a stage key by key, of those below `seen` (see any_not_finite).
-  __device__ __forceinline__ void add_values_apart(const Op (&w)[4], const f32x16 (&s)[2], const lds_char* v, int lane, int seen) {
+  // The values of a stage key by key, of those that the row sees (see any_not_finite).
+  template <typename Sees>
+  __device__ __forceinline__ void add_values_apart(const Op (&w)[4], const f32x16 (&s)[2], const lds_char* v, int lane, Sees sees) {
     auto weight = [&](int i) {                                   // of the 32 that I hold
       float x = 0.f;
 #pragma unroll
       for (int e = 0; e < 32; ++e) x = e == i ? (kTerms == 1 ? (float)w[e / 8][e % 8] : s[e / 16][e % 16]) : x;
       return x;
     };
-    add_apart<Op>(o, weight, v, kPipeKeys, seen, lane);
+    add_apart<Op>(o, weight, v, kPipeKeys, sees, lane);
   }
 
   // Scores of keys that the row does not see.
-  __device__ __forceinline__ void hide(f32x16 (&s)[2], int first, int h) const {
+  template <typename Rows>
+  __device__ __forceinline__ void hide(f32x16 (&s)[2], int first, int h, const Rows& rows) const {
 #pragma unroll
     for (int b = 0; b < 2; ++b)
 #pragma unroll
-      for (int r = 0; r < 16; ++r)
-        if (first + 32 * b + 8 * (r / 4) + 4 * h + r % 4 >= limit) s[b][r] = -INFINITY;
+      for (int r = 0; r < 16; ++r) {
+        const int j = first + 32 * b + 8 * (r / 4) + 4 * h + r % 4;
+        if (j >= limit || rows.hides(j)) s[b][r] = -INFINITY;
+      }
   }
   __device__ __forceinline__ static float largest(const f32x16 (&s)[2]) {
     float mx[4];
@@ -284,16 +288,18 @@ template <typename Op, int kTerms>
 constexpr int pipe_lds() { return PipeState<Op, kTerms>::kRest ? kRestAt + kPipeWaves * kRestWave : kPipeLds; }
 // least: keys that all rows of the workgroup see.
 // active: the wave has rows of its own; one that has none only brings its share of the cache's.
-template <int kKind, typename TK, typename TV, typename Op, int kTerms>
+// rows: the cache's rows that [first, end) stand for (a gap lies between stages).
+template <int kKind, typename TK, typename TV, typename Op, int kTerms, typename Rows = AllRows>
 __device__ __forceinline__ void pipe_loop(char* lds_, const CacheRows<TK>& K, const CacheRows<TV>& V, int first, int end, int least, bool active,
-                                          PipeState<Op, kTerms>& st) {
+                                          PipeState<Op, kTerms>& st, const Rows& rows = Rows()) {
   lds_char* const lds = (lds_char*)lds_;
   const int lane = threadIdx.x & 63, wave = wave_of(), n = lane & 31, h = lane >> 5;
   const bool late = wave >= kPipeWaves / 2;
   Feed<TK, kKind, Op> fk;
   Feed<TV, kKind, Op> fv;
   constexpr int kV = kPipeStages * kPipeStage;
-  auto row_of = [&](int k) { return first_row(k, end, wave); };
+  const int row_end = rows.end(end);
+  auto row_of = [&](int k) { return first_row(rows.row(k), row_end, wave); };
   auto look_up = [&](int k) { return kKind == kPages ? RowMap<true>::block(K.pg, K.b, row_of(k)) : 0; };
   auto uniform = [](int e) { return __builtin_amdgcn_readfirstlane(e); };
   constexpr bool kRest = PipeState<Op, kTerms>::kRest;
@@ -306,11 +312,11 @@ __device__ __forceinline__ void pipe_loop(char* lds_, const CacheRows<TK>& K, co
 #pragma unroll
   for (int i = 0; i < 3; ++i) {                                  // K of the first three stages, V of two
     const int k = first + i * kPipeKeys, e = uniform(e_first[i]);
-    fk.aim(K, row_of(k), end, e, lane);
+    fk.aim(K, row_of(k), row_end, e, lane);
     fk.ask(lds + i * kPipeStage, wave);
     fk.put(lds + i * kPipeStage, lane, wave);
     if (i < 2) {
-      fv.aim(V, row_of(k), end, e, lane);
+      fv.aim(V, row_of(k), row_end, e, lane);
       fv.ask(lds + kV + i * kPipeStage, wave);
       fv.put(lds + kV + i * kPipeStage, lane, wave);
     }
@@ -332,7 +338,7 @@ __device__ __forceinline__ void pipe_loop(char* lds_, const CacheRows<TK>& K, co
     constexpr bool kMasked = decltype(masked)::value, kWorks = decltype(works)::value;
     // vector half
     if constexpr (kWorks) {
-      if (kMasked) st.hide(s, k0, h);
+      if (kMasked) st.hide(s, rows.row(k0), h, rows);
       st.follow(st.largest(s));
       const float at = st.m == -INFINITY ? 0.f : st.m - (PipeState<Op, kTerms>::kLift);
 #pragma unroll
@@ -344,8 +350,8 @@ __device__ __forceinline__ void pipe_loop(char* lds_, const CacheRows<TK>& K, co
       e_v = e_k;
       e_k = e_new;
     }
-    fk.aim(K, row_of(k0 + 3 * kPipeKeys), end, uniform(e_k), lane);
-    fv.aim(V, row_of(k0 + 2 * kPipeKeys), end, uniform(e_v), lane);
+    fk.aim(K, row_of(k0 + 3 * kPipeKeys), row_end, uniform(e_k), lane);
+    fv.aim(V, row_of(k0 + 2 * kPipeKeys), row_end, uniform(e_v), lane);
     landed();
     const lds_char* const v = lds + kV + now;
     const lds_char* const k = lds + next;                        // (of the last stage: what lies there, unused)
@@ -364,7 +370,7 @@ __device__ __forceinline__ void pipe_loop(char* lds_, const CacheRows<TK>& K, co
     // matrix half
     if constexpr (kWorks) {
       if (kMasked && !kRest) apart = *(volatile int*)found == k0 + kPipeKeys;
-      if (apart) st.add_values_apart(w, s, v, lane, st.limit - k0);
+      if (apart) st.add_values_apart(w, s, v, lane, rows.seen_from(rows.row(k0), st.limit));
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         __builtin_amdgcn_sched_barrier(0);
@@ -394,10 +400,14 @@ __device__ __forceinline__ void pipe_loop(char* lds_, const CacheRows<TK>& K, co
   const std::true_type yes;
   const std::false_type no;
   if (active) {
-    while (k0 + kPipeKeys <= least && k0 < end) stage(no, yes);
+    if constexpr (Rows::kGap)
+      while (k0 < rows.clear && k0 < end) stage(yes, yes);
+    while (rows.row(k0) + kPipeKeys <= least && k0 < end) stage(no, yes);
     while (k0 < end) stage(yes, yes);
   } else {
-    while (k0 + kPipeKeys <= least && k0 < end) stage(no, no);
+    if constexpr (Rows::kGap)
+      while (k0 < rows.clear && k0 < end) stage(yes, no);
+    while (rows.row(k0) + kPipeKeys <= least && k0 < end) stage(no, no);
     while (k0 < end) stage(yes, no);
   }
   if (!late) __syncthreads();
