@@ -1108,7 +1108,7 @@ int lfps_window_attn_decode(lfps_ctx* ctx, const float* q, const lfps_kv* kv, in
   const OnDevice on(ctx->cfg.device);
   hipStream_t st = (hipStream_t)stream;
   LAUNCH(ctx, LFPS_KERNEL_WINDOW_ATTN, st,
-         launch_window_attn_decode(ctx->shape, ctx->cfg.kv_dtype, v, q, window, n_sink, out, ctx->part, attn_part_rows(ctx->shape), st));
+         launch_window_attn_decode(ctx->shape, ctx->cfg.kv_dtype, v, q, window, n_sink, out, ctx->part, st));
   return LFPS_OK;
 }
 
@@ -1148,9 +1148,8 @@ int lfps_full_attn_mass_decode(lfps_ctx* ctx, const float* q, const lfps_kv* kv,
   if (overlap(in, row) || overlap(in, sums) || overlap(row, sums)) return fail(ctx, LFPS_EINVAL, "lfps_full_attn_mass_decode: q, out and mass overlap");
   const OnDevice on(ctx->cfg.device);
   hipStream_t st = (hipStream_t)stream;
-  LAUNCH(ctx, LFPS_KERNEL_FULL_ATTN, st, launch_full_attn(s, ctx->cfg.kv_dtype, q, v, ctx->part, ctx->n_split_full, st));
-  LAUNCH(ctx, LFPS_KERNEL_FULL_MERGE, st, launch_full_merge(s, v.seq_lens, ctx->part, ctx->n_split_full, out, st));
-  LAUNCH(ctx, LFPS_KERNEL_ATTN_MASS, st, launch_attn_mass_decode(s, ctx->cfg.kv_dtype, v, q, held, decay, mass, ctx->part, attn_part_rows(s), st));
+  LAUNCH(ctx, LFPS_KERNEL_ATTN_MASS, st,
+         launch_mass_step(s, ctx->cfg.kv_dtype, v, q, held, decay, mass, out, ctx->score, s.score_stride, ctx->part, ctx->n_split_full, st));
   return LFPS_OK;
 }
 

@@ -22,6 +22,7 @@ constexpr int64_t kKeptStreamBytes = 288 << 20;
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x2t __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
@@ -305,7 +306,7 @@ hipError_t launch_append(const Shape& s, int dtype, const KvView& kv, const void
 hipError_t launch_prompt_attn(const Shape& s, int dtype, const KvView& kv, const void* q, int64_t q_stride, const int32_t* cu,
                               int n_tokens, void* out, float* part, int64_t part_rows, hipStream_t st);
 // Heads normed and turned on their way into the cache; attention over a window and the first rows; accumulated weights, and what they leave of a
-// cache.  See rotate.hip, window_attn.hip, attn_mass.hip and evict.hip.
+// cache.  See rotate.hip, window_attn.hip, window_step.hip, attn_mass.hip, mass_step.hip and evict.hip.
 struct Rotary {                   // lfps_rotary, checked
   const float *q_weight, *k_weight;
   const float* inv_freq;
@@ -318,11 +319,11 @@ hipError_t launch_rotate_append(const Shape& s, int dtype, const KvView& kv, con
 hipError_t launch_window_attn(const Shape& s, int dtype, const KvView& kv, const void* q, int64_t q_stride, const int32_t* cu, int n_tokens, int window,
                               int n_sink, void* out, float* part, int64_t part_rows, hipStream_t st);
 hipError_t launch_window_attn_decode(const Shape& s, int dtype, const KvView& kv, const float* q, int window, int n_sink, float* out, float* part,
-                                     int64_t part_rows, hipStream_t st);
+                                     hipStream_t st);
 hipError_t launch_attn_mass(const Shape& s, int dtype, const KvView& kv, const void* q, int64_t q_stride, const int32_t* cu, int n_tokens,
                             const int32_t* held, float decay, float* mass, float* part, int64_t part_rows, hipStream_t st);
-hipError_t launch_attn_mass_decode(const Shape& s, int dtype, const KvView& kv, const float* q, const int32_t* held, float decay, float* mass,
-                                   float* part, int64_t part_rows, hipStream_t st);
+hipError_t launch_mass_step(const Shape& s, int dtype, const KvView& kv, const float* q, const int32_t* held, float decay, float* mass, float* out,
+                            float* score, int64_t score_stride, float* part, int n_split, hipStream_t st);
 hipError_t launch_evict(const Shape& s, int dtype, const KvView& kv, const float* mass, const int32_t* budget, int n_sink, int n_recent, const KvView* to,
                         float* mass_out, int32_t* kept, int32_t* lens_out, hipStream_t st);
 hipError_t launch_prefix_attn(const Shape& s, int dtype, const KvView& kv, const float* q, const int32_t* group_start,

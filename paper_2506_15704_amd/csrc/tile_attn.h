@@ -23,7 +23,6 @@ constexpr float kLog2e = 1.4426950408889634f;
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
-typedef float f32x2t __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2t __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x2t __attribute__((ext_vector_type(2)));
 typedef __attribute__((address_space(3))) char lds_char;
