@@ -13,14 +13,19 @@ namespace lfps {
 
 namespace {
 
-constexpr int kMassThreads = 256, kMassStage = 64;     // keys or query rows of a stage
+constexpr int kMassThreads = 256, kMassWaves = kMassThreads / 64;
+constexpr int kMassRing = 4;                           // stages of streamed rows in LDS
 constexpr float kMassLazy = 6.f;                       // growth of a maximum, in powers of two, that is let pass
+constexpr float kMassUnit = kLog2e * 0.08838834764831845f;      // from products to scores in powers of two
 
-// Blocks of 32 rows that a wave keeps in registers: of 16-bit operands two, so that a row read from LDS serves two products.
+// Blocks of 32 rows that a wave keeps in registers: of 16-bit operands two, so that a row read from LDS serves two products.  A stage of streamed
+// rows is 16 KB.
 template <typename Op>
-constexpr int mass_blocks() { return std::is_same<Op, float>::value ? 1 : 2; }
-template <typename Op>
-constexpr int mass_rows() { return 4 * 32 * mass_blocks<Op>(); }        // of a workgroup
+struct MassShape {
+  static constexpr bool kF32 = std::is_same<Op, float>::value;
+  static constexpr int kBlocks = kF32 ? 1 : 2, kMine = 32 * kBlocks, kRows = kMassWaves * kMine;       // of a wave; of a workgroup
+  static constexpr int kRowBytes = kF32 ? 512 : 256, kStage = kF32 ? 32 : 64, kSubs = kStage / 32, kBytes = kStage * kRowBytes;
+};
 
 template <typename TQ>
 struct MassArgs {
@@ -31,9 +36,11 @@ struct MassArgs {
   const int32_t *cu, *held;
   int32_t n_tokens, t0, t1;        // the tokens of this launch
   float decay;
-  float* stats;                    // [t1 - t0, Hq, splits, 2] of a query row: its largest score in powers of two, the sum of the weights from there; whole
-                                   // rows (one split): the sum's inverse
+  float* stats;                    // [Hkv, t1 - t0, G, 2] of a query row: its largest score in powers of two, the inverse of the sum of the weights from there
+  float* split_stats;              // [splits, Hkv, t1 - t0, G, 2] of its parts, if there are several: the sums themselves
   int32_t splits;
+  int32_t chunk;                   // query rows of a request that a workgroup of k_mass_add takes
+  float* sums;                     // [chunks, B * Hkv, Lcap] what they leave, if there are several
   float* mass;
 };
 
@@ -41,54 +48,76 @@ struct MassArgs {
 template <typename Op>
 struct MassRow {
   Op x[8];
+  __device__ __forceinline__ static Op chunk(const lds_char* rows, int c, int n, int h) {
+    return *(const __attribute__((address_space(3))) Op*)(rows + n * 256 + 16 * chunk_place(n, 2 * c + h));
+  }
   template <typename T>
   __device__ __forceinline__ void load(const T* p, int h) {
 #pragma unroll
-    for (int s = 0; s < 8; ++s) {
-      if constexpr (sizeof(T) == 1) {
-        const u32x2 w = *reinterpret_cast<const u32x2*>(p + 16 * s + 8 * h);
-        x[s] = fp8x8_to<Op>(w[0], w[1]);
-      } else {
-        x[s] = *reinterpret_cast<const Op*>(p + 16 * s + 8 * h);
-      }
-    }
+    for (int c = 0; c < 8; ++c) x[c] = *reinterpret_cast<const Op*>(p + 16 * c + 8 * h);
+  }
+  __device__ __forceinline__ void load(const lds_char* rows, int n, int h) {
+#pragma unroll
+    for (int c = 0; c < 8; ++c) x[c] = chunk(rows, c, n, h);
   }
 };
 template <>
 struct MassRow<float> {
   f32x4 x[16];
+  __device__ __forceinline__ static f32x4 chunk(const lds_char* rows, int c, int n, int h) {
+    return *(const __attribute__((address_space(3))) f32x4*)(rows + n * 512 + 16 * chunk_place_f32(n, 2 * c + h));
+  }
   __device__ __forceinline__ void load(const float* p, int h) {
 #pragma unroll
-    for (int s = 0; s < 16; ++s) x[s] = *reinterpret_cast<const f32x4*>(p + 8 * s + 4 * h);
+    for (int c = 0; c < 16; ++c) x[c] = *reinterpret_cast<const f32x4*>(p + 8 * c + 4 * h);
+  }
+  __device__ __forceinline__ void load(const lds_char* rows, int n, int h) {
+#pragma unroll
+    for (int c = 0; c < 16; ++c) x[c] = chunk(rows, c, n, h);
   }
 };
 
-// out[i] = 32 rows in LDS times my block i, or with kLdsIsKeys = false my blocks times the rows in LDS (keys are the first operand).
-template <bool kLdsIsKeys, typename Op, int kBlocks>
-__device__ __forceinline__ void mass_scores(f32x16 (&out)[kBlocks], const lds_char* rows, const MassRow<Op> (&mine)[kBlocks], int n, int h) {
-#pragma unroll
-  for (int i = 0; i < kBlocks; ++i) out[i] = zeros16();
+// out[i] = 32 rows in LDS times my block i, or with kLdsIsKeys = false my blocks times the rows in LDS (keys are the first operand), and beside the
+// products, in eight pieces, beside(0) .. beside(7): vector instructions that do not wait for them.  (Left to itself the compiler puts all products
+// first, and reads their operands one product ahead.)
+template <bool kLdsIsKeys, typename Op, int kBlocks, typename Beside>
+__device__ __forceinline__ void mass_scores(f32x16 (&out)[kBlocks], const lds_char* rows, const MassRow<Op> (&mine)[kBlocks], int n, int h, Beside beside) {
   if constexpr (std::is_same<Op, float>::value) {
+    f32x4 a[3] = {MassRow<float>::chunk(rows, 0, n, h), MassRow<float>::chunk(rows, 1, n, h)};
 #pragma unroll
     for (int c = 0; c < 16; ++c) {
-      const f32x4 a = *(const __attribute__((address_space(3))) f32x4*)(rows + n * 512 + 16 * chunk_place_f32(n, 2 * c + h));
+      __builtin_amdgcn_sched_barrier(0);
+      if (c + 2 < 16) a[(c + 2) % 3] = MassRow<float>::chunk(rows, c + 2, n, h);
 #pragma unroll
       for (int e = 0; e < 4; ++e)
 #pragma unroll
-        for (int i = 0; i < kBlocks; ++i)
-          out[i] = kLdsIsKeys ? mfma32(a[e], mine[i].x[c][e], out[i]) : mfma32(mine[i].x[c][e], a[e], out[i]);
+        for (int i = 0; i < kBlocks; ++i) {
+          const f32x16 before = c + e == 0 ? zeros16() : out[i];
+          out[i] = kLdsIsKeys ? mfma32(a[c % 3][e], mine[i].x[c][e], before) : mfma32(mine[i].x[c][e], a[c % 3][e], before);
+        }
+      if (c % 2) beside(c / 2);
     }
   } else {
+    Op a[3] = {MassRow<Op>::chunk(rows, 0, n, h), MassRow<Op>::chunk(rows, 1, n, h)};
 #pragma unroll
     for (int c = 0; c < 8; ++c) {
-      const Op a = *(const __attribute__((address_space(3))) Op*)(rows + n * 256 + 16 * chunk_place(n, 2 * c + h));
+      __builtin_amdgcn_sched_barrier(0);
+      if (c + 2 < 8) a[(c + 2) % 3] = MassRow<Op>::chunk(rows, c + 2, n, h);
 #pragma unroll
-      for (int i = 0; i < kBlocks; ++i) out[i] = kLdsIsKeys ? mfma32(a, mine[i].x[c], out[i]) : mfma32(mine[i].x[c], a, out[i]);
+      for (int i = 0; i < kBlocks; ++i) {
+        const f32x16 before = c == 0 ? zeros16() : out[i];
+        out[i] = kLdsIsKeys ? mfma32(a[c % 3], mine[i].x[c], before) : mfma32(mine[i].x[c], a[c % 3], before);
+      }
+      beside(c);
     }
   }
+  __builtin_amdgcn_sched_barrier(0);
 }
 
-constexpr float kMassUnit = kLog2e * 0.08838834764831845f;      // from products to scores in powers of two
+// All but the newest kNewer requests to memory of this wave have been answered.
+template <int kNewer>
+__device__ __forceinline__ void answered_but() { __builtin_amdgcn_s_waitcnt(0x0f70 | (kNewer & 15) | (kNewer >> 4 << 14)); }
+
 // The key of a lane's product r among 32.
 __device__ __forceinline__ int key_of(int r, int h) { return 8 * (r / 4) + 4 * h + r % 4; }
 
@@ -104,14 +133,18 @@ __device__ __forceinline__ int launch_tokens(const A& a, int b, int* c0, int* c1
 
 }  // namespace
 
-// grid Hkv * splits * tiles (of mass_rows query rows; at most T G / rows + B), the latest rows first: they see most
+// grid Hkv * splits * tiles (of kRows query rows; at most T G / rows + B), the latest rows first: they see most.
+// Stage j of keys is in LDS slot j % 4.  While a wave's weights of 32 keys are made, the products of the next 32 run; when the last 32 of stage j - 1
+// are, a barrier says that nobody reads its slot any more and that stage j is there, and stage j + 3 is asked for (FP8: comes from registers, and
+// j + 4 is asked for).
 template <typename TK, typename TQ>
 __global__ __launch_bounds__(kMassThreads, sizeof(TK) == 4 ? 1 : 2) void k_mass_stats(MassArgs<TQ> a, int tiles) {
   typedef typename InLds<TQ>::Op Op;
-  constexpr int kBlocks = mass_blocks<Op>(), kRows = mass_rows<Op>(), kBytes = kMassStage * InLds<TQ>::kRowBytes;
-  __shared__ __attribute__((aligned(16))) char lds_[2 * kBytes];
+  typedef MassShape<Op> M;
+  constexpr int kBlocks = M::kBlocks;
+  __shared__ __attribute__((aligned(16))) char lds_[kMassRing * M::kBytes];
   const Shape& s = a.s;
-  const int G = s.G, shift = G == 4 ? 2 : G - 1, per = kRows / G;
+  const int G = s.G, shift = G == 4 ? 2 : G - 1, per = M::kRows / G;
   const int g = blockIdx.x % s.Hkv, x0 = blockIdx.x / s.Hkv, split = x0 % a.splits, x = tiles - 1 - x0 / a.splits;
   auto first_tile = [&](int i) {
     const int c = a.cu[i];
@@ -120,26 +153,26 @@ __global__ __launch_bounds__(kMassThreads, sizeof(TK) == 4 ? 1 : 2) void k_mass_
   const int b = last_not_above(s.B - 1, x, first_tile);
   int c0, c1;
   const int first = launch_tokens(a, b, &c0, &c1);
-  const int row0 = (x - first_tile(b)) * kRows, rows = c1 > c0 ? (c1 - c0) << shift : 0;
+  const int row0 = (x - first_tile(b)) * M::kRows, rows = c1 > c0 ? (c1 - c0) << shift : 0;
   if (row0 < 0 || row0 >= rows) return;
   const int lane = threadIdx.x & 63, wave = wave_of(), n = lane & 31, h = lane >> 5;
   auto seen = [&](int m) {                                     // keys that query row m sees
     const int y = first + c0 + (m >> shift) + 1;
     return y < 0 ? 0 : y;
   };
-  const int last = (row0 + kRows < rows ? row0 + kRows : rows) - 1;
+  const int last = (row0 + M::kRows < rows ? row0 + M::kRows : rows) - 1;
   int lo, hi;
-  split_rows(0, seen(last), a.splits, split, kMassStage, &lo, &hi);
-  const int mine0 = row0 + 32 * kBlocks * wave;
+  split_rows(0, seen(last), a.splits, split, M::kStage, &lo, &hi);
+  const int mine0 = row0 + M::kMine * wave;
   int m[kBlocks], limit[kBlocks];
-  MassRow<Op> q[kBlocks];
 #pragma unroll
   for (int i = 0; i < kBlocks; ++i) {
     m[i] = mine0 + 32 * i + n;
     limit[i] = m[i] < rows ? seen(m[i]) : 0;
+    limit[i] = limit[i] < hi ? limit[i] : hi;
   }
-  const int least = mine0 + 32 * kBlocks <= rows ? seen(mine0) : 0;      // keys that all of my rows see, and that any does
-  const int most = mine0 < rows ? seen(mine0 + 32 * kBlocks - 1 < last ? mine0 + 32 * kBlocks - 1 : last) : 0;
+  int least = mine0 + M::kMine <= rows ? seen(mine0) : 0;      // keys that all of my rows see
+  least = least < hi ? least : hi;
   float top[kBlocks], l[kBlocks][4];
 #pragma unroll
   for (int i = 0; i < kBlocks; ++i) {
@@ -150,59 +183,89 @@ __global__ __launch_bounds__(kMassThreads, sizeof(TK) == 4 ? 1 : 2) void k_mass_
   if (lo < hi) {
     lds_char* const lds = (lds_char*)lds_;
     const CacheRows<TK> K(a.kv.k, a.kv, b, g);
-    StageFeed<TK, kMassStage / 4, Op> feed;
-    typename decltype(feed)::Places at;
+    typedef StageFeed<TK, M::kStage / kMassWaves, Op> Feed;
+    Feed feed;
+    typename Feed::Places at;
+    const int stages = (hi - lo + M::kStage - 1) / M::kStage;
+    auto slot = [&](int j) { return lds + (j & (kMassRing - 1)) * M::kBytes; };
+    auto row_of = [&](int j) { return lo + j * M::kStage; };
+    // stage j, whose places have been looked up; then the look-up of the next one comes first, so that waiting for it is no wait for the rows
+    auto ask = [&](int j) {
+      at.aim(K, row_of(j), hi, lane);
+      __builtin_amdgcn_sched_barrier(0);
+      if (j + 1 < stages) at.look_up(K, row_of(j + 1), hi, lane);
+      __builtin_amdgcn_sched_barrier(0);
+      feed.ask(K, at.off, slot(j), lane);
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    constexpr int kAhead = kMassRing - 1;                      // stages that are on their way
     at.look_up(K, lo, hi, lane);
-    at.aim(K, lo, hi, lane);
-    feed.ask(K, at.off, lds, lane);
-    if (lo + kMassStage < hi) at.look_up(K, lo + kMassStage, hi, lane);
+    for (int j = 0; j <= kAhead && j < stages; ++j) {
+      ask(j);
+      if (j < kAhead) feed.put(slot(j), lane);                 // (FP8: the last one stays in registers)
+    }
+    MassRow<Op> q[kBlocks];
 #pragma unroll
     for (int i = 0; i < kBlocks; ++i) {
       const int token = c0 + ((m[i] < rows ? m[i] : rows - 1) >> shift);
       q[i].load(a.q + (int64_t)token * a.q_stride + (g * G + (m[i] & (G - 1))) * kD, h);
     }
-    feed.put(lds, lane);
-    int now = 0;
-    for (int k0 = lo; k0 < hi; k0 += kMassStage, now = kBytes - now) {
-      const bool more = k0 + kMassStage < hi;
-      __builtin_amdgcn_s_waitcnt(0x0f70);                      // vmcnt(0)
-      __syncthreads();                                         // what all asked for is there; nobody reads the other stage any more
-      if (more) {
-        at.aim(K, k0 + kMassStage, hi, lane);
-        feed.ask(K, at.off, lds + kBytes - now, lane);
-        if (k0 + 2 * kMassStage < hi) at.look_up(K, k0 + 2 * kMassStage, hi, lane);
+    answered_but<0>();
+    __syncthreads();
+    const int subs = (hi - lo + 31) / 32;
+    // between the products of the keys 32 i .. and those of the next: where these begin a stage j, stage j - 1 has been read
+    auto turn = [&](int i) __attribute__((always_inline)) {
+      if ((i + 1) % M::kSubs != 0 || i + 1 >= subs) return;
+      const int j = (i + 1) / M::kSubs;
+      if (Feed::kDirect && j + 2 < stages) answered_but<2 * Feed::kLoads>();
+      else if (Feed::kDirect) answered_but<0>();
+      __syncthreads();
+      if (!Feed::kDirect && j + kAhead - 1 < stages) feed.put(slot(j + kAhead - 1), lane);
+      if (j + kAhead < stages) ask(j + kAhead);
+    };
+    // the weights of the keys 32 i .. of the walk, from y, beside the products of the next 32, to next
+    auto step = [&](int i, f32x16 (&y)[kBlocks], f32x16 (&next)[kBlocks]) __attribute__((always_inline)) {
+      const int key0 = lo + 32 * i;
+      if (key0 + 32 > least) {                                 // (some of my rows do not see all of them)
+#pragma unroll
+        for (int c = 0; c < kBlocks; ++c)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) y[c][r] = key0 + key_of(r, h) < limit[c] ? y[c][r] : -INFINITY;
       }
+      turn(i);
+      float from[kBlocks];
+      auto weigh = [&](int c) __attribute__((always_inline)) {
+        if (c < kBlocks) {                                     // (block c's new maximum)
+          float mx = fmaxf(y[c][0], y[c][1]);
 #pragma unroll
-      for (int kb = 0; kb < kMassStage / 32; ++kb) {
-        const int key0 = k0 + 32 * kb;
-        if (key0 < most) {
-          f32x16 y[kBlocks];
-          mass_scores<true, Op, kBlocks>(y, lds + now + 32 * kb * InLds<TQ>::kRowBytes, q, n, h);
+          for (int r = 2; r < 16; r += 2) mx = fmaxf(fmaxf(mx, y[c][r]), y[c][r + 1]);
+          mx *= kMassUnit;
+          const bool grows = mx > top[c] + kMassLazy;
+          const float shrink = grows ? __builtin_amdgcn_exp2f(top[c] - mx) : 1.f;      // (0 on the first keys)
+          top[c] = grows ? mx : top[c];
+          from[c] = top[c] == -INFINITY ? 0.f : top[c];
 #pragma unroll
-          for (int i = 0; i < kBlocks; ++i) {
-            if (key0 + 32 > least || key0 + 32 > hi) {
-              const int end = limit[i] < hi ? limit[i] : hi;
+          for (int e = 0; e < 4; ++e) l[c][e] *= shrink;
+        } else {
+          constexpr int kAll = 16 * kBlocks, kPieces = 8 - kBlocks;
 #pragma unroll
-              for (int r = 0; r < 16; ++r) y[i][r] = key0 + key_of(r, h) < end ? y[i][r] : -INFINITY;
-            }
-            float mx = fmaxf(y[i][0], y[i][1]);
-#pragma unroll
-            for (int r = 2; r < 16; r += 2) mx = fmaxf(fmaxf(mx, y[i][r]), y[i][r + 1]);
-            mx *= kMassUnit;
-            const float now_top = mx > top[i] + kMassLazy ? mx : top[i];
-            if (__ballot(now_top != top[i])) {
-              const float shrink = now_top == top[i] ? 1.f : __builtin_amdgcn_exp2f(top[i] - now_top);
-#pragma unroll
-              for (int e = 0; e < 4; ++e) l[i][e] *= shrink;
-              top[i] = now_top;
-            }
-            const float from = top[i] == -INFINITY ? 0.f : top[i];
-#pragma unroll
-            for (int r = 0; r < 16; ++r) l[i][r % 4] += __builtin_amdgcn_exp2f(fmaf(y[i][r], kMassUnit, -from));
-          }
+          for (int e = kAll * (c - kBlocks) / kPieces; e < kAll * (c - kBlocks + 1) / kPieces; ++e)
+            l[e / 16][e % 4] += __builtin_amdgcn_exp2f(fmaf(y[e / 16][e % 16], kMassUnit, -from[e / 16]));
         }
+      };
+      const lds_char* const keys = slot((i + 1) / M::kSubs) + (i + 1) % M::kSubs * (32 * M::kRowBytes);
+      mass_scores<true, Op, kBlocks>(next, keys, q, n, h, weigh);       // (behind the last keys: what lies there, unused)
+    };
+    if (mine0 < rows) {
+      f32x16 even[kBlocks], odd[kBlocks];
+      mass_scores<true, Op, kBlocks>(even, slot(0), q, n, h, [](int) {});
+      for (int i = 0; i < subs; i += 2) {
+        step(i, even, odd);
+        if (i + 1 >= subs) break;
+        step(i + 1, odd, even);
       }
-      if (more) feed.put(lds + kBytes - now, lane);
+    } else {                                                   // (a wave without rows only brings its share of the keys)
+      for (int i = 0; i < subs; ++i) turn(i);
     }
   }
 #pragma unroll
@@ -213,158 +276,240 @@ __global__ __launch_bounds__(kMassThreads, sizeof(TK) == 4 ? 1 : 2) void k_mass_
     auto part = [&](float t, float y) { return y != y ? y : (t == -INFINITY ? 0.f : y * __builtin_amdgcn_exp2f(t - mx)); };
     const float both = part(top[i], sum) + part(other_top, other);
     if (h == 0 && m[i] < rows) {
-      float* const to = a.stats + (((int64_t)(c0 - a.t0 + (m[i] >> shift)) * s.Hq + g * G + (m[i] & (G - 1))) * a.splits + split) * 2;
-      const bool whole = a.splits == 1;
-      *reinterpret_cast<f32x2t*>(to) = f32x2t{whole && mx == -INFINITY ? 0.f : mx, whole ? (both == 0.f ? 0.f : 1.f / both) : both};
+      const int64_t count = a.t1 - a.t0, row = (g * count + (c0 - a.t0)) * G + m[i];
+      if (a.splits > 1) *reinterpret_cast<f32x2t*>(a.split_stats + 2 * (split * count * s.Hq + row)) = f32x2t{mx, both};
+      else *reinterpret_cast<f32x2t*>(a.stats + 2 * row) = f32x2t{mx == -INFINITY ? 0.f : mx, both == 0.f ? 0.f : 1.f / both};
     }
   }
 }
 
-// The parts of a query row -> its first part's place, as of one part.
-__global__ __launch_bounds__(256) void k_mass_join(float* __restrict__ stats, int64_t rows, int splits) {
-  const int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (x >= rows) return;
-  const f32x2t* const part = reinterpret_cast<const f32x2t*>(stats) + x * splits;
-  float mx = -INFINITY, sum = 0.f;
-  for (int i = 0; i < splits; ++i) mx = fmaxf(mx, part[i][0]);
-  for (int i = 0; i < splits; ++i) {
-    const float y = part[i][1];
-    sum += y != y ? y : (part[i][0] == -INFINITY ? 0.f : y * __builtin_amdgcn_exp2f(part[i][0] - mx));
+// The parts of every query row, joined: 16 rows a workgroup, 16 threads a row.
+__global__ __launch_bounds__(256) void k_mass_join(const float* __restrict__ split_stats, float* __restrict__ stats, int64_t rows, int splits) {
+  __shared__ f32x2t half[4][16];
+  const int64_t row = (int64_t)blockIdx.x * 16 + (threadIdx.x & 15), at = row < rows ? row : rows - 1;
+  constexpr int kEach = kMaxSplits / 16;
+  const f32x2t* const part = reinterpret_cast<const f32x2t*>(split_stats) + at;
+  f32x2t x[kEach];
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) {
+    const int p = (int)(threadIdx.x >> 4) + 16 * i;
+    x[i] = part[(p < splits ? p : 0) * rows];
+    if (p >= splits) x[i] = f32x2t{-INFINITY, 0.f};
   }
-  *reinterpret_cast<f32x2t*>(stats + x * splits * 2) = f32x2t{mx == -INFINITY ? 0.f : mx, sum == 0.f ? 0.f : 1.f / sum};
+  float mx = -INFINITY, sum = 0.f;
+  auto scaled = [&](f32x2t y) { return y[1] != y[1] ? y[1] : (y[0] == -INFINITY ? 0.f : y[1] * __builtin_amdgcn_exp2f(y[0] - mx)); };
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) mx = fmaxf(mx, x[i][0]);
+  mx = fmaxf(mx, __shfl_xor(mx, 16));
+  mx = fmaxf(mx, __shfl_xor(mx, 32));
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) sum += scaled(x[i]);
+  sum += __shfl_xor(sum, 16);
+  sum += __shfl_xor(sum, 32);
+  if ((threadIdx.x & 63) < 16) half[threadIdx.x >> 6][threadIdx.x & 15] = f32x2t{mx, sum};
+  __syncthreads();
+  if (threadIdx.x >= 16 || row >= rows) return;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) mx = fmaxf(mx, half[w][threadIdx.x][0]);
+  sum = 0.f;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) sum += scaled(half[w][threadIdx.x]);
+  reinterpret_cast<f32x2t*>(stats)[row] = f32x2t{mx == -INFINITY ? 0.f : mx, sum == 0.f ? 0.f : 1.f / sum};
 }
 
-// grid (tiles of mass_rows keys, B * Hkv): the first ones are seen by most
+// grid (tiles of kRows keys, B * Hkv, chunks of query rows): the first keys are seen by most.
+// A wave's keys come through the ring's slot of its number into registers; then the query rows stream through it as the keys do in k_mass_stats.
 template <typename TK, typename TQ>
 __global__ __launch_bounds__(kMassThreads, sizeof(TK) == 4 ? 1 : 2) void k_mass_add(MassArgs<TQ> a) {
   typedef typename InLds<TQ>::Op Op;
-  constexpr int kBlocks = mass_blocks<Op>(), kKeys = mass_rows<Op>(), kRowBytes = InLds<TQ>::kRowBytes, kBytes = kMassStage * kRowBytes;
-  __shared__ __attribute__((aligned(16))) char lds_[2 * kBytes];
-  __shared__ float sums[4][32 * kBlocks];
+  typedef MassShape<Op> M;
+  constexpr int kBlocks = M::kBlocks, kBytes = M::kBytes + M::kStage * 8;      // (with the rows' statistics)
+  static_assert(kMassWaves == kMassRing && M::kMine * M::kRowBytes == M::kBytes, "a slot is a wave's keys");
+  __shared__ __attribute__((aligned(16))) char lds_[kMassRing * kBytes];       // (one array: of several the compiler waits for all requests before any read)
   const Shape& s = a.s;
   const int G = s.G, shift = G == 4 ? 2 : G - 1;
-  const int bg = blockIdx.y, b = bg / s.Hkv, g = bg % s.Hkv, tile = blockIdx.x * kKeys, len = length_of(s, a.kv.seq_lens, b);
+  const int bg = blockIdx.y, b = bg / s.Hkv, g = bg % s.Hkv, tile = blockIdx.x * M::kRows, len = length_of(s, a.kv.seq_lens, b);
   if (tile >= len) return;
   const int lane = threadIdx.x & 63, wave = wave_of(), n = lane & 31, h = lane >> 5;
   int c0, c1;
   const int first = launch_tokens(a, b, &c0, &c1);
-  const int rows = c1 > c0 ? (c1 - c0) << shift : 0;
+  const int all = c1 > c0 ? (c1 - c0) << shift : 0, chunk0 = (int)blockIdx.z * a.chunk;
+  const int rows = all - chunk0 < a.chunk ? all : chunk0 + a.chunk;
   int from = tile - (first + c0);                              // the first token that sees a key of the tile
   from = from < 0 ? 0 : from;
-  const int key0 = tile + 32 * kBlocks * wave;
+  const int key0 = tile + M::kMine * wave;
   float sum[kBlocks][16];
 #pragma unroll
   for (int i = 0; i < kBlocks; ++i)
 #pragma unroll
     for (int r = 0; r < 16; ++r) sum[i][r] = 0.f;
-  const int m0 = (from << shift) & ~(kMassStage - 1);
+  lds_char* const lds = (lds_char*)lds_;
+  int m0 = (from << shift) & ~(M::kStage - 1);
+  m0 = m0 < chunk0 ? chunk0 : m0;
   if (m0 < rows) {
-    lds_char* const lds = (lds_char*)lds_;
-    // a stage of query rows: 1 KB an instruction, lane l fills the l-th 16 bytes of it with the chunk that belongs there
-    constexpr int kPieces = kRowBytes / 16, kEach = 64 / kPieces, kLoads = kMassStage / 4 / kEach;
-    auto ask = [&](int m, lds_char* stage) {
+    auto slot = [&](int j) { return lds + (j & (kMassRing - 1)) * kBytes; };
+    MassRow<Op> k[kBlocks];
+    {
+      const CacheRows<TK> K(a.kv.k, a.kv, b, g);
+      typedef StageFeed<TK, M::kMine, Op> Feed;                // (as many rows as a wave's: "stage" rows kMine * wave .. are my own keys)
+      Feed feed;
+      typename Feed::Places at;
+      at.look_up(K, tile, len, lane);
+      at.aim(K, tile, len, lane);
+      lds_char* const mine = slot(wave) - wave * M::kBytes;    // (the feed adds its own rows' places)
+      feed.ask(K, at.off, mine, lane);
+      feed.put(mine, lane);
+      wave_lds_order();
+      __builtin_amdgcn_s_waitcnt(0x0070);                      // vmcnt(0) lgkmcnt(0)
+      wave_lds_order();
+#pragma unroll
+      for (int i = 0; i < kBlocks; ++i) k[i].load(slot(wave) + 32 * i * M::kRowBytes, n, h);
+      __builtin_amdgcn_s_waitcnt(0xc07f);                      // lgkmcnt(0)
+      __syncthreads();
+    }
+    // a stage of query rows: 1 KB an instruction, lane l fills the l-th 16 bytes of it with the chunk that belongs there; and their statistics, 4
+    // bytes a lane
+    constexpr int kPieces = M::kRowBytes / 16, kEach = 64 / kPieces, kWaveRows = M::kStage / kMassWaves, kLoads = kWaveRows / kEach;
+    const int stages = (rows - m0 + M::kStage - 1) / M::kStage;
+    const float* const stats = a.stats + 2 * (((int64_t)g * (a.t1 - a.t0) + (c0 - a.t0)) * G);
+    auto ask = [&](int j) {
+      lds_char* const to = slot(j);
+      const int r0 = m0 + j * M::kStage + kWaveRows * wave;
 #pragma unroll
       for (int i = 0; i < kLoads; ++i) {
-        const int r = kMassStage / 4 * wave + kEach * i + lane / kPieces, place = lane % kPieces;
-        const int row = m + r < rows ? m + r : rows - 1;
+        const int r = kWaveRows * wave + kEach * i + lane / kPieces, place = lane % kPieces;
+        const int row = r0 + kEach * i + lane / kPieces < rows ? r0 + kEach * i + lane / kPieces : rows - 1;
         const char* const p = reinterpret_cast<const char*>(a.q + (int64_t)(c0 + (row >> shift)) * a.q_stride + (g * G + (row & (G - 1))) * kD) +
-                              16 * (sizeof(TQ) == 4 ? chunk_place_f32(r, place) : chunk_place(r, place));
+                              16 * (M::kF32 ? chunk_place_f32(r, place) : chunk_place(r, place));
         __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) char*)p,
-                                         (__attribute__((address_space(3))) void*)(stage + (kMassStage / 4 * wave + kEach * i) * kRowBytes), 16, 0, 0);
+                                         (__attribute__((address_space(3))) void*)(to + (kWaveRows * wave + kEach * i) * M::kRowBytes), 16, 0, 0);
       }
+      const int row = r0 + lane / 2 < rows ? r0 + lane / 2 : rows - 1;
+      if (lane < 2 * kWaveRows)
+        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) char*)(stats + 2 * (int64_t)row + (lane & 1)),
+                                         (__attribute__((address_space(3))) void*)(to + M::kBytes + kWaveRows * wave * 8), 4, 0, 0);
     };
-    constexpr int kSubs = kMassStage / 32;
-    f32x2t st[kSubs], next[kSubs];                             // of my query rows of a stage
-    auto stats = [&](int m, f32x2t (&to)[kSubs]) {
-#pragma unroll
-      for (int i = 0; i < kSubs; ++i) {
-        const int row = m + 32 * i + n < rows ? m + 32 * i + n : rows - 1;
-        to[i] = *reinterpret_cast<const f32x2t*>(a.stats + ((int64_t)(c0 - a.t0 + (row >> shift)) * s.Hq + g * G + (row & (G - 1))) * a.splits * 2);
-      }
-    };
-    ask(m0, lds);
-    stats(m0, next);
-    const CacheRows<TK> K(a.kv.k, a.kv, b, g);
-    MassRow<Op> k[kBlocks];
-#pragma unroll
-    for (int i = 0; i < kBlocks; ++i) {
-      const int row = key0 + 32 * i + n < len ? key0 + 32 * i + n : len - 1;
-      k[i].load(K.at(row, K.entry(row)), h);
-    }
-    int now = 0;
-    for (int m = m0; m < rows; m += kMassStage, now = kBytes - now) {
-      __builtin_amdgcn_s_waitcnt(0x0f70);                      // vmcnt(0)
+    constexpr int kRequests = kLoads + 1;
+    for (int j = 0; j < kMassRing && j < stages; ++j) ask(j);
+    answered_but<0>();
+    __syncthreads();
+    const int subs = (rows - m0 + 31) / 32;
+    auto turn = [&](int i) __attribute__((always_inline)) {      // as in k_mass_stats; of stage j - 1 the statistics have been read too
+      if ((i + 1) % M::kSubs != 0 || i + 1 >= subs) return;
+      const int j = (i + 1) / M::kSubs;
+      if (j + 2 < stages) answered_but<2 * kRequests>();
+      else answered_but<0>();
+      __builtin_amdgcn_s_waitcnt(0xc07f);                      // lgkmcnt(0)
       __syncthreads();
+      if (j + kMassRing - 1 < stages) ask(j + kMassRing - 1);
+    };
+    auto step = [&](int i, f32x16 (&y)[kBlocks], f32x16 (&next)[kBlocks]) __attribute__((always_inline)) {
+      f32x2t st = *(const __attribute__((address_space(3))) f32x2t*)(slot(i / M::kSubs) + M::kBytes + 8 * (i % M::kSubs * 32 + n));
+      const int mi = m0 + 32 * i;
+      if (mi + 32 > rows || first + c0 + (mi >> shift) < key0 + M::kMine - 1) {      // not all of these queries see all of my keys: the weights here
+        const int pos = mi + n < rows ? first + c0 + ((mi + n) >> shift) - key0 : -1;
 #pragma unroll
-      for (int i = 0; i < kSubs; ++i) st[i] = next[i];
-      if (m + kMassStage < rows) {
-        ask(m + kMassStage, lds + kBytes - now);
-        stats(m + kMassStage, next);
-      }
-      if (key0 >= len) continue;
-#pragma unroll
-      for (int i = 0; i < kSubs; ++i) {
-        const int mi = m + 32 * i;
-        const int pos = mi + n < rows ? first + c0 + ((mi + n) >> shift) : -1;      // my query's row
-        const int most = first + c0 + ((mi + 31 < rows ? mi + 31 : rows - 1) >> shift);
-        if (mi >= rows || most < key0) continue;
-        f32x16 y[kBlocks];
-        mass_scores<false, Op, kBlocks>(y, lds + now + 32 * i * kRowBytes, k, n, h);
-        if (mi + 32 <= rows && first + c0 + (mi >> shift) >= key0 + 32 * kBlocks - 1) {
-#pragma unroll
-          for (int kb = 0; kb < kBlocks; ++kb)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) sum[kb][r] = fmaf(__builtin_amdgcn_exp2f(fmaf(y[kb][r], kMassUnit, -st[i][0])), st[i][1], sum[kb][r]);
-        } else {
-#pragma unroll
-          for (int kb = 0; kb < kBlocks; ++kb)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-              const float e = __builtin_amdgcn_exp2f(fmaf(y[kb][r], kMassUnit, -st[i][0])) * st[i][1];
-              sum[kb][r] += key0 + 32 * kb + key_of(r, h) <= pos ? e : 0.f;
-            }
+        for (int e = 0; e < 16 * kBlocks; ++e) {
+          const float w = __builtin_amdgcn_exp2f(fmaf(y[e / 16][e % 16], kMassUnit, -st[0])) * st[1];
+          sum[e / 16][e % 16] += 32 * (e / 16) + key_of(e % 16, h) <= pos ? w : 0.f;
+          y[e / 16][e % 16] = -INFINITY;
         }
+        st = f32x2t{0.f, 0.f};
       }
+      turn(i);
+      auto weigh = [&](int c) __attribute__((always_inline)) {
+        constexpr int kAll = 16 * kBlocks;
+#pragma unroll
+        for (int e = kAll * c / 8; e < kAll * (c + 1) / 8; ++e)
+          sum[e / 16][e % 16] = fmaf(__builtin_amdgcn_exp2f(fmaf(y[e / 16][e % 16], kMassUnit, -st[0])), st[1], sum[e / 16][e % 16]);
+      };
+      const lds_char* const queries = slot((i + 1) / M::kSubs) + (i + 1) % M::kSubs * (32 * M::kRowBytes);
+      mass_scores<false, Op, kBlocks>(next, queries, k, n, h, weigh);
+    };
+    if (key0 < len) {
+      f32x16 even[kBlocks], odd[kBlocks];
+      mass_scores<false, Op, kBlocks>(even, slot(0), k, n, h, [](int) {});
+      for (int i = 0; i < subs; i += 2) {
+        step(i, even, odd);
+        if (i + 1 >= subs) break;
+        step(i + 1, odd, even);
+      }
+    } else {
+      for (int i = 0; i < subs; ++i) turn(i);
     }
+    __syncthreads();
   }
+  float* const mine = reinterpret_cast<float*>(lds_) + wave * M::kMine;
 #pragma unroll
   for (int kb = 0; kb < kBlocks; ++kb)
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
       float x = row16_sum(sum[kb][r]);
       x += __shfl_xor(x, 16);
-      if (n == 0) sums[wave][32 * kb + key_of(r, h)] = x;
+      if (n == 0) mine[32 * kb + key_of(r, h)] = x;
     }
   wave_lds_order();
   const int key = key0 + lane;
-  if (lane < 32 * kBlocks && key < len) {
-    float* const to = a.mass + (int64_t)bg * s.Lcap + key;
-    const int held = a.held ? a.held[b] : 0;
-    *to = sums[wave][lane] + (a.t0 > 0 ? *to : (key < held ? a.decay * *to : 0.f));
+  if (lane < M::kMine && key < len) {
+    if (gridDim.z > 1) {
+      a.sums[((int64_t)blockIdx.z * gridDim.y + bg) * s.Lcap + key] = mine[lane];
+    } else {
+      float* const to = a.mass + (int64_t)bg * s.Lcap + key;
+      const int held = a.held ? a.held[b] : 0;
+      *to = mine[lane] + (a.t0 > 0 ? *to : (key < held ? a.decay * *to : 0.f));
+    }
   }
 }
 
+// The chunks' sums, in order.  grid (rows / 256, B * Hkv)
+template <typename A>
+__global__ __launch_bounds__(256) void k_mass_sum(A a, int chunks) {
+  const int bg = blockIdx.y, b = bg / a.s.Hkv, key = blockIdx.x * 256 + threadIdx.x;
+  if (key >= length_of(a.s, a.kv.seq_lens, b)) return;
+  const float* const from = a.sums + (int64_t)bg * a.s.Lcap + key;
+  float sum = 0.f;
+#pragma unroll 4
+  for (int c = 0; c < chunks; ++c) sum += from[(int64_t)c * gridDim.y * a.s.Lcap];
+  float* const to = a.mass + (int64_t)bg * a.s.Lcap + key;
+  const int held = a.held ? a.held[b] : 0;
+  *to = sum + (a.t0 > 0 ? *to : (key < held ? a.decay * *to : 0.f));
+}
+
 template <typename TK, typename TQ>
-static hipError_t mass_t(MassArgs<TQ> a, int64_t room, hipStream_t st) {
-  typedef typename InLds<TQ>::Op Op;
-  constexpr int kRows = mass_rows<Op>();
+static hipError_t mass_t(MassArgs<TQ> a, float* work, int64_t room, hipStream_t st) {
+  typedef MassShape<typename InLds<TQ>::Op> M;
   const int64_t most = room / 2 / a.s.Hq;                            // tokens that the workspace has room for
-  const int per = kRows / a.s.G;
-  const dim3 keys((unsigned)((a.s.Lcap + kRows - 1) / kRows), (unsigned)(a.s.B * a.s.Hkv));
+  const int per = M::kRows / a.s.G;
+  const int64_t masses = (int64_t)a.s.B * a.s.Hkv * a.s.Lcap;
   for (int t0 = 0; t0 == 0 || t0 < a.n_tokens; t0 = a.t1) {           // (also of no tokens: what is held decays)
     a.t0 = t0;
     a.t1 = a.n_tokens - t0 > most ? t0 + (int)most : a.n_tokens;
     const int n = a.t1 - t0, tiles = n / per + a.s.B;
+    const int64_t rows = (int64_t)n * a.s.Hq, left = room - 2 * rows;
+    a.stats = work;
+    a.split_stats = a.sums = work + 2 * rows;                         // (the parts are joined before there are sums)
     if (n > 0) {
-      const int64_t groups = (int64_t)tiles * a.s.Hkv, rows = (int64_t)n * a.s.Hq, by_len = (a.s.Lcap + 255) / 256;
+      const int64_t groups = (int64_t)tiles * a.s.Hkv, by_len = (a.s.Lcap + 255) / 256;
       int64_t splits = (512 + groups - 1) / groups;
-      if (splits * rows * 2 > room) splits = room / 2 / rows;
+      if (splits * rows * 2 > left) splits = left / 2 / rows;
       if (splits > by_len) splits = by_len;
       a.splits = (int)(splits > kMaxSplits ? kMaxSplits : (splits < 1 ? 1 : splits));
       hipLaunchKernelGGL((k_mass_stats<TK, TQ>), dim3((unsigned)(groups * a.splits)), dim3(kMassThreads), 0, st, a, tiles);
-      if (a.splits > 1) hipLaunchKernelGGL(k_mass_join, dim3((unsigned)((rows + 255) / 256)), dim3(256), 0, st, a.stats, rows, a.splits);
+      if (a.splits > 1)
+        hipLaunchKernelGGL(k_mass_join, dim3((unsigned)((rows + 15) / 16)), dim3(256), 0, st, a.split_stats, a.stats, rows, a.splits);
     }
-    hipLaunchKernelGGL((k_mass_add<TK, TQ>), keys, dim3(kMassThreads), 0, st, a);
+    // Of the query rows as many chunks as make work for the whole chip several times over: a tile's work falls with its place.
+    const int64_t queries = (int64_t)n * a.s.G, key_tiles = (a.s.Lcap + M::kRows - 1) / M::kRows, wanted = 4096;
+    int64_t chunks = (wanted + key_tiles * a.s.B * a.s.Hkv - 1) / (key_tiles * a.s.B * a.s.Hkv);
+    if (chunks > (queries + 1023) / 1024) chunks = (queries + 1023) / 1024;
+    if (chunks * masses > left) chunks = left / masses;
+    chunks = chunks < 1 ? 1 : chunks;
+    a.chunk = (int)(((queries + chunks - 1) / chunks + M::kStage - 1) / M::kStage * M::kStage);
+    a.chunk = a.chunk < M::kStage ? M::kStage : a.chunk;
+    const int z = queries > a.chunk ? (int)((queries + a.chunk - 1) / a.chunk) : 1;
+    hipLaunchKernelGGL((k_mass_add<TK, TQ>), dim3((unsigned)key_tiles, (unsigned)(a.s.B * a.s.Hkv), (unsigned)z), dim3(kMassThreads), 0, st, a);
+    if (z > 1)
+      hipLaunchKernelGGL((k_mass_sum<MassArgs<TQ>>), dim3((unsigned)((a.s.Lcap + 255) / 256), (unsigned)(a.s.B * a.s.Hkv)), dim3(256), 0, st, a, z);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.n_tokens == 0) return e;
   }
@@ -373,8 +518,9 @@ static hipError_t mass_t(MassArgs<TQ> a, int64_t room, hipStream_t st) {
 
 hipError_t launch_attn_mass(const Shape& s, int dtype, const KvView& kv, const void* q, int64_t q_stride, const int32_t* cu, int n_tokens,
                             const int32_t* held, float decay, float* mass, float* part, int64_t part_rows, hipStream_t st) {
-#define LFPS_MASS(TK, TQ)                                                                                                  \
-  return mass_t<TK, TQ>(MassArgs<TQ>{s, kv, (const TQ*)q, q_stride, cu, held, n_tokens, 0, 0, decay, part, 1, mass}, part_rows * kPartFloats, st)
+#define LFPS_MASS(TK, TQ)                                                                                                              \
+  return mass_t<TK, TQ>(MassArgs<TQ>{s, kv, (const TQ*)q, q_stride, cu, held, n_tokens, 0, 0, decay, nullptr, nullptr, 1, 0, nullptr, mass}, \
+                        part, part_rows * kPartFloats, st)
   if (dtype == LFPS_F32) LFPS_MASS(float, float);
   if (dtype == LFPS_F16) LFPS_MASS(_Float16, _Float16);
   if (kv.k_fp8) LFPS_MASS(uint8_t, uint16_t);

@@ -13,6 +13,8 @@ constexpr int kAttnThreads = 256;       // full attention
 __host__ __device__ __forceinline__ int rows_per_split(int n, int n_split) { return (((n + n_split - 1) / n_split) + 15) & ~15; }
 struct RowsOf { int b, g, begin, end; int64_t part; int at, by; };      // (from row `at` on: the cache's row `by` further up)
 // Further arguments of the kernels: what else than all rows of a request they take or leave.
+template <typename... Own>
+constexpr int attn_waves() { return (std::is_same<Own, OwnRows>::value || ... || (sizeof...(Own) == 0)) ? 1 : 3; }
 struct WindowRows { int32_t window, n_sink; };        // the newest `window` rows of a request and its first n_sink
 struct ScoresTo { float* score; int64_t stride; };    // all rows, whose scores go to score [B, Hq, stride] (no grouping: in powers of two)
 // The rows of a window in order: the first `at` of the cache, then those from `at + by` on, `count` in all.
@@ -128,7 +130,7 @@ __device__ __forceinline__ float row16_shared_sums(float (&a)[G], int j) {
 // 207 us with the kernel as it was); fewer are found there by the next call, whatever the context has room for (8 x 8192 of
 // 131072 rows in bf16 52.9 -> 48.8 us, 8 x 16384 in FP8 62.3 -> 57.3, against that capacity deciding).
 template <typename TK, typename T, int G, bool kPaged, bool kMayOnce, typename... Own>
-__global__ __launch_bounds__(kAttnThreads) void k_full_attn(Shape s, const float* __restrict__ q,
+__global__ __launch_bounds__(kAttnThreads, attn_waves<Own...>()) void k_full_attn(Shape s, const float* __restrict__ q,
                                                             const TK* __restrict__ K, const T* __restrict__ V,
                                                             int64_t stride_b, int64_t stride_h, int64_t stride_n,
                                                             KvPage pg, const int32_t* __restrict__ seq_lens,
@@ -188,10 +190,12 @@ __global__ __launch_bounds__(kAttnThreads) void k_full_attn(Shape s, const float
 #pragma unroll
     for (int c = 0; c < 8; ++c) acc[h][c] = 0.f;
 
-  float* to_scores = nullptr;                               // of head j % G
+  float* to_scores = nullptr;                               // of the group; with head j % G's offset
+  uint32_t my_scores = 0;
   if constexpr (kScores) {
     const ScoresTo& to = std::get<0>(std::tie(own...));
-    to_scores = to.score + ((int64_t)b * s.Hq + g * G + j % G) * to.stride;
+    to_scores = to.score + ((int64_t)b * s.Hq + g * G) * to.stride;
+    my_scores = (uint32_t)(j % G) * (uint32_t)to.stride;
   }
   constexpr int kStep = 4 * kRows;                          // wave w takes tiles w, w + 4, ...
   auto walk = [&](auto once) {
@@ -223,7 +227,7 @@ __global__ __launch_bounds__(kAttnThreads) void k_full_attn(Shape s, const float
 #pragma unroll
       for (int t = 0; t < NV; ++t) {
         const int r = r0 + 4 * (t * kShare + my_u) + rs;
-        if (mine && r < r_end) to_scores[r] = v[t];
+        if (mine && r < r_end) to_scores[my_scores + (uint32_t)r] = v[t];
       }
     }
     if constexpr (kGap || kScores) {
