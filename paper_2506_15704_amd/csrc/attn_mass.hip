@@ -317,7 +317,9 @@ __global__ __launch_bounds__(256) void k_mass_join(const float* __restrict__ spl
   reinterpret_cast<f32x2t*>(stats)[row] = f32x2t{mx == -INFINITY ? 0.f : mx, sum == 0.f ? 0.f : 1.f / sum};
 }
 
-// grid (tiles of kRows keys, B * Hkv, chunks of query rows): the first keys are seen by most.
+// grid (B * Hkv, tiles of kRows keys, chunks of query rows).  Workgroups go round the XCDs, and within one round its shader engines, in the order of
+// their numbers: with the tiles first, of which the later ones are seen by fewer, the first engines of every XCD had twice the work of the
+// average (8192 tokens of 32 heads 528 us).
 // A wave's keys come through the ring's slot of its number into registers; then the query rows stream through it as the keys do in k_mass_stats.
 template <typename TK, typename TQ>
 __global__ __launch_bounds__(kMassThreads, sizeof(TK) == 4 ? 1 : 2) void k_mass_add(MassArgs<TQ> a) {
@@ -328,7 +330,7 @@ __global__ __launch_bounds__(kMassThreads, sizeof(TK) == 4 ? 1 : 2) void k_mass_
   __shared__ __attribute__((aligned(16))) char lds_[kMassRing * kBytes];       // (one array: of several the compiler waits for all requests before any read)
   const Shape& s = a.s;
   const int G = s.G, shift = G == 4 ? 2 : G - 1;
-  const int bg = blockIdx.y, b = bg / s.Hkv, g = bg % s.Hkv, tile = blockIdx.x * M::kRows, len = length_of(s, a.kv.seq_lens, b);
+  const int bg = blockIdx.x, b = bg / s.Hkv, g = bg % s.Hkv, tile = blockIdx.y * M::kRows, len = length_of(s, a.kv.seq_lens, b);
   if (tile >= len) return;
   const int lane = threadIdx.x & 63, wave = wave_of(), n = lane & 31, h = lane >> 5;
   int c0, c1;
@@ -372,21 +374,35 @@ __global__ __launch_bounds__(kMassThreads, sizeof(TK) == 4 ? 1 : 2) void k_mass_
     constexpr int kPieces = M::kRowBytes / 16, kEach = 64 / kPieces, kWaveRows = M::kStage / kMassWaves, kLoads = kWaveRows / kEach;
     const int stages = (rows - m0 + M::kStage - 1) / M::kStage;
     const float* const stats = a.stats + 2 * (((int64_t)g * (a.t1 - a.t0) + (c0 - a.t0)) * G);
-    auto ask = [&](int j) {
-      lds_char* const to = slot(j);
-      const int r0 = m0 + j * M::kStage + kWaveRows * wave;
+    // My pieces of a stage, counted from its first query row: a stage begins with a token.
+    int64_t off[kLoads];
+    auto place_of = [&](int i, int row) {                      // of query row `row` of those that the pieces are counted from
+      const int r = kWaveRows * wave + kEach * i + lane / kPieces, place = lane % kPieces;
+      return ((int64_t)(row >> shift) * a.q_stride + (row & (G - 1)) * kD) * (int64_t)sizeof(TQ) + 16 * (M::kF32 ? chunk_place_f32(r, place) : chunk_place(r, place));
+    };
+    auto my_row = [&](int i) { return kWaveRows * wave + kEach * i + lane / kPieces; };
 #pragma unroll
-      for (int i = 0; i < kLoads; ++i) {
-        const int r = kWaveRows * wave + kEach * i + lane / kPieces, place = lane % kPieces;
-        const int row = r0 + kEach * i + lane / kPieces < rows ? r0 + kEach * i + lane / kPieces : rows - 1;
-        const char* const p = reinterpret_cast<const char*>(a.q + (int64_t)(c0 + (row >> shift)) * a.q_stride + (g * G + (row & (G - 1))) * kD) +
-                              16 * (M::kF32 ? chunk_place_f32(r, place) : chunk_place(r, place));
-        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) char*)p,
-                                         (__attribute__((address_space(3))) void*)(to + (kWaveRows * wave + kEach * i) * M::kRowBytes), 16, 0, 0);
+    for (int i = 0; i < kLoads; ++i) off[i] = place_of(i, my_row(i));
+    auto ask = [&](int j) __attribute__((always_inline)) {
+      lds_char* const to = slot(j);
+      const int m = m0 + j * M::kStage;
+      const char* const q = reinterpret_cast<const char*>(a.q + (int64_t)(c0 + (m >> shift)) * a.q_stride + g * G * kD);
+      const char* p[kLoads];
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) p[i] = q + off[i];
+      int row = kWaveRows * wave + lane / 2;
+      if (m + M::kStage > rows) {                              // (rows that are not there repeat the last one)
+        const int last = rows - 1 - m;
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) p[i] = q + place_of(i, my_row(i) < last ? my_row(i) : last);
+        row = row < last ? row : last;
       }
-      const int row = r0 + lane / 2 < rows ? r0 + lane / 2 : rows - 1;
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i)
+        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) char*)p[i],
+                                         (__attribute__((address_space(3))) void*)(to + (kWaveRows * wave + kEach * i) * M::kRowBytes), 16, 0, 0);
       if (lane < 2 * kWaveRows)
-        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) char*)(stats + 2 * (int64_t)row + (lane & 1)),
+        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) char*)(stats + 2 * (int64_t)m + (2 * row + (lane & 1))),
                                          (__attribute__((address_space(3))) void*)(to + M::kBytes + kWaveRows * wave * 8), 4, 0, 0);
     };
     constexpr int kRequests = kLoads + 1;
@@ -452,7 +468,7 @@ __global__ __launch_bounds__(kMassThreads, sizeof(TK) == 4 ? 1 : 2) void k_mass_
   const int key = key0 + lane;
   if (lane < M::kMine && key < len) {
     if (gridDim.z > 1) {
-      a.sums[((int64_t)blockIdx.z * gridDim.y + bg) * s.Lcap + key] = mine[lane];
+      a.sums[((int64_t)blockIdx.z * gridDim.x + bg) * s.Lcap + key] = mine[lane];
     } else {
       float* const to = a.mass + (int64_t)bg * s.Lcap + key;
       const int held = a.held ? a.held[b] : 0;
@@ -501,13 +517,14 @@ static hipError_t mass_t(MassArgs<TQ> a, float* work, int64_t room, hipStream_t 
     // Of the query rows as many chunks as make work for the whole chip several times over: a tile's work falls with its place.
     const int64_t queries = (int64_t)n * a.s.G, key_tiles = (a.s.Lcap + M::kRows - 1) / M::kRows, wanted = 4096;
     int64_t chunks = (wanted + key_tiles * a.s.B * a.s.Hkv - 1) / (key_tiles * a.s.B * a.s.Hkv);
+    if (chunks > 1 || queries > 4096) chunks = chunks > (queries + 2047) / 2048 ? chunks : (queries + 2047) / 2048;
     if (chunks > (queries + 1023) / 1024) chunks = (queries + 1023) / 1024;
     if (chunks * masses > left) chunks = left / masses;
     chunks = chunks < 1 ? 1 : chunks;
     a.chunk = (int)(((queries + chunks - 1) / chunks + M::kStage - 1) / M::kStage * M::kStage);
     a.chunk = a.chunk < M::kStage ? M::kStage : a.chunk;
     const int z = queries > a.chunk ? (int)((queries + a.chunk - 1) / a.chunk) : 1;
-    hipLaunchKernelGGL((k_mass_add<TK, TQ>), dim3((unsigned)key_tiles, (unsigned)(a.s.B * a.s.Hkv), (unsigned)z), dim3(kMassThreads), 0, st, a);
+    hipLaunchKernelGGL((k_mass_add<TK, TQ>), dim3((unsigned)(a.s.B * a.s.Hkv), (unsigned)key_tiles, (unsigned)z), dim3(kMassThreads), 0, st, a);
     if (z > 1)
       hipLaunchKernelGGL((k_mass_sum<MassArgs<TQ>>), dim3((unsigned)((a.s.Lcap + 255) / 256), (unsigned)(a.s.B * a.s.Hkv)), dim3(256), 0, st, a, z);
     const hipError_t e = hipGetLastError();
