@@ -1,11 +1,12 @@
 // Eviction: of the n_b rows of a request every KV head keeps m = min(n_b, budget): the first n_sink, the n_recent newest, and between them those of
 // the largest accumulated weight (equal ones: the lower rows; NaN: as the least).  They move to the front, in order, and with them their weights.
 //
-// k_evict_plan, a workgroup a (request, KV head): the weight at the cut by three passes of a histogram over the bits of its order-preserving key,
+// k_evict_plan, a workgroup a (request, KV head), or where that leaves CUs without work several that all find the cut and share the rest: the weight at the cut by three passes of a histogram over the bits of its order-preserving key,
 // then the rows that are kept, in order: every wave has a stretch of the rows, counts what it keeps, and writes it behind what the waves
-// before it keep.
-// k_evict_move carries the rows.  In place (kept rows only ever move down) a workgroup takes a slice of 64 bytes of every row in order, a stretch at a
-// time: all of it is read before any of it is written, and what later stretches read lies behind what this one writes.
+// before it keep.  Up to 32768 rows stay in registers from the first pass to the last; of more, every pass reads them again.
+// k_evict_move carries the rows.  In place (kept rows only ever move down) a workgroup takes a slice of every row in order, a stretch at a
+// time: all of it is read before any of it is written, and what later stretches read lies behind what this one writes, so that they are asked
+// for before it is.
 #include "tile_attn.h"
 
 namespace lfps {
@@ -13,18 +14,18 @@ namespace lfps {
 namespace {
 
 constexpr int kPlanThreads = 1024, kPlanWaves = kPlanThreads / 64, kBins = 2048;
-constexpr int kMoveThreads = 512, kMoveU = 4;          // rows pieces of 16 bytes that a thread has on its way
+constexpr int kPlanEach = 32, kPlanChunk = kPlanThreads * kPlanEach;       // weights of a thread; rows of the workgroup at a time
+constexpr int kMoveU = 8;                              // pieces of 16 bytes that a thread has on its way
 
-__device__ __forceinline__ uint32_t weight_key(float x) { return x != x ? 0u : f2key(x + 0.f); }      // (-0 is 0)
+__device__ __forceinline__ uint32_t weight_key(float x) { return x != x ? 1u : f2key(x + 0.f); }      // (-0 is 0; a NaN below all numbers)
 
 struct Cut {
-  int n, m, sinks, last, pick;         // rows; kept ones; kept first ones; where the kept newest begin; kept ones between
+  int n, m, sinks, last;               // rows; kept ones; kept first ones; where the kept newest begin
   __device__ __forceinline__ Cut(int n_, int budget, int n_sink, int n_recent) : n(n_) {
     m = budget < 0 ? 0 : (budget < n ? budget : n);
     sinks = n_sink < m ? n_sink : m;
     const int recent = n_recent < m - sinks ? n_recent : m - sinks;
     last = n - recent;
-    pick = m - sinks - recent;
   }
 };
 
@@ -36,154 +37,232 @@ __global__ __launch_bounds__(kPlanThreads) void k_evict_plan(Shape s, const int3
   __shared__ int bins[kBins], sums[kPlanWaves][2], found[2];
   const int bg = blockIdx.x, b = bg / s.Hkv, tid = threadIdx.x, lane = tid & 63, wave = wave_of();
   const Cut cut(length_of(s, seq_lens, b), budget[b], n_sink, n_recent);
-  if (bg % s.Hkv == 0 && tid == 0) lens_out[b] = cut.m;
+  if (bg % s.Hkv == 0 && blockIdx.y == 0 && tid == 0) lens_out[b] = cut.m;
   const float* const w = mass + (int64_t)bg * s.Lcap;
+  // Chunk c's rows of a thread, `each` of them: row(c, i), in the order chunk, wave, i, lane.  Their keys: the first and the newest ones' above all,
+  // those of rows that are not there below all.  So the m largest keys are kept, of equal ones the lower rows.
+  const int chunks = (cut.n + kPlanChunk - 1) / kPlanChunk, each = chunks > 1 ? kPlanEach : (cut.n + kPlanThreads - 1) / kPlanThreads;
+  uint32_t key[kPlanEach];
+  auto row = [&](int c, int i) { return c * kPlanChunk + (wave * each + i) * 64 + lane; };
+  auto weight = [&](int r) { return w[r < cut.n ? r : cut.n - 1]; };
+  // (a count that the compiler cannot know again: 32 comparisons with `each`, kept for every loop, do not fit the scalar registers)
+  auto fresh = [&] {
+    int e = each;
+    asm volatile("" : "+s"(e));
+    return e;
+  };
+  auto fetch = [&](int c) __attribute__((always_inline)) {
+    const int e0 = fresh();
+#pragma unroll
+    for (int i = 0; i < kPlanEach; ++i)
+      if (i < e0) key[i] = __float_as_uint(weight(row(c, i)));
+    const int e1 = fresh();
+#pragma unroll
+    for (int i = 0; i < kPlanEach; ++i)
+      if (i < e1) {
+        key[i] = weight_key(__uint_as_float(key[i]));
+        const int r0 = row(c, i) - lane;
+        if (r0 < cut.sinks || r0 + 64 > cut.last) {
+          const int r = r0 + lane;
+          key[i] = r >= cut.n ? 0u : (r < cut.sinks || r >= cut.last ? 0xFFFFFFFFu : key[i]);
+        }
+      }
+  };
+  if (chunks == 1) fetch(0);
   // the key at the cut, from its highest bits down: `least` is its bits so far, `left` how many of those that have these bits are kept
   uint32_t least = 0;
-  int left = cut.pick;
+  int left = cut.m;
   if (left > 0) {
     int shift = 32;
+#pragma unroll 1
     for (int pass = 0; pass < 3; ++pass) {
       const int bits = pass < 2 ? 11 : 10, before = shift;
       shift -= bits;
       for (int i = tid; i < kBins; i += kPlanThreads) bins[i] = 0;
       __syncthreads();
-      for (int i = cut.sinks + tid; i < cut.last; i += kPlanThreads) {
-        const uint32_t key = weight_key(w[i]);
-        if (pass == 0 || key >> before == least >> before) atomicAdd(&bins[(key >> shift) & ((1 << bits) - 1)], 1);
+      for (int c = 0; c < chunks; ++c) {
+        if (chunks > 1) fetch(c);
+        const int e = fresh();
+#pragma unroll
+        for (int i = 0; i < kPlanEach; ++i)
+          if (i < e && (pass == 0 || key[i] >> before == least >> before)) atomicAdd(&bins[(key[i] >> shift) & ((1 << bits) - 1)], 1);
       }
       __syncthreads();
-      if (wave == 0) {                                       // lane l has the bins of the l-th highest part of them
-        constexpr int kEach = kBins / 64;
-        const int each = (1 << bits) / 64, top = (1 << bits) - 1 - lane * each;
-        int sum = 0;
-        for (int i = 0; i < each; ++i) sum += bins[top - i];
-        int above = wave_inclusive_sum(sum) - sum;
-        if (above < left && left <= above + sum) {
-          int i = 0;
-          while (above + bins[top - i] < left) above += bins[top - i++];
-          found[0] = top - i;
-          found[1] = left - above;
-        }
-        static_assert(kEach * 64 == kBins, "");
+      // thread t has the t-th highest bin or two: those above them come from the threads before
+      const int mine = (1 << bits) / kPlanThreads, top = (1 << bits) - 1 - tid * mine, high = bins[top], low = mine > 1 ? bins[top - 1] : 0;
+      int above = wave_inclusive_sum(high + low);
+      if (lane == 63) sums[wave][0] = above;
+      above -= high + low;
+      __syncthreads();
+      for (int i = 0; i < kPlanWaves; ++i) above += i < wave ? sums[i][0] : 0;
+      if (above < left && left <= above + high + low) {
+        const bool second = left > above + high;
+        found[0] = top - second;
+        found[1] = left - above - (second ? high : 0);
       }
       __syncthreads();
       least |= (uint32_t)found[0] << shift;
       left = found[1];
       __syncthreads();
     }
+  } else {
+    least = 0xFFFFFFFFu;                                     // (nothing is kept: no row has this key then)
   }
-  // of my wave's rows: kept whatever else is, and at the cut
-  const int each = ((cut.n + kPlanWaves - 1) / kPlanWaves + 63) & ~63, from = wave * each, to = from + each < cut.n ? from + each : cut.n;
-  auto look = [&](int i, float x, bool* at_cut) {
-    const bool between = i >= cut.sinks && i < cut.last;
-    const uint32_t key = weight_key(x);
-    *at_cut = i < to && between && cut.pick > 0 && key == least;
-    return i < to && (!between || (cut.pick > 0 && key > least));
-  };
-  int sure = 0, equal = 0;
-  for (int i0 = from; i0 < to; i0 += 64) {
-    const int i = i0 + lane;
-    bool at_cut;
-    const bool keep = look(i, w[i < to ? i : to - 1], &at_cut);
-    sure += __popcll(__ballot(keep));
-    equal += __popcll(__ballot(at_cut));
-  }
-  if (lane == 0) {
-    sums[wave][0] = sure;
-    sums[wave][1] = equal;
-  }
-  __syncthreads();
-  int place = 0, equals = 0;
-  for (int i = 0; i < wave; ++i) {
-    place += sums[i][0];
-    equals += sums[i][1];
-  }
-  place += equals < left ? equals : left;
-  const uint64_t below = ((uint64_t)1 << lane) - 1;
-  for (int i0 = from; i0 < to; i0 += 64) {
-    const int i = i0 + lane;
-    const float x = w[i < to ? i : to - 1];
-    bool at_cut;
-    const bool keep = look(i, x, &at_cut);
-    const uint64_t same = __ballot(at_cut);
-    const bool mine = keep || (at_cut && equals + __popcll(same & below) < left);
-    const uint64_t all = __ballot(mine);
-    if (mine) {
-      const int64_t at = (int64_t)bg * s.Lcap + place + __popcll(all & below);
-      kept[at] = i;
-      mass_out[at] = x;
+  int base = 0, equals_before = 0;                           // kept rows, and rows at the cut, of the chunks before
+  for (int c = 0; c < chunks; ++c) {
+    if (chunks > 1) fetch(c);
+    // of my wave's rows: kept whatever else is, and in the upper half those at the cut (at most 2048 of either); and of those before my part
+    const int part0 = each * (int)blockIdx.y / (int)gridDim.y, part1 = each * ((int)blockIdx.y + 1) / (int)gridDim.y, e = fresh();
+    int mine = 0, early = 0;
+#pragma unroll
+    for (int i = 0; i < kPlanEach; ++i)
+      if (i < e) {
+        early = i == part0 ? mine : early;
+        mine += key[i] > least ? 1 : (key[i] == least ? 1 << 16 : 0);
+      }
+    mine = wave_inclusive_sum(mine);
+    early = __builtin_amdgcn_readlane(wave_inclusive_sum(part0 < each ? early : 0), 63);
+    if (lane == 63) {
+      sums[wave][0] = mine & 0xFFFF;
+      sums[wave][1] = mine >> 16;
     }
-    equals += __popcll(same);
-    place += __popcll(all);
+    __syncthreads();
+    int place = base, equals = equals_before, all_sure = 0, all_equal = 0;
+    for (int i = 0; i < kPlanWaves; ++i) {
+      place += i < wave ? sums[i][0] : 0;
+      equals += i < wave ? sums[i][1] : 0;
+      all_sure += sums[i][0];
+      all_equal += sums[i][1];
+    }
+    place += early & 0xFFFF;
+    equals += early >> 16;
+    // (base counts the rows at the cut that were kept)
+    place += (equals < left ? equals : left) - (equals_before < left ? equals_before : left);
+    int32_t* const to = kept + (int64_t)bg * s.Lcap;
+    float* const to_mass = mass_out + (int64_t)bg * s.Lcap;
+    auto rank = [](uint64_t mask) { return (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0)); };
+    constexpr int kBatch = 8;
+#pragma unroll
+    for (int i0 = 0; i0 < kPlanEach; i0 += kBatch) {
+      if (i0 + kBatch <= part0 || i0 >= part1) continue;
+      float x[kBatch];
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i) x[i] = weight(row(c, i0 + i));
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i) {
+        if (i0 + i < part0 || i0 + i >= part1) continue;
+        const uint32_t k = key[i0 + i];
+        const uint64_t same = __ballot(k == least);
+        bool keep = k > least;
+        if (same) keep = keep || (k == least && equals + rank(same) < left);
+        const uint64_t all = __ballot(keep);
+        if (keep) {
+          const int at = place + rank(all);
+          to[at] = row(c, i0 + i);
+          to_mass[at] = x[i];
+        }
+        equals += __popcll(same);
+        place += __popcll(all);
+      }
+    }
+    const int equals_after = equals_before + all_equal;
+    base += all_sure + (equals_after < left ? equals_after : left) - (equals_before < left ? equals_before : left);
+    equals_before = equals_after;
+    __syncthreads();
   }
 }
 
-// kInPlace: grid (slices of four pieces of K's row, then of V's; B * Hkv); else (parts of the kept rows; B * Hkv; K, V).
-template <bool kInPlace>
-__global__ __launch_bounds__(kMoveThreads) void k_evict_move(Shape s, KvView kv, KvView to, int k_bytes, int v_bytes, const int32_t* __restrict__ budget,
-                                                             const int32_t* __restrict__ kept) {
-  const int bg = blockIdx.y, b = bg / s.Hkv, g = bg % s.Hkv, n = length_of(s, kv.seq_lens, b);
+// A workgroup moves `slice` pieces of 16 bytes of every kept row: grid (B * Hkv; slices of K's row, then of V's; in place: 1, else parts of the kept
+// rows).  A group's slices come from one XCD, where they share the lines that they do not fill.
+template <bool kInPlace, int kThreads>
+__global__ __launch_bounds__(kThreads) void k_evict_move(Shape s, KvView kv, KvView to, int k_bytes, int v_bytes, int slice, const int32_t* __restrict__ budget,
+                                                         const int32_t* __restrict__ kept) {
+  const int bg = blockIdx.x, b = bg / s.Hkv, g = bg % s.Hkv, n = length_of(s, kv.seq_lens, b);
   const int m = budget[b] < 0 ? 0 : (budget[b] < n ? budget[b] : n);
   if (kInPlace && m == n) return;
-  constexpr int kSlice = 4;                                  // pieces of 16 bytes
-  const int k_slices = kD * k_bytes / 16 / kSlice;
-  const bool is_v = kInPlace ? (int)blockIdx.x >= k_slices : blockIdx.z == 1;
-  const int esz = is_v ? v_bytes : k_bytes, pieces = kInPlace ? kSlice : kD * esz / 16;
-  const int piece = (kInPlace ? kSlice * ((int)blockIdx.x - (is_v ? k_slices : 0)) : 0) + (int)threadIdx.x % pieces;
-  const int rows = kMoveThreads / pieces;
-  auto address = [&](const KvView& c, int i, bool* there) {
-    const CacheRows<char> rows_of(is_v ? c.v : c.k, c, 0, 0);
-    int64_t off = (int64_t)g * c.stride_h;
-    *there = true;
-    if (c.page.table) {
-      const int e = RowMap<true>::block(c.page, b, i);
-      *there = (uint32_t)e < (uint32_t)c.page.n_blocks;
-      off += RowMap<true>::offset_in(c.page, e, i, c.stride_b, c.stride_n);
-    } else {
-      off += (int64_t)b * c.stride_b + (int64_t)i * c.stride_n;
-    }
-    return reinterpret_cast<u32x4*>(const_cast<char*>(rows_of.base) + off * esz) + piece;
-  };
-  const int32_t* const mine = kept + (int64_t)bg * s.Lcap;
-  const int step = rows * kMoveU, first = kInPlace ? 0 : blockIdx.x * step, hop = kInPlace ? step : step * (int)gridDim.x;
-  for (int i0 = first; i0 < m; i0 += hop) {
-    u32x4 x[kMoveU];
+  const int k_slices = kD * k_bytes / 16 / slice;
+  const bool is_v = (int)blockIdx.y >= k_slices;
+  const int esz = is_v ? v_bytes : k_bytes, piece = slice * ((int)blockIdx.y - (is_v ? k_slices : 0)) + (int)threadIdx.x % slice;
+  const int rows = kThreads / slice, step = rows * kMoveU, mine = (int)threadIdx.x / slice;
+  const int64_t group = (int64_t)g * kv.stride_h, group_to = (int64_t)g * to.stride_h;
+  const char* const from_base = (const char*)(is_v ? kv.v : kv.k) + 16 * piece;
+  char* const to_base = (char*)const_cast<void*>(is_v ? to.v : to.k) + 16 * piece;
+  const int32_t* const list = kept + (int64_t)bg * s.Lcap;
+  const int first = kInPlace ? 0 : (int)blockIdx.z * step, end = kInPlace ? m : (first + step < m ? first + step : m);
+  if (first >= end) return;
+  struct Stretch {
     int from[kMoveU];
+    u32x4 x[kMoveU];
+  };
+  auto look = [&](int i0, int (&from)[kMoveU]) {              // rows that do not move, or are not there: -1
 #pragma unroll
     for (int u = 0; u < kMoveU; ++u) {
-      const int i = i0 + u * rows + (int)threadIdx.x / pieces;
-      bool there;
-      from[u] = i < m ? mine[i] : -1;
-      if (from[u] >= 0) x[u] = *address(kv, from[u], &there);
+      const int i = i0 + u * rows + mine;
+      from[u] = list[i < end ? i : end - 1];
+      if (i >= end || (kInPlace && from[u] == i)) from[u] = -1;
     }
-    if (kInPlace) {
+  };
+  auto read = [&](Stretch& t) {
+    int64_t off[kMoveU];
+#pragma unroll
+    for (int u = 0; u < kMoveU; ++u) {
+      const int r = t.from[u] < 0 ? 0 : t.from[u];
+      off[u] = kv.page.table ? RowMap<true>::offset_in(kv.page, RowMap<true>::block(kv.page, b, r), r, kv.stride_b, kv.stride_n)
+                             : (int64_t)b * kv.stride_b + (int64_t)r * kv.stride_n;
+    }
+#pragma unroll
+    for (int u = 0; u < kMoveU; ++u)
+      if (t.from[u] >= 0) t.x[u] = *reinterpret_cast<const u32x4*>(from_base + (group + off[u]) * esz);
+  };
+  auto write = [&](int i0, const Stretch& t) {
+#pragma unroll
+    for (int u = 0; u < kMoveU; ++u) {
+      const int i = i0 + u * rows + mine;
+      if (t.from[u] < 0) continue;
+      int64_t off = (int64_t)b * to.stride_b + (int64_t)i * to.stride_n;
+      if (to.page.table) {
+        const int e = RowMap<true>::block(to.page, b, i);
+        if ((uint32_t)e >= (uint32_t)to.page.n_blocks) continue;
+        off = RowMap<true>::offset_in(to.page, e, i, to.stride_b, to.stride_n);
+      }
+      *reinterpret_cast<u32x4*>(to_base + (group_to + off) * esz) = t.x[u];
+    }
+  };
+  Stretch t;
+  look(first, t.from);
+  read(t);
+  if constexpr (!kInPlace) {
+    write(first, t);
+  } else {
+    for (int i0 = 0;; i0 += step) {
+      const bool more = i0 + step < end;
+      Stretch next;
+      if (more) look(i0 + step, next.from);
       __builtin_amdgcn_s_waitcnt(0x0f70);                    // vmcnt(0): what I read is here
-      __syncthreads();
+      __syncthreads();                                       // ... and what the others read
+      if (more) read(next);                                  // (rows behind those that are written now)
+      write(i0, t);
+      if (!more) break;
+      t = next;
     }
-#pragma unroll
-    for (int u = 0; u < kMoveU; ++u) {
-      const int i = i0 + u * rows + (int)threadIdx.x / pieces;
-      bool there = false;
-      if (from[u] < 0 || (kInPlace && from[u] == i)) continue;
-      u32x4* const at = address(to, i, &there);
-      if (there) *at = x[u];
-    }
-    if (kInPlace) __syncthreads();
   }
 }
 
 hipError_t launch_evict(const Shape& s, int dtype, const KvView& kv, const float* mass, const int32_t* budget, int n_sink, int n_recent, const KvView* to,
                         float* mass_out, int32_t* kept, int32_t* lens_out, hipStream_t st) {
   const int e = dtype == LFPS_F32 ? 4 : 2, k_bytes = kv.k_fp8 ? 1 : e, v_bytes = kv.v_fp8 ? 1 : e;
-  hipLaunchKernelGGL(k_evict_plan, dim3((unsigned)(s.B * s.Hkv)), dim3(kPlanThreads), 0, st, s, kv.seq_lens, mass, budget, n_sink, n_recent, mass_out, kept,
-                     lens_out);
+  const int groups = s.B * s.Hkv, pieces = kD * (k_bytes < v_bytes ? k_bytes : v_bytes) / 16;
+  const int shares = groups <= 64 ? 4 : (groups <= 128 ? 2 : 1);
+  hipLaunchKernelGGL(k_evict_plan, dim3((unsigned)groups, (unsigned)shares), dim3(kPlanThreads), 0, st, s, kv.seq_lens, mass, budget, n_sink, n_recent, mass_out, kept, lens_out);
   if (!to) {
-    const dim3 grid((unsigned)(kD * (k_bytes + v_bytes) / 64), (unsigned)(s.B * s.Hkv));
-    hipLaunchKernelGGL((k_evict_move<true>), grid, dim3(kMoveThreads), 0, st, s, kv, kv, k_bytes, v_bytes, budget, kept);
+    int slice = 4;                                           // the widest slices that give every CU a workgroup
+    while (slice < pieces && (int64_t)groups * kD * (k_bytes + v_bytes) / 16 / (2 * slice) >= 256) slice *= 2;
+    const dim3 grid((unsigned)groups, (unsigned)(kD * (k_bytes + v_bytes) / 16 / slice));
+    hipLaunchKernelGGL((k_evict_move<true, 1024>), grid, dim3(1024), 0, st, s, kv, kv, k_bytes, v_bytes, slice, budget, kept);
   } else {
-    const dim3 grid((unsigned)((s.Lcap + 255) / 256 < 64 ? (s.Lcap + 255) / 256 : 64), (unsigned)(s.B * s.Hkv), 2);
-    hipLaunchKernelGGL((k_evict_move<false>), grid, dim3(kMoveThreads), 0, st, s, kv, *to, k_bytes, v_bytes, budget, kept);
+    const int step = 256 / pieces * kMoveU;
+    const dim3 grid((unsigned)groups, (unsigned)(kD * (k_bytes + v_bytes) / 16 / pieces), (unsigned)((s.Lcap + step - 1) / step));
+    hipLaunchKernelGGL((k_evict_move<false, 256>), grid, dim3(256), 0, st, s, kv, *to, k_bytes, v_bytes, pieces, budget, kept);
   }
   return hipGetLastError();
 }
