@@ -15,6 +15,7 @@ namespace {
 
 constexpr int kPlanThreads = 1024, kPlanWaves = kPlanThreads / 64, kBins = 2048;
 constexpr int kPlanEach = 32, kPlanChunk = kPlanThreads * kPlanEach;       // weights of a thread; rows of the workgroup at a time
+constexpr int kPlanBatch = 8;
 constexpr int kMoveU = 8;                              // pieces of 16 bytes that a thread has on its way
 
 __device__ __forceinline__ uint32_t weight_key(float x) { return x != x ? 1u : f2key(x + 0.f); }      // (-0 is 0; a NaN below all numbers)
@@ -45,28 +46,32 @@ __global__ __launch_bounds__(kPlanThreads) void k_evict_plan(Shape s, const int3
   uint32_t key[kPlanEach];
   auto row = [&](int c, int i) { return c * kPlanChunk + (wave * each + i) * 64 + lane; };
   auto weight = [&](int r) { return w[r < cut.n ? r : cut.n - 1]; };
-  // (a count that the compiler cannot know again: 32 comparisons with `each`, kept for every loop, do not fit the scalar registers)
-  auto fresh = [&] {
+  // f(i) for all i below `each` and some behind, whose keys are 0, in batches: a taken branch for every further i took longer than most f.
+  // (The count is one that the compiler cannot know again: comparisons with it, kept for every loop, would fill the scalar registers.)
+  auto batches = [&](auto f) __attribute__((always_inline)) {
     int e = each;
     asm volatile("" : "+s"(e));
-    return e;
+#pragma unroll
+    for (int i0 = 0; i0 < kPlanEach; i0 += kPlanBatch)
+      if (i0 < e) f(i0);
   };
   auto fetch = [&](int c) __attribute__((always_inline)) {
-    const int e0 = fresh();
+    batches([&](int i0) __attribute__((always_inline)) {
 #pragma unroll
-    for (int i = 0; i < kPlanEach; ++i)
-      if (i < e0) key[i] = __float_as_uint(weight(row(c, i)));
-    const int e1 = fresh();
+      for (int i = i0; i < i0 + kPlanBatch; ++i) key[i] = __float_as_uint(weight(row(c, i)));
+    });
+    batches([&](int i0) __attribute__((always_inline)) {
 #pragma unroll
-    for (int i = 0; i < kPlanEach; ++i)
-      if (i < e1) {
-        key[i] = weight_key(__uint_as_float(key[i]));
-        const int r0 = row(c, i) - lane;
-        if (r0 < cut.sinks || r0 + 64 > cut.last) {
-          const int r = r0 + lane;
-          key[i] = r >= cut.n ? 0u : (r < cut.sinks || r >= cut.last ? 0xFFFFFFFFu : key[i]);
+      for (int i = i0; i < i0 + kPlanBatch; ++i) key[i] = weight_key(__uint_as_float(key[i]));
+      const int r0 = row(c, i0) - lane;
+      if (r0 < cut.sinks || r0 + 64 * kPlanBatch > cut.last || i0 + kPlanBatch > each) {
+#pragma unroll
+        for (int i = i0; i < i0 + kPlanBatch; ++i) {
+          const int r = row(c, i);
+          key[i] = r >= cut.n || i >= each ? 0u : (r < cut.sinks || r >= cut.last ? 0xFFFFFFFFu : key[i]);
         }
       }
+    });
   };
   if (chunks == 1) fetch(0);
   // the key at the cut, from its highest bits down: `least` is its bits so far, `left` how many of those that have these bits are kept
@@ -82,10 +87,20 @@ __global__ __launch_bounds__(kPlanThreads) void k_evict_plan(Shape s, const int3
       __syncthreads();
       for (int c = 0; c < chunks; ++c) {
         if (chunks > 1) fetch(c);
-        const int e = fresh();
+        const uint32_t mask = (1 << bits) - 1;
+        if (pass == 0) {
+          batches([&](int i0) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < kPlanEach; ++i)
-          if (i < e && (pass == 0 || key[i] >> before == least >> before)) atomicAdd(&bins[(key[i] >> shift) & ((1 << bits) - 1)], 1);
+            for (int i = i0; i < i0 + kPlanBatch; ++i)
+              if (key[i]) atomicAdd(&bins[key[i] >> 21], 1);         // (64 additions to one place are one after the other)
+          });
+        } else {
+          batches([&](int i0) __attribute__((always_inline)) {
+#pragma unroll
+            for (int i = i0; i < i0 + kPlanBatch; ++i)
+              if ((key[i] ^ least) >> before == 0) atomicAdd(&bins[(key[i] >> shift) & mask], 1);
+          });
+        }
       }
       __syncthreads();
       // thread t has the t-th highest bin or two: those above them come from the threads before
@@ -112,16 +127,16 @@ __global__ __launch_bounds__(kPlanThreads) void k_evict_plan(Shape s, const int3
   for (int c = 0; c < chunks; ++c) {
     if (chunks > 1) fetch(c);
     // of my wave's rows: kept whatever else is, and in the upper half those at the cut (at most 2048 of either); and of those before my part
-    const int part0 = each * (int)blockIdx.y / (int)gridDim.y, part1 = each * ((int)blockIdx.y + 1) / (int)gridDim.y, e = fresh();
+    const int all_batches = (each + kPlanBatch - 1) / kPlanBatch;
+    const int part0 = all_batches * (int)blockIdx.y / (int)gridDim.y * kPlanBatch, part1 = all_batches * ((int)blockIdx.y + 1) / (int)gridDim.y * kPlanBatch;
     int mine = 0, early = 0;
+    batches([&](int i0) __attribute__((always_inline)) {
+      early = i0 == part0 ? mine : early;
 #pragma unroll
-    for (int i = 0; i < kPlanEach; ++i)
-      if (i < e) {
-        early = i == part0 ? mine : early;
-        mine += key[i] > least ? 1 : (key[i] == least ? 1 << 16 : 0);
-      }
+      for (int i = i0; i < i0 + kPlanBatch; ++i) mine += key[i] > least ? 1 : (key[i] == least ? 1 << 16 : 0);
+    });
     mine = wave_inclusive_sum(mine);
-    early = __builtin_amdgcn_readlane(wave_inclusive_sum(part0 < each ? early : 0), 63);
+    early = __builtin_amdgcn_readlane(wave_inclusive_sum(early), 63);
     if (lane == 63) {
       sums[wave][0] = mine & 0xFFFF;
       sums[wave][1] = mine >> 16;
@@ -141,16 +156,13 @@ __global__ __launch_bounds__(kPlanThreads) void k_evict_plan(Shape s, const int3
     int32_t* const to = kept + (int64_t)bg * s.Lcap;
     float* const to_mass = mass_out + (int64_t)bg * s.Lcap;
     auto rank = [](uint64_t mask) { return (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0)); };
-    constexpr int kBatch = 8;
+    batches([&](int i0) __attribute__((always_inline)) {
+      if (i0 < part0 || i0 >= part1) return;
+      float x[kPlanBatch];
 #pragma unroll
-    for (int i0 = 0; i0 < kPlanEach; i0 += kBatch) {
-      if (i0 + kBatch <= part0 || i0 >= part1) continue;
-      float x[kBatch];
+      for (int i = 0; i < kPlanBatch; ++i) x[i] = weight(row(c, i0 + i));
 #pragma unroll
-      for (int i = 0; i < kBatch; ++i) x[i] = weight(row(c, i0 + i));
-#pragma unroll
-      for (int i = 0; i < kBatch; ++i) {
-        if (i0 + i < part0 || i0 + i >= part1) continue;
+      for (int i = 0; i < kPlanBatch; ++i) {
         const uint32_t k = key[i0 + i];
         const uint64_t same = __ballot(k == least);
         bool keep = k > least;
@@ -164,7 +176,7 @@ __global__ __launch_bounds__(kPlanThreads) void k_evict_plan(Shape s, const int3
         equals += __popcll(same);
         place += __popcll(all);
       }
-    }
+    });
     const int equals_after = equals_before + all_equal;
     base += all_sure + (equals_after < left ? equals_after : left) - (equals_before < left ? equals_before : left);
     equals_before = equals_after;
