@@ -125,15 +125,22 @@ __device__ __forceinline__ void prompt_pipe(char* lds, const PromptArgs<TQ, See>
   PipeState<Op> st;
   st.clear();
   st.limit = seen(token);
+  lds_char* room = (lds_char*)lds + wave * (kPipeLds / kPipeWaves & ~15);
   if (lo < hi) {
     st.q.load(a.q + (int64_t)(c0 + token) * a.q_stride + head * kD, h);
     const CacheRows<TK> K(a.kv.k, a.kv, b, g);
     const CacheRows<TV> V(a.kv.v, a.kv, b, g);
-    pipe_loop<kKind, TK, TV>(lds, K, V, lo, hi, seen(row0 >> shift), row0 + 32 * wave < rows, st, walk);
+    room = pipe_loop<kKind, TK, TV>(lds, K, V, lo, hi, seen(row0 >> shift), row0 + 32 * wave < rows, st, walk);
   }
-  if (!valid) return;
-  if (a.splits > 1) st.finish((TQ*)nullptr, a.part + (part_row(a, false, 0, b, c0, token, head) + split) * kPartFloats, h);
-  else st.finish(a.out + ((int64_t)(c0 + token) * s.Hq + head) * kD, nullptr, h);
+  if (a.splits > 1) {
+    if (valid) st.finish((TQ*)nullptr, a.part + (part_row(a, false, 0, b, c0, token, head) + split) * kPartFloats, h);
+    return;
+  }
+  const int first = row0 + 32 * wave;
+  st.template finish_rows<TQ>(room, [&](int i) {
+    const int x = first + i;
+    return x < rows ? a.out + ((int64_t)(c0 + (x >> shift)) * s.Hq + g * G + (x & (G - 1))) * kD : nullptr;
+  });
 }
 
 }  // namespace

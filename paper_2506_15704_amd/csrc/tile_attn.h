@@ -52,7 +52,6 @@ struct AllRows {
   __device__ __forceinline__ int row(int k) const { return k; }
   __device__ __forceinline__ int end(int e) const { return e; }
   __device__ __forceinline__ int steps(int e) const { return e; }
-  __device__ __forceinline__ bool hides(int) const { return false; }
   // is key `key` of those from row `base` on seen by a query row of this limit?
   __device__ __forceinline__ auto seen_from(int base, int limit) const {
     return [seen = limit - base](int key) { return key < seen; };
@@ -64,9 +63,10 @@ struct GapRows {
   __device__ __forceinline__ int row(int k) const { return k < at ? k : k + by; }
   __device__ __forceinline__ int end(int e) const { return e > at ? e + by : e; }      // of the cache's rows, for a walk that ends at e
   __device__ __forceinline__ int steps(int e) const { return e - by; }                 // and the other way round, e > at + by
-  __device__ __forceinline__ bool hides(int j) const { return j < from && j >= sinks; }
-  __device__ __forceinline__ auto seen_from(int base, int limit) const {
-    return [seen = limit - base, first = sinks - base, begin = from - base](int key) { return key < seen && (key >= begin || key < first); };
+  __device__ __forceinline__ auto seen_from(int base, int limit) const {        // (no branches: a key's place in the gap is one unsigned comparison)
+    return [seen = limit - base, first = sinks - base, gap = (uint32_t)(from > sinks ? from - sinks : 0)](int key) {
+      return (bool)((int)(key < seen) & (int)((uint32_t)(key - first) >= gap));
+    };
   }
 };
 
@@ -253,17 +253,17 @@ struct QueryTile<float, kTerms> {
 // by key, by the rows that see the key.
 template <typename Op>
 __device__ __forceinline__ bool any_not_finite(const lds_char* rows, int bytes) {
-  constexpr uint32_t kExp = std::is_same<Op, float>::value ? 0x7F800000u : (std::is_same<Op, f16x8>::value ? 0x7C00u : 0x7F80u);
-  bool found = false;
+  // One more than an exponent of ones is a carry into the sign's place.
+  constexpr bool kF32 = std::is_same<Op, float>::value, kF16 = std::is_same<Op, f16x8>::value;
+  constexpr uint32_t kExp = kF32 ? 0x7F800000u : (kF16 ? 0x7C007C00u : 0x7F807F80u), kOne = kF32 ? 0x00800000u : (kF16 ? 0x04000400u : 0x00800080u);
+  uint32_t carries = 0;
+#pragma unroll 4
   for (int at = 16 * (threadIdx.x & 63); at < bytes; at += 1024) {
     const u32x4 x = *(const __attribute__((address_space(3))) u32x4*)(rows + at);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      found |= (x[i] & kExp) == kExp;
-      if constexpr (!std::is_same<Op, float>::value) found |= ((x[i] >> 16) & kExp) == kExp;
-    }
+    for (int i = 0; i < 4; ++i) carries |= (x[i] & kExp) + kOne;
   }
-  return __ballot(found) != 0;
+  return __ballot((carries & (kF32 ? 0x80000000u : 0x80008000u)) != 0) != 0;
 }
 // o += weights of `keys` keys (a multiple of 32) times their values at v, key by key on the vector units, of keys that the row sees(key).
 // weight(i, half): my weight of the i-th of the keys that that half of the wave holds.  Slow, and small: almost no call comes here.
@@ -371,13 +371,13 @@ struct RowState {
   __device__ __forceinline__ void step(f32x16 (&s)[kBlocks], const char* v, float unit, int first, int limit, bool masked, int lane, const Rows& rows) {
     const int h = lane >> 5;
     float mx = m;
+    const auto sees = rows.seen_from(first + 4 * h, limit);
 #pragma unroll
     for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         s[b][r] *= unit;
-        const int j = first + 32 * b + 8 * (r / 4) + 4 * h + r % 4;
-        if (masked && (j >= limit || rows.hides(j))) s[b][r] = -INFINITY;
+        if (masked) s[b][r] = sees(32 * b + 8 * (r / 4) + r % 4) ? s[b][r] : -INFINITY;
         mx = fmaxf(mx, s[b][r]);
       }
     mx = fmaxf(mx, __shfl_xor(mx, 32));

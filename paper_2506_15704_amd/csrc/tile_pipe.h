@@ -189,13 +189,11 @@ struct PipeState {
   // Scores of keys that the row does not see.
   template <typename Rows>
   __device__ __forceinline__ void hide(f32x16 (&s)[2], int first, int h, const Rows& rows) const {
+    const auto sees = rows.seen_from(first + 4 * h, limit);
 #pragma unroll
     for (int b = 0; b < 2; ++b)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const int j = first + 32 * b + 8 * (r / 4) + 4 * h + r % 4;
-        if (j >= limit || rows.hides(j)) s[b][r] = -INFINITY;
-      }
+      for (int r = 0; r < 16; ++r) s[b][r] = sees(32 * b + 8 * (r / 4) + r % 4) ? s[b][r] : -INFINITY;
   }
   __device__ __forceinline__ static float largest(const f32x16 (&s)[2]) {
     float mx[4];
@@ -250,6 +248,30 @@ struct PipeState {
       }
     }
   }
+  // The results of the wave's 32 rows by way of 8 KB of LDS, so that a store is four whole rows: to(i) is where the wave's row i goes, nullptr:
+  // nowhere.  (Straight from the registers a store is 16 bytes of 32 rows each, and took the last 3 us of a workgroup.)
+  template <typename TO, typename To>
+  __device__ __forceinline__ void finish_rows(lds_char* room, To to) const {
+    static_assert(sizeof(TO) == 2, "");
+    const int lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5;
+    const float half = (l[0] + l[1]) + (l[2] + l[3]), sum = half + __shfl_xor(half, 32), inv = sum == 0.f ? 0.f : 1.f / sum;
+    typedef typename std::conditional<std::is_same<TO, uint16_t>::value, __bf16, _Float16>::type Elem;
+    typedef Elem Elem4 __attribute__((ext_vector_type(4)));
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; r += 4) {
+        const f32x4 y = {o[d][r] * inv, o[d][r + 1] * inv, o[d][r + 2] * inv, o[d][r + 3] * inv};
+        *(__attribute__((address_space(3))) Elem4*)(room + n * 256 + 16 * chunk_place(n, 4 * d + r / 4) + 8 * h) = __builtin_convertvector(y, Elem4);
+      }
+    wave_lds_order();
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int i = 4 * j + (lane >> 4);
+      TO* const p = to(i);
+      if (p) *reinterpret_cast<u32x4*>(p + 8 * (lane & 15)) = *(const __attribute__((address_space(3))) u32x4*)(room + i * 256 + 16 * chunk_place(i, lane & 15));
+    }
+  }
   // The row's result, or with part != nullptr a part of it.  The lanes of a row's two halves call together.
   template <typename TO>
   __device__ __forceinline__ void finish(TO* out, float* part, int h) const {
@@ -288,9 +310,10 @@ template <typename Op, int kTerms>
 constexpr int pipe_lds() { return PipeState<Op, kTerms>::kRest ? kRestAt + kPipeWaves * kRestWave : kPipeLds; }
 // least: keys that all rows of the workgroup see.
 // active: the wave has rows of its own; one that has none only brings its share of the cache's.
+// Returns 8 KB of LDS that are the wave's from then on: of the four stages that nothing is on its way to any more.
 // rows: the cache's rows that [first, end) stand for (a gap lies between stages).
 template <int kKind, typename TK, typename TV, typename Op, int kTerms, typename Rows = AllRows>
-__device__ __forceinline__ void pipe_loop(char* lds_, const CacheRows<TK>& K, const CacheRows<TV>& V, int first, int end, int least, bool active,
+__device__ __forceinline__ lds_char* pipe_loop(char* lds_, const CacheRows<TK>& K, const CacheRows<TV>& V, int first, int end, int least, bool active,
                                           PipeState<Op, kTerms>& st, const Rows& rows = Rows()) {
   lds_char* const lds = (lds_char*)lds_;
   const int lane = threadIdx.x & 63, wave = wave_of(), n = lane & 31, h = lane >> 5;
@@ -314,6 +337,7 @@ __device__ __forceinline__ void pipe_loop(char* lds_, const CacheRows<TK>& K, co
     const int k = first + i * kPipeKeys, e = uniform(e_first[i]);
     fk.aim(K, row_of(k), row_end, e, lane);
     fk.ask(lds + i * kPipeStage, wave);
+    __builtin_amdgcn_sched_barrier(0);
     fk.put(lds + i * kPipeStage, lane, wave);
     if (i < 2) {
       fv.aim(V, row_of(k), row_end, e, lane);
@@ -321,7 +345,9 @@ __device__ __forceinline__ void pipe_loop(char* lds_, const CacheRows<TK>& K, co
       fv.put(lds + kV + i * kPipeStage, lane, wave);
     }
   }
-  landed();
+  // (what is asked for first, K of the first stage, is what the first products wait for)
+  constexpr int kBehind = Feed<TK, kKind, Op>::kDirect && Feed<TV, kKind, Op>::kDirect ? 2 * Feed<TK, kKind, Op>::kLoads + 2 * Feed<TV, kKind, Op>::kLoads : 0;
+  __builtin_amdgcn_s_waitcnt(0x0f70 | kBehind);      // vmcnt(kBehind)
   __syncthreads();
   f32x16 s[2];                                // scores of a stage
   constexpr int kAhead = kTerms == 1 ? 2 : 1, kOperands = kAhead + 1;      // groups read ahead (of two terms a group is twice as long)
@@ -332,7 +358,10 @@ __device__ __forceinline__ void pipe_loop(char* lds_, const CacheRows<TK>& K, co
     st.add_scores(s, a[0], g, rest);
   }
   __syncthreads();                            // (K of the first stage has been read)
-  if (late) __syncthreads();
+  if (late) {
+    landed();
+    __syncthreads();
+  }
   int k0 = first, now = 0, next = kPipeStage, last = 2 * kPipeStage;      // places of this stage, the next, the one after
   auto stage = [&](auto masked, auto works) {
     constexpr bool kMasked = decltype(masked)::value, kWorks = decltype(works)::value;
@@ -411,6 +440,9 @@ __device__ __forceinline__ void pipe_loop(char* lds_, const CacheRows<TK>& K, co
     while (k0 < end) stage(yes, no);
   }
   if (!late) __syncthreads();
+  // (the last stage has asked for rows of K into what is now the last stage, and of V into the next)
+  const int of_wave[4] = {now, next, kV + now, kV + last};
+  return lds + (wave < 2 ? of_wave[0] : (wave < 4 ? of_wave[1] : (wave < 6 ? of_wave[2] : of_wave[3]))) + (wave & 1) * (kPipeStage / 2);
 }
 
 }  // namespace lfps
