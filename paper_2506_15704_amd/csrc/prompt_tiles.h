@@ -20,11 +20,11 @@ struct SeesWindow {
     const int f = p + 1 > window ? p + 1 - window : 0;
     return f <= n_sink ? 0 : f;
   }
-  // for a tile of tokens at rows first .. last, of which mine is at p: whole stages of the first rows, then those from the first window's on
+  // for a tile of tokens at rows first .. last, of which mine is at p: the first rows, then those from the first window's on, in eights
   __device__ __forceinline__ GapRows walk(int first, int last, int p) const {
-    const int lo = from(first) & ~63, sinks = n_sink < lo ? n_sink : lo, at = (sinks + 63) & ~63, by = lo - at;
-    const int all = ((from(last) + 63) & ~63) - by;
-    return {at, by, from(last) == 0 ? 0 : (all > at ? all : at), n_sink, from(p)};
+    const int lo = from(first) & ~7, sinks = n_sink < lo ? n_sink : lo, at = (sinks + 7) & ~7, by = lo - at;
+    const int all = from(last) - by;
+    return {at, by, from(last) == 0 ? 0 : (all > at ? all : at), n_sink, from(p) - by};
   }
   // rows that a tile of `tokens` walks at most
   __host__ int most(int cap, int tokens) const {
@@ -82,9 +82,9 @@ __device__ __forceinline__ void prompt_tile(char* lds, const PromptArgs<TQ, See>
   const bool valid = m < rows;
   m = valid ? m : rows - 1;
   const int token = m >> shift, head = g * G + (m & (G - 1));
-  const int limit = valid ? seen(token) : 0;
   const int last = (row0 + 32 * kRowWaves < rows ? row0 + 32 * kRowWaves : rows) - 1;
   const auto walk = a.see.walk(seen(row0 >> shift) - 1, seen(last >> shift) - 1, seen(token) - 1);
+  const int limit = valid ? walk.steps(seen(token)) : 0;
   int lo, hi;
   split_rows(0, walk.steps(seen(last >> shift)), splits, split, tile_rows(kKeyWaves), &lo, &hi);
   RowState<Op, 1> st;
@@ -124,13 +124,13 @@ __device__ __forceinline__ void prompt_pipe(char* lds, const PromptArgs<TQ, See>
   split_rows(0, walk.steps(seen(last >> shift)), a.splits, split, kPipeKeys, &lo, &hi);
   PipeState<Op> st;
   st.clear();
-  st.limit = seen(token);
+  st.limit = walk.steps(seen(token));
   lds_char* room = (lds_char*)lds + wave * (kPipeLds / kPipeWaves & ~15);
   if (lo < hi) {
     st.q.load(a.q + (int64_t)(c0 + token) * a.q_stride + head * kD, h);
     const CacheRows<TK> K(a.kv.k, a.kv, b, g);
     const CacheRows<TV> V(a.kv.v, a.kv, b, g);
-    room = pipe_loop<kKind, TK, TV>(lds, K, V, lo, hi, seen(row0 >> shift), row0 + 32 * wave < rows, st, walk);
+    room = pipe_loop<kKind, TK, TV>(lds, K, V, lo, hi, walk.steps(seen(row0 >> shift)), row0 + 32 * wave < rows, st, walk);
   }
   if (a.splits > 1) {
     if (valid) st.finish((TQ*)nullptr, a.part + (part_row(a, false, 0, b, c0, token, head) + split) * kPartFloats, h);

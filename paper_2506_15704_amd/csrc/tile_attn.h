@@ -44,9 +44,9 @@ struct CacheRows {
 };
 
 // ---- the rows that a loop walks --------------------------------------------------------------------------------
-// All of a range, in which a query row sees those below its limit; or a range with a gap: from row `at` of the walk on, it has the cache's rows
-// `by` further up, and a query row does not see the cache's rows [sinks, from) either.  clear: row of the walk from which on no query
-// row of the workgroup misses one for its window.
+// All of a range, in which a query row sees those below its limit; or a range with a gap: from row `at` of the walk on (a multiple of eight), it has
+// the cache's rows `by` further up.  All else is counted along the walk: a query row does not see its rows [sinks, from) either, and from `clear` on
+// none of the workgroup's misses one for its window.
 struct AllRows {
   static constexpr bool kGap = false;
   __device__ __forceinline__ int row(int k) const { return k; }
@@ -490,7 +490,7 @@ __device__ __forceinline__ void tile_loop(char* lds, const CacheRows<TK>& K, con
   }
   most = __builtin_amdgcn_readfirstlane(most);
   least = __builtin_amdgcn_readfirstlane(least);
-  int begun = 0;                              // the row from which on none of my wave's misses one for its window
+  int begun = 0;                              // from there on none of my wave's rows misses one for its window
   if constexpr (Rows::kGap) {
     begun = rows.from;
 #pragma unroll
@@ -544,7 +544,7 @@ __device__ __forceinline__ void tile_loop(char* lds, const CacheRows<TK>& K, con
     const char* v = lds + at + kStageK + mine * InLds<TV>::kRowBytes;
 #pragma unroll
     for (int b = 0; b < kBlocks; ++b) {
-      const int k_mine = rows.row(k0 + mine + 32 * b);
+      const int k_mine = k0 + mine + 32 * b;
       if (k_mine < most) {
         f32x16 s[1] = {RowState<Op, kTerms>::scores(k + 32 * b * InLds<TK>::kRowBytes, q, n, h)};
         st.template step<1>(s, v + 32 * b * InLds<TV>::kRowBytes, q.unit, k_mine, limit, k_mine + 32 > least || (Rows::kGap && k_mine < begun), lane, rows);

@@ -81,9 +81,8 @@ struct Feed {
     }
   }
 };
-// The first row that a wave brings of the stage at k0: one that exists.
-__device__ __forceinline__ int first_row(int k0, int end, int wave) {
-  const int w0 = k0 + kFeedRows * wave;
+// The first row that a wave brings of a stage, given where it would be: one that exists.
+__device__ __forceinline__ int first_row(int w0, int end) {
   return __builtin_amdgcn_readfirstlane(w0 < end ? w0 : (end - 1) & ~(kFeedRows - 1));
 }
 
@@ -311,7 +310,7 @@ constexpr int pipe_lds() { return PipeState<Op, kTerms>::kRest ? kRestAt + kPipe
 // least: keys that all rows of the workgroup see.
 // active: the wave has rows of its own; one that has none only brings its share of the cache's.
 // Returns 8 KB of LDS that are the wave's from then on: of the four stages that nothing is on its way to any more.
-// rows: the cache's rows that [first, end) stand for (a gap lies between stages).
+// rows: the cache's rows that [first, end) stand for.
 template <int kKind, typename TK, typename TV, typename Op, int kTerms, typename Rows = AllRows>
 __device__ __forceinline__ lds_char* pipe_loop(char* lds_, const CacheRows<TK>& K, const CacheRows<TV>& V, int first, int end, int least, bool active,
                                           PipeState<Op, kTerms>& st, const Rows& rows = Rows()) {
@@ -322,7 +321,7 @@ __device__ __forceinline__ lds_char* pipe_loop(char* lds_, const CacheRows<TK>& 
   Feed<TV, kKind, Op> fv;
   constexpr int kV = kPipeStages * kPipeStage;
   const int row_end = rows.end(end);
-  auto row_of = [&](int k) { return first_row(rows.row(k), row_end, wave); };
+  auto row_of = [&](int k) { return first_row(rows.row(k + kFeedRows * wave), row_end); };
   auto look_up = [&](int k) { return kKind == kPages ? RowMap<true>::block(K.pg, K.b, row_of(k)) : 0; };
   auto uniform = [](int e) { return __builtin_amdgcn_readfirstlane(e); };
   constexpr bool kRest = PipeState<Op, kTerms>::kRest;
@@ -367,7 +366,7 @@ __device__ __forceinline__ lds_char* pipe_loop(char* lds_, const CacheRows<TK>& 
     constexpr bool kMasked = decltype(masked)::value, kWorks = decltype(works)::value;
     // vector half
     if constexpr (kWorks) {
-      if (kMasked) st.hide(s, rows.row(k0), h, rows);
+      if (kMasked) st.hide(s, k0, h, rows);
       st.follow(st.largest(s));
       const float at = st.m == -INFINITY ? 0.f : st.m - (PipeState<Op, kTerms>::kLift);
 #pragma unroll
@@ -399,7 +398,7 @@ __device__ __forceinline__ lds_char* pipe_loop(char* lds_, const CacheRows<TK>& 
     // matrix half
     if constexpr (kWorks) {
       if (kMasked && !kRest) apart = *(volatile int*)found == k0 + kPipeKeys;
-      if (apart) st.add_values_apart(w, s, v, lane, rows.seen_from(rows.row(k0), st.limit));
+      if (apart) st.add_values_apart(w, s, v, lane, rows.seen_from(k0, st.limit));
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         __builtin_amdgcn_sched_barrier(0);
@@ -431,12 +430,12 @@ __device__ __forceinline__ lds_char* pipe_loop(char* lds_, const CacheRows<TK>& 
   if (active) {
     if constexpr (Rows::kGap)
       while (k0 < rows.clear && k0 < end) stage(yes, yes);
-    while (rows.row(k0) + kPipeKeys <= least && k0 < end) stage(no, yes);
+    while (k0 + kPipeKeys <= least && k0 < end) stage(no, yes);
     while (k0 < end) stage(yes, yes);
   } else {
     if constexpr (Rows::kGap)
       while (k0 < rows.clear && k0 < end) stage(yes, no);
-    while (rows.row(k0) + kPipeKeys <= least && k0 < end) stage(no, no);
+    while (k0 + kPipeKeys <= least && k0 < end) stage(no, no);
     while (k0 < end) stage(yes, no);
   }
   if (!late) __syncthreads();
