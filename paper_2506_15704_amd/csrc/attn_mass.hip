@@ -135,8 +135,8 @@ __device__ __forceinline__ int launch_tokens(const A& a, int b, int* c0, int* c1
 
 // grid Hkv * splits * tiles (of kRows query rows; at most T G / rows + B), the latest rows first: they see most.
 // Stage j of keys is in LDS slot j % 4.  While a wave's weights of 32 keys are made, the products of the next 32 run; when the last 32 of stage j - 1
-// are, a barrier says that nobody reads its slot any more and that stage j is there, and stage j + 3 is asked for (FP8: comes from registers, and
-// j + 4 is asked for).
+// are, a barrier says that nobody reads its slot any more and that stage j is there, and stage j + 3 is asked for (FP8: it comes from registers when
+// its turn is next but one).
 // kBlocks: blocks of 32 rows of a wave.  Where the requests have no more than 128 query rows each, one block gives all four waves some: 32 tokens of
 // 32 heads over 32768 rows 25 -> 21 us.
 template <typename TK, typename TQ, int kBlocks>

@@ -24,6 +24,15 @@ __device__ __forceinline__ void window_rows(const WindowRows& w, int n, int* at,
   *by = lo - *at;
   *count = n - *by;
 }
+// The shape with the rows that a kernel takes of a request at most.
+template <typename... Own>
+__host__ __device__ __forceinline__ Shape walked(const Shape& s, const Own&...) { return s; }
+__host__ __device__ __forceinline__ Shape walked(const Shape& s, const WindowRows& w) {
+  const int64_t most = (int64_t)w.window + w.n_sink;
+  Shape fewer = s;
+  fewer.Lcap = most < s.Lcap ? (int)most : s.Lcap;
+  return fewer;
+}
 __device__ __forceinline__ RowsOf rows_of_block(const Shape& s, const int32_t* seq_lens, int n_split) {
   const int bg = blockIdx.y, b = bg / s.Hkv, split = blockIdx.x;
   int n = seq_lens[b];
@@ -150,7 +159,7 @@ __global__ __launch_bounds__(kAttnThreads, attn_waves<Own...>()) void k_full_att
   const RowsOf here = rows_of_block(s, seq_lens, n_split, own...);
   const int b = here.b, g = here.g, r_begin = here.begin, r_end = here.end;
   if (r_begin >= r_end) return;
-  const bool once_here = kMayOnce && outgrow_cache(s, held_rows(s, seq_lens), kD * (int)(sizeof(TK) + sizeof(T)), kKeptStreamBytes);
+  const bool once_here = kMayOnce && outgrow_cache(s, held_rows(walked(s, own...), seq_lens), kD * (int)(sizeof(TK) + sizeof(T)), kKeptStreamBytes);
 
   float qr[G][8];
 #pragma unroll
@@ -338,7 +347,7 @@ __global__ __launch_bounds__(kAttnThreads) void k_full_attn_single(Shape s, cons
   const RowsOf here = rows_of_block(s, seq_lens, n_split, own...);
   const int b = here.b, g = here.g, r_begin = here.begin, r_end = here.end;
   if (r_begin >= r_end) return;
-  const bool once_here = kMayOnce && outgrow_cache(s, held_rows(s, seq_lens), kD * (int)(sizeof(TK) + sizeof(T)), kKeptStreamBytes);
+  const bool once_here = kMayOnce && outgrow_cache(s, held_rows(walked(s, own...), seq_lens), kD * (int)(sizeof(TK) + sizeof(T)), kKeptStreamBytes);
 
   float qr[8];
 #pragma unroll

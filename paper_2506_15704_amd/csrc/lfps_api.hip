@@ -1031,6 +1031,11 @@ int lfps_prompt_attn(lfps_ctx* ctx, const void* q, int64_t stride_t, const int32
   return LFPS_OK;
 }
 
+static Span table_span(const lfps_ctx* ctx, const KvView& v) {
+  const int64_t entries = v.page.table ? (ctx->shape.Lcap + ((int64_t)1 << v.page.shift) - 1) >> v.page.shift : 0;
+  return {v.page.table, 4 * ((int64_t)(ctx->shape.B - 1) * v.page.table_stride + entries)};
+}
+
 int lfps_rotate_append(lfps_ctx* ctx, const lfps_rotary* rot, const void* q, const void* k_new, const void* v_new, int64_t stride_t,
                        const int32_t* positions, const int32_t* cu, int32_t n_tokens, const lfps_kv* kv, void* q_out, int32_t q_out_dtype, void* stream) {
   if (!ctx) return LFPS_EINVAL;
@@ -1059,7 +1064,11 @@ int lfps_rotate_append(lfps_ctx* ctx, const lfps_rotary* rot, const void* q, con
   const int64_t e = elem_bytes(ctx->cfg), before = e * (n_tokens - 1) * stride_t;
   const Span in_q = {q, before + e * s.Hq * kD}, in_k = {k_new, before + e * s.Hkv * kD}, in_v = {v_new, before + e * s.Hkv * kD};
   const Span out = {q_out, (int64_t)n_tokens * s.Hq * kD * (q_f32 ? 4 : e)};
-  if (overlap(out, in_q) || overlap(out, in_k) || overlap(out, in_v)) return fail(ctx, LFPS_EINVAL, "lfps_rotate_append: q_out overlaps an input");
+  const Span small[] = {{positions, 4 * (int64_t)rot->n_axes * n_tokens}, {cu, 4 * (int64_t)(s.B + 1)}, {v.seq_lens, 4 * (int64_t)s.B}, {rot->q_weight, 4 * kD},
+                        {rot->k_weight, 4 * kD}, {rot->inv_freq, 2 * (int64_t)rot->rotary_dim}, {rot->pair_axis, 2 * (int64_t)rot->rotary_dim}, table_span(ctx, v)};
+  bool bad = overlap(out, in_q) || overlap(out, in_k) || overlap(out, in_v);
+  for (const Span& x : small) bad = bad || overlap(out, x);
+  if (bad) return fail(ctx, LFPS_EINVAL, "lfps_rotate_append: q_out overlaps an input");
   const Rotary r = {rot->q_weight, rot->k_weight, rot->inv_freq, rot->pair_axis, rot->eps, rot->rotary_dim, rot->n_axes, rot->interleaved};
   const OnDevice on(ctx->cfg.device);
   hipStream_t st = (hipStream_t)stream;
@@ -1113,6 +1122,11 @@ int lfps_window_attn_decode(lfps_ctx* ctx, const float* q, const lfps_kv* kv, in
 }
 
 static Span mass_span(const lfps_ctx* ctx, const void* p) { return {p, 4 * (int64_t)ctx->shape.B * ctx->shape.Hkv * ctx->shape.Lcap}; }
+// Does mass share memory with an array that the call reads, beside its queries?
+static bool mass_over_input(const lfps_ctx* ctx, const float* mass, const KvView& v, const int32_t* held, const int32_t* cu) {
+  const Span m = mass_span(ctx, mass), lens = {v.seq_lens, 4 * (int64_t)ctx->shape.B};
+  return overlap(m, lens) || overlap(m, {held, lens.bytes}) || overlap(m, {cu, lens.bytes + 4}) || overlap(m, table_span(ctx, v));
+}
 
 int lfps_attn_mass(lfps_ctx* ctx, const void* q, int64_t stride_t, const int32_t* cu, int32_t n_tokens, const lfps_kv* kv, const int32_t* held,
                    float decay, float* mass, void* stream) {
@@ -1126,6 +1140,9 @@ int lfps_attn_mass(lfps_ctx* ctx, const void* q, int64_t stride_t, const int32_t
   if (rc != LFPS_OK) return rc;
   if (!(decay >= 0.f && decay <= 1.f)) return fail(ctx, LFPS_EINVAL, "lfps_attn_mass: decay must be in [0, 1]");
   if ((uintptr_t)mass % 16) return fail(ctx, LFPS_EINVAL, "lfps_attn_mass: mass must be 16-byte aligned");
+  const int64_t e = elem_bytes(ctx->cfg);
+  if ((n_tokens && overlap({q, e * ((n_tokens - 1) * stride_t + (int64_t)ctx->shape.Hq * kD)}, mass_span(ctx, mass))) || mass_over_input(ctx, mass, v, held, cu))
+    return fail(ctx, LFPS_EINVAL, "lfps_attn_mass: mass overlaps an input");
   const OnDevice on(ctx->cfg.device);
   hipStream_t st = (hipStream_t)stream;
   LAUNCH(ctx, LFPS_KERNEL_ATTN_MASS, st,
@@ -1145,7 +1162,7 @@ int lfps_full_attn_mass_decode(lfps_ctx* ctx, const float* q, const lfps_kv* kv,
     return fail(ctx, LFPS_EINVAL, "lfps_full_attn_mass_decode: q, out and mass must be 16-byte aligned");
   const Shape& s = ctx->shape;
   const Span in = {q, 4 * (int64_t)s.B * s.Hq * kD}, row = {out, in.bytes}, sums = mass_span(ctx, mass);
-  if (overlap(in, row) || overlap(in, sums) || overlap(row, sums)) return fail(ctx, LFPS_EINVAL, "lfps_full_attn_mass_decode: q, out and mass overlap");
+  if (overlap(in, row) || overlap(in, sums) || overlap(row, sums) || mass_over_input(ctx, mass, v, held, nullptr)) return fail(ctx, LFPS_EINVAL, "lfps_full_attn_mass_decode: q, out and mass overlap");
   const OnDevice on(ctx->cfg.device);
   hipStream_t st = (hipStream_t)stream;
   LAUNCH(ctx, LFPS_KERNEL_ATTN_MASS, st,
@@ -1166,8 +1183,7 @@ int lfps_evict(lfps_ctx* ctx, const lfps_kv* kv, const float* mass, const int32_
     return fail(ctx, LFPS_EINVAL, "lfps_evict: rows go to the cache that they come from (in place: to = NULL)");
   const int64_t B = ctx->shape.B;
   const Span out[] = {mass_span(ctx, mass_out), mass_span(ctx, kept), {lens_out, 4 * B}};
-  const int64_t entries = v.page.table ? (ctx->shape.Lcap + ((int64_t)1 << v.page.shift) - 1) >> v.page.shift : 0;
-  const Span in[] = {mass_span(ctx, mass), {budget, 4 * B}, {v.seq_lens, 4 * B}, {v.page.table, 4 * ((B - 1) * v.page.table_stride + entries)}};
+  const Span in[] = {mass_span(ctx, mass), {budget, 4 * B}, {v.seq_lens, 4 * B}, table_span(ctx, v), to ? table_span(ctx, w) : Span{nullptr, 0}};
   for (const Span& x : out) {
     for (const Span& y : in)
       if (overlap(x, y)) return fail(ctx, LFPS_EINVAL, "lfps_evict: an array that is written overlaps one that is read");

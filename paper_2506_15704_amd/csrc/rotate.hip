@@ -5,7 +5,8 @@
 //
 // An angle is reduced in 64 bits: position * frequency / 2 pi as a product and its rounding error, of which the nearest quarter turn is
 // taken off before it becomes fp32, so that a position of 2^24 is turned as exactly as one of 16; the sine and cosine of what is left, at
-// most pi / 4, are their Taylor sums.  A wave has a token, a lane a pair of it: the angles are made once and serve every head.
+// most pi / 4, are their Taylor sums.  A wave has a token's angles, made by a lane a pair, and serves eight or sixteen of its head rows; other
+// waves make them again.
 #include "stored_rows.h"
 #include "tile_attn.h"
 
@@ -150,7 +151,11 @@ static hipError_t rotate_t(const RotateArgs<TS>& a, hipStream_t st) {
 
 hipError_t launch_rotate_append(const Shape& s, int dtype, const KvView& kv, const Rotary& rot, const void* q, const void* k_new, const void* v_new,
                                 int64_t stride_t, const int32_t* positions, const int32_t* cu, int n_tokens, void* q_out, bool q_f32, hipStream_t st) {
-  const int blocks = (s.Hq + 2 * s.Hkv + 7) / 8, waves = blocks;
+  // A wave takes eight rows, or sixteen where that leaves as many waves as the chip holds (8192) and an element is not four bytes wide.  us by graphs,
+  // eight / sixteen, 32 + 16 heads: bf16 64 tokens 3.4 / 4.0, 1024 6.6 / 6.5, 2048 11.3 / 10.0, 4096 19.6 / 17.5, 16384 79.2 / 76.4; FP8 cache
+  // 2048 11.5 / 10.2, 16384 78 / 71.3; fp32 2048 18.0 / 18.0, 16384 147 / 153; all 48 rows: bf16 64 tokens 6.3, 4096 18.1, 16384 81.
+  const int blocks = (s.Hq + 2 * s.Hkv + 7) / 8;
+  const int waves = dtype != LFPS_F32 && (int64_t)n_tokens * blocks >= 8192 ? (blocks + 1) / 2 : blocks;
 #define LFPS_ROTATE(TS, TK, TV)                                                                                                   \
   do {                                                                                                                            \
     const RotateArgs<TS> a = {s, kv, rot, (const TS*)q, (const TS*)k_new, (const TS*)v_new, stride_t, positions, cu, n_tokens, waves, q_out}; \

@@ -114,6 +114,14 @@ def test_heads_and_requests(Hq, Hkv, news, lens, q_f32):
     c.ctx.close()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32", "fp8kv"])
+@pytest.mark.parametrize("Hq,Hkv,news,lens", [(32, 8, [1400, 2], [1405, 2]), (4, 2, [8192], [8192]), (9, 9, [2100], [2100])])
+def test_thousands_of_tokens(dtype, Hq, Hkv, news, lens):
+    c = CacheCase(dtype, Hq, Hkv, lens, 16, seed=Hq)
+    _run(c, news, 96, interleaved=Hq == 4, lead=1, extra=2)
+    c.ctx.close()
+
+
 @pytest.mark.parametrize("axes,interleaved", [(2, False), (3, False), (3, True), (8, False)])
 def test_positions_of_several_axes(axes, interleaved):
     c = CacheCase("bf16", 4, 2, [100, 9], 16, seed=axes)
