@@ -14,6 +14,7 @@ namespace lfps {
 namespace {
 
 constexpr int kMassThreads = 256, kMassWaves = kMassThreads / 64;
+constexpr int kMassChunk = 1024;                       // query rows that a workgroup of k_mass_add takes at least, if there are as many
 constexpr int kMassRing = 4;                           // stages of streamed rows in LDS
 constexpr float kMassLazy = 6.f;                       // growth of a maximum, in powers of two, that is let pass
 constexpr float kMassUnit = kLog2e * 0.08838834764831845f;      // from products to scores in powers of two
@@ -39,8 +40,8 @@ struct MassArgs {
   float* stats;                    // [Hkv, t1 - t0, G, 2] of a query row: its largest score in powers of two, the inverse of the sum of the weights from there
   float* split_stats;              // [splits, Hkv, t1 - t0, G, 2] of its parts, if there are several: the sums themselves
   int32_t splits;
-  int32_t chunk;                   // query rows of a request that a workgroup of k_mass_add takes
-  float* sums;                     // [chunks, B * Hkv, Lcap] what they leave, if there are several
+  int32_t chunks;                  // of the query rows of a request
+  float* sums;                     // [chunks, B * Hkv, Lcap] what the chunks of query rows leave for the rows that they see, if there are several
   float* mass;
 };
 
@@ -318,9 +319,20 @@ __global__ __launch_bounds__(256) void k_mass_join(const float* __restrict__ spl
   reinterpret_cast<f32x2t*>(stats)[row] = f32x2t{mx == -INFINITY ? 0.f : mx, sum == 0.f ? 0.f : 1.f / sum};
 }
 
-// grid (B * Hkv, tiles of kRows keys, chunks of query rows).  Workgroups go round the XCDs, and within one round its shader engines, in the order of
-// their numbers: with the tiles first, of which the later ones are seen by fewer, the first engines of every XCD had twice the work of the
-// average (8192 tokens of 32 heads 528 us).
+// Query rows of a chunk, of `all`; and the first row that sees keys from `tile` on, a multiple of kStage, `first` being the place of row 0's token.
+template <int kStage>
+__device__ __forceinline__ int chunk_rows(int all, int chunks) {
+  const int even = ((all + chunks - 1) / chunks + kStage - 1) & ~(kStage - 1);
+  return even > kMassChunk ? even : kMassChunk;
+}
+template <int kStage>
+__device__ __forceinline__ int first_to_see(int tile, int first, int shift) { return tile > first ? ((tile - first) << shift) & ~(kStage - 1) : 0; }
+
+// grid (B * Hkv, tiles of kRows keys, chunks of query rows: of every request the same number).  Workgroups go round the XCDs, and within one round its
+// shader engines, in the order of their numbers, and one that waits for a place keeps the others waiting: with the tiles first, of which the later
+// ones are seen by fewer, the first engines of every XCD had twice the work of the average (8192 tokens of 32 heads 528 us); where a round of groups
+// is two to the XCD, its engines would have one request each, so their order changes from tile to tile (prompts of 5449 and 7958 tokens 570 -> 465 us).
+// (As many workgroups as the chip holds, which took the parts from a line with a counter, spilled registers: 489.)
 // A wave's keys come through the ring's slot of its number into registers; then the query rows stream through it as the keys do in k_mass_stats.
 template <typename TK, typename TQ>
 __global__ __launch_bounds__(kMassThreads, sizeof(TK) == 4 ? 1 : 2) void k_mass_add(MassArgs<TQ> a) {
@@ -329,17 +341,19 @@ __global__ __launch_bounds__(kMassThreads, sizeof(TK) == 4 ? 1 : 2) void k_mass_
   constexpr int kBlocks = M::kBlocks, kBytes = M::kBytes + M::kStage * 8;      // (with the rows' statistics)
   static_assert(kMassWaves == kMassRing && M::kMine * M::kRowBytes == M::kBytes, "a slot is a wave's keys");
   __shared__ __attribute__((aligned(16))) char lds_[kMassRing * kBytes];       // (one array: of several the compiler waits for all requests before any read)
+  request_arguments<decltype(&k_mass_add<TK, TQ>)>();
   const Shape& s = a.s;
-  const int G = s.G, shift = G == 4 ? 2 : G - 1;
-  const int bg = blockIdx.x, b = bg / s.Hkv, g = bg % s.Hkv, tile = blockIdx.y * M::kRows, len = length_of(s, a.kv.seq_lens, b);
+  const int G = s.G, shift = G == 4 ? 2 : G - 1, chunks = a.chunks;
+  const int bg = (blockIdx.x + 8 * (blockIdx.y / 2 + blockIdx.z)) % (s.B * s.Hkv), b = bg / s.Hkv, g = bg % s.Hkv, tile = blockIdx.y * M::kRows, len = length_of(s, a.kv.seq_lens, b);
   if (tile >= len) return;
   const int lane = threadIdx.x & 63, wave = wave_of(), n = lane & 31, h = lane >> 5;
   int c0, c1;
   const int first = launch_tokens(a, b, &c0, &c1);
-  const int all = c1 > c0 ? (c1 - c0) << shift : 0, chunk0 = (int)blockIdx.z * a.chunk;
-  const int rows = all - chunk0 < a.chunk ? all : chunk0 + a.chunk;
-  int from = tile - (first + c0);                              // the first token that sees a key of the tile
-  from = from < 0 ? 0 : from;
+  const int all = c1 > c0 ? (c1 - c0) << shift : 0, chunk = chunk_rows<M::kStage>(all, chunks), at_chunk = blockIdx.z, chunk0 = at_chunk * chunk;
+  const int rows = all - chunk0 < chunk ? all : chunk0 + chunk;
+  int m0 = first_to_see<M::kStage>(tile, first + c0, shift);
+  m0 = m0 < chunk0 ? chunk0 : m0;
+  if (m0 >= rows && chunks > 1) return;                     // (k_mass_sum leaves such chunks out)
   const int key0 = tile + M::kMine * wave;
   float sum[kBlocks][16];
 #pragma unroll
@@ -347,8 +361,6 @@ __global__ __launch_bounds__(kMassThreads, sizeof(TK) == 4 ? 1 : 2) void k_mass_
 #pragma unroll
     for (int r = 0; r < 16; ++r) sum[i][r] = 0.f;
   lds_char* const lds = (lds_char*)lds_;
-  int m0 = (from << shift) & ~(M::kStage - 1);
-  m0 = m0 < chunk0 ? chunk0 : m0;
   if (m0 < rows) {
     auto slot = [&](int j) { return lds + (j & (kMassRing - 1)) * kBytes; };
     MassRow<Op> k[kBlocks];
@@ -423,15 +435,15 @@ __global__ __launch_bounds__(kMassThreads, sizeof(TK) == 4 ? 1 : 2) void k_mass_
     auto step = [&](int i, f32x16 (&y)[kBlocks], f32x16 (&next)[kBlocks]) __attribute__((always_inline)) {
       f32x2t st = *(const __attribute__((address_space(3))) f32x2t*)(slot(i / M::kSubs) + M::kBytes + 8 * (i % M::kSubs * 32 + n));
       const int mi = m0 + 32 * i;
-      if (mi + 32 > rows || first + c0 + (mi >> shift) < key0 + M::kMine - 1) {      // not all of these queries see all of my keys: the weights here
+      if (mi + 32 > rows || first + c0 + (mi >> shift) < key0 + M::kMine - 1) {      // not all of these queries see all of my keys
         const int pos = mi + n < rows ? first + c0 + ((mi + n) >> shift) - key0 : -1;
+        const bool none = st[1] != st[1];                       // (a row of NaN: its scores say so, for its factor would to all keys)
+        if (none) st = f32x2t{0.f, 0.f};
 #pragma unroll
         for (int e = 0; e < 16 * kBlocks; ++e) {
-          const float w = __builtin_amdgcn_exp2f(fmaf(y[e / 16][e % 16], kMassUnit, -st[0])) * st[1];
-          sum[e / 16][e % 16] += 32 * (e / 16) + key_of(e % 16, h) <= pos ? w : 0.f;
-          y[e / 16][e % 16] = -INFINITY;
+          const float x = none ? __builtin_nanf("") : y[e / 16][e % 16];
+          y[e / 16][e % 16] = 32 * (e / 16) + key_of(e % 16, h) <= pos ? x : -INFINITY;
         }
-        st = f32x2t{0.f, 0.f};
       }
       turn(i);
       auto weigh = [&](int c) __attribute__((always_inline)) {
@@ -445,8 +457,13 @@ __global__ __launch_bounds__(kMassThreads, sizeof(TK) == 4 ? 1 : 2) void k_mass_
     };
     if (key0 < len) {
       f32x16 even[kBlocks], odd[kBlocks];
-      mass_scores<false, Op, kBlocks>(even, slot(0), k, n, h, [](int) {});
-      for (int i = 0; i < subs; i += 2) {
+      // (the first queries, which see none of my keys, are the other waves')
+      int skip = ((key0 - first - c0) << shift) - m0;
+      skip = skip < 0 ? 0 : skip / 32;
+      skip = skip < subs ? skip : subs;
+      for (int i = 0; i < skip; ++i) turn(i);
+      if (skip < subs) mass_scores<false, Op, kBlocks>(even, slot(skip / M::kSubs) + skip % M::kSubs * (32 * M::kRowBytes), k, n, h, [](int) {});
+      for (int i = skip; i < subs; i += 2) {
         step(i, even, odd);
         if (i + 1 >= subs) break;
         step(i + 1, odd, even);
@@ -468,8 +485,8 @@ __global__ __launch_bounds__(kMassThreads, sizeof(TK) == 4 ? 1 : 2) void k_mass_
   wave_lds_order();
   const int key = key0 + lane;
   if (lane < M::kMine && key < len) {
-    if (gridDim.z > 1) {
-      a.sums[((int64_t)blockIdx.z * gridDim.x + bg) * s.Lcap + key] = mine[lane];
+    if (chunks > 1) {
+      a.sums[((int64_t)at_chunk * (s.B * s.Hkv) + bg) * s.Lcap + key] = mine[lane];
     } else {
       float* const to = a.mass + (int64_t)bg * s.Lcap + key;
       const int held = a.held ? a.held[b] : 0;
@@ -478,15 +495,20 @@ __global__ __launch_bounds__(kMassThreads, sizeof(TK) == 4 ? 1 : 2) void k_mass_
   }
 }
 
-// The chunks' sums, in order.  grid (rows / 256, B * Hkv)
-template <typename A>
-__global__ __launch_bounds__(256) void k_mass_sum(A a, int chunks) {
-  const int bg = blockIdx.y, b = bg / a.s.Hkv, key = blockIdx.x * 256 + threadIdx.x;
+// The chunks' sums, in order.  grid (rows / 256, B * Hkv).  kRows, kStage: of k_mass_add
+template <int kRows, int kStage, typename A>
+__global__ __launch_bounds__(256) void k_mass_sum(A a) {
+  const int chunks = a.chunks, bg = blockIdx.y, b = bg / a.s.Hkv, key = blockIdx.x * 256 + threadIdx.x, G = a.s.G, shift = G == 4 ? 2 : G - 1;
   if (key >= length_of(a.s, a.kv.seq_lens, b)) return;
+  int c0, c1;
+  const int first = launch_tokens(a, b, &c0, &c1), all = c1 > c0 ? (c1 - c0) << shift : 0, chunk = chunk_rows<kStage>(all, chunks);
+  const int m0 = first_to_see<kStage>(key / kRows * kRows, first + c0, shift);
   const float* const from = a.sums + (int64_t)bg * a.s.Lcap + key;
   float sum = 0.f;
+  if (m0 < all) {
 #pragma unroll 4
-  for (int c = 0; c < chunks; ++c) sum += from[(int64_t)c * gridDim.y * a.s.Lcap];
+    for (int c = m0 / chunk; c < (all + chunk - 1) / chunk; ++c) sum += from[(int64_t)c * gridDim.y * a.s.Lcap];
+  }
   float* const to = a.mass + (int64_t)bg * a.s.Lcap + key;
   const int held = a.held ? a.held[b] : 0;
   *to = sum + (a.t0 > 0 ? *to : (key < held ? a.decay * *to : 0.f));
@@ -519,19 +541,16 @@ static hipError_t mass_t(MassArgs<TQ> a, float* work, int64_t room, hipStream_t 
       if (a.splits > 1)
         hipLaunchKernelGGL(k_mass_join, dim3((unsigned)((rows + 15) / 16)), dim3(256), 0, st, a.split_stats, a.stats, rows, a.splits);
     }
-    // Of the query rows as many chunks as make work for the whole chip several times over: a tile's work falls with its place.
-    const int64_t queries = (int64_t)n * a.s.G, key_tiles = (a.s.Lcap + M::kRows - 1) / M::kRows, wanted = 4096;
+    // Of the query rows as many chunks as make work for the whole chip many times over: not all tiles are seen by all of them.  (The prompts above, for
+    // 2048 / 4096 / 6000 / 8192 parts: 486 / 464 / 460 / 551 us.)
+    const int64_t queries = (int64_t)n * a.s.G, key_tiles = (a.s.Lcap + M::kRows - 1) / M::kRows, wanted = 6000;
     int64_t chunks = (wanted + key_tiles * a.s.B * a.s.Hkv - 1) / (key_tiles * a.s.B * a.s.Hkv);
-    if (chunks > 1 || queries > 4096) chunks = chunks > (queries + 2047) / 2048 ? chunks : (queries + 2047) / 2048;
-    if (chunks > (queries + 1023) / 1024) chunks = (queries + 1023) / 1024;
+    if (chunks > (queries + kMassChunk - 1) / kMassChunk) chunks = (queries + kMassChunk - 1) / kMassChunk;
     if (chunks * masses > left) chunks = left / masses;
-    chunks = chunks < 1 ? 1 : chunks;
-    a.chunk = (int)(((queries + chunks - 1) / chunks + M::kStage - 1) / M::kStage * M::kStage);
-    a.chunk = a.chunk < M::kStage ? M::kStage : a.chunk;
-    const int z = queries > a.chunk ? (int)((queries + a.chunk - 1) / a.chunk) : 1;
-    hipLaunchKernelGGL((k_mass_add<TK, TQ>), dim3((unsigned)(a.s.B * a.s.Hkv), (unsigned)key_tiles, (unsigned)z), dim3(kMassThreads), 0, st, a);
-    if (z > 1)
-      hipLaunchKernelGGL((k_mass_sum<MassArgs<TQ>>), dim3((unsigned)((a.s.Lcap + 255) / 256), (unsigned)(a.s.B * a.s.Hkv)), dim3(256), 0, st, a, z);
+    a.chunks = (int)(chunks < 1 ? 1 : chunks);
+    hipLaunchKernelGGL((k_mass_add<TK, TQ>), dim3((unsigned)(a.s.B * a.s.Hkv), (unsigned)key_tiles, (unsigned)a.chunks), dim3(kMassThreads), 0, st, a);
+    if (a.chunks > 1)
+      hipLaunchKernelGGL((k_mass_sum<M::kRows, M::kStage, MassArgs<TQ>>), dim3((unsigned)((a.s.Lcap + 255) / 256), (unsigned)(a.s.B * a.s.Hkv)), dim3(256), 0, st, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.n_tokens == 0) return e;
   }
@@ -541,7 +560,7 @@ static hipError_t mass_t(MassArgs<TQ> a, float* work, int64_t room, hipStream_t 
 hipError_t launch_attn_mass(const Shape& s, int dtype, const KvView& kv, const void* q, int64_t q_stride, const int32_t* cu, int n_tokens,
                             const int32_t* held, float decay, float* mass, float* part, int64_t part_rows, hipStream_t st) {
 #define LFPS_MASS(TK, TQ)                                                                                                              \
-  return mass_t<TK, TQ>(MassArgs<TQ>{s, kv, (const TQ*)q, q_stride, cu, held, n_tokens, 0, 0, decay, nullptr, nullptr, 1, 0, nullptr, mass}, \
+  return mass_t<TK, TQ>(MassArgs<TQ>{s, kv, (const TQ*)q, q_stride, cu, held, n_tokens, 0, 0, decay, nullptr, nullptr, 1, 1, nullptr, mass}, \
                         part, part_rows * kPartFloats, st)
   if (dtype == LFPS_F32) LFPS_MASS(float, float);
   if (dtype == LFPS_F16) LFPS_MASS(_Float16, _Float16);
