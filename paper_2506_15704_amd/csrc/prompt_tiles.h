@@ -12,6 +12,7 @@ namespace {
 struct SeesAll {
   __device__ __forceinline__ AllRows walk(int, int, int) const { return {}; }
   __host__ int most(int cap, int) const { return cap; }
+  __host__ bool few_apart(int) const { return true; }
 };
 struct SeesWindow {
   int32_t window, n_sink;
@@ -31,6 +32,8 @@ struct SeesWindow {
     const int64_t n = (int64_t)window + n_sink + tokens + 128;
     return n < cap ? (int)n : cap;
   }
+  // May requests of few tokens, whose tile walks `rows` at most, have a kernel of their own?
+  __host__ bool few_apart(int rows) const { return rows > 6000; }
 };
 
 template <typename TQ, typename See>
@@ -245,7 +248,11 @@ hipError_t prompt_t(const Shape& s, const KvView& kv, const See& see, const void
   // long prompt are a workgroup a KV head (20 behind 30000 rows beside 2048: 607 us), and so are the few requests with tokens in a
   // context of many (20 tokens of one request behind 32768 rows: 41 us in a context of one, 335 of 16, 665 of 64; 512 tokens 319, 440, 771).
   const bool small = sizeof(TK) != 4 && s.B * s.Hkv <= 128 && n_tokens <= (int64_t)per * s.B;
-  const bool all_few = !small && (int64_t)n_tokens * s.G <= kMost, none_few = small || (!all_few && s.B == 1);
+  const bool all_few = !small && (int64_t)n_tokens * s.G <= kMost;
+  // Over a short window a tile of few tokens is no longer than the others, and where the requests have a tile's tokens on average the two launches
+  // cost more than they bring (six ragged fp16 chunks, window 517: 121 / 116 us; seven tokens and 512, window 5500: 131 / 97; one of 1000 and seven of 3,
+  // window 4096: 128 / 132; 32 of 5, which have less: 105 / 213).
+  const bool none_few = small || (!all_few && (s.B == 1 || (sizeof(TK) != 4 && n_tokens >= (int64_t)per * s.B && !see.few_apart(see.most(s.Lcap, per)))));
   const int tiles = n_tokens / per + s.B;
   if (!all_few) a.splits = parts((int64_t)tiles * s.Hkv, (int64_t)n_tokens * s.Hq, part_rows);
   if (a.splits > 1) a.few_part = (int64_t)n_tokens * s.Hq * a.splits;
