@@ -7,6 +7,12 @@
 // its query rows in registers while the keys stream through LDS, and a lane the maximum and sum of its own keys; in the second a wave keeps its keys
 // while the queries stream, and a lane the sum of its own queries' weights for each key.  So either reduces over lanes once, at the end, and the sums
 // come in the same order every time.
+//
+// Long prompts are bound by the vector unit: a score costs three instructions, one of them an exponential of four times an ordinary one's cycles, in either
+// kernel (81 % of the busy SIMDs' time in the first).  32 heads over 8 KV heads: 8192 tokens in bf16 620 us, two products of 550 GFLOP in all at 890 TFLOP/s;
+// prompts of 5449 and 7958 tokens over FP8 pages 842 to 880 (by the profiler k_mass_stats 475, k_mass_add 460, k_mass_sum 5).  Few tokens over many rows wait for the
+// bytes, twice: 32 tokens over 32768 rows 48 us, 20 + 4.6 + 28, where K's 67 MB are 14 (the second time from the memory-side cache, but a workgroup
+// has two stages of queries only and waits for its keys before it asks for them).
 #include "tile_attn.h"
 
 namespace lfps {

@@ -10,7 +10,7 @@
 //
 // 32 heads over 8 KV heads: 16384 tokens in bf16 1.90 ms, 1160 TFLOP/s of the 1370 that the largest products of the BLAS library reach
 // here; 8192 behind 24576 rows of FP8 pages 3.34 ms, 1150; eight prompts of 61 to 4096 tokens over 16 heads in fp16 232 us, 710; two of
-// 944 and 1307 in fp32 279 us, 76 of 155 TFLOP/s; five tokens over 4104 rows 15.5 us in two launches (cards differ: 214 to 233, 13.4 to 15.8).  What each step gave is beside
+// 944 and 1307 in fp32 269 us, 79 of 155 TFLOP/s; five tokens over 4104 rows 15.5 us in two launches (cards differ: 214 to 233, 13.4 to 15.8).  What each step gave is beside
 // the loops.
 #include "prompt_tiles.h"
 

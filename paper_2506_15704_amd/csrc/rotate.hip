@@ -7,6 +7,9 @@
 // taken off before it becomes fp32, so that a position of 2^24 is turned as exactly as one of 16; the sine and cosine of what is left, at
 // most pi / 4, are their Taylor sums.  A wave has a token's angles, made by a lane a pair, and serves eight or sixteen of its head rows; other
 // waves make them again.
+//
+// Bound by the bytes: eight prompts of 1000 to 6000 tokens, 32 + 16 heads in bf16, 0.63 GB in and out, 116 us, 5.4 TB/s (a large copy reaches 5.0; part
+// of the bytes stay in the memory-side cache); 0.30 GB in fp16 57 us, 5.3.  32 single tokens 4.1 us in the kernel, 10.5 with the call.
 #include "stored_rows.h"
 #include "tile_attn.h"
 
