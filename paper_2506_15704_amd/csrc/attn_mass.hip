@@ -10,9 +10,8 @@
 //
 // Long prompts are bound by the vector unit: a score costs three instructions, one of them an exponential of four times an ordinary one's cycles, in either
 // kernel (81 % of the busy SIMDs' time in the first).  32 heads over 8 KV heads: 8192 tokens in bf16 620 us, two products of 550 GFLOP in all at 890 TFLOP/s;
-// prompts of 5449 and 7958 tokens over FP8 pages 842 to 880 (by the profiler k_mass_stats 475, k_mass_add 460, k_mass_sum 5).  Few tokens over many rows wait for the
-// bytes, twice: 32 tokens over 32768 rows 48 us, 20 + 4.6 + 28, where K's 67 MB are 14 (the second time from the memory-side cache, but a workgroup
-// has two stages of queries only and waits for its keys before it asks for them).
+// prompts of 5449 and 7958 tokens over FP8 pages 842 to 880 (by the profiler k_mass_stats 475, k_mass_add 460, k_mass_sum 5).  Requests of few tokens
+// (k_mass_add_few) are bound by the bytes of K, read twice: 32 tokens over 32768 rows 37 us, 20 + 4.7 + 18 by the profiler, where K's 67 MB are 14.
 #include "tile_attn.h"
 
 namespace lfps {
@@ -21,6 +20,7 @@ namespace {
 
 constexpr int kMassThreads = 256, kMassWaves = kMassThreads / 64;
 constexpr int kMassChunk = 1024;                       // query rows that a workgroup of k_mass_add takes at least, if there are as many
+constexpr int kMassFew = 128;                          // query rows of a request that k_mass_add_few takes at most
 constexpr int kMassRing = 4;                           // stages of streamed rows in LDS
 constexpr float kMassLazy = 6.f;                       // growth of a maximum, in powers of two, that is let pass
 constexpr float kMassUnit = kLog2e * 0.08838834764831845f;      // from products to scores in powers of two
@@ -47,6 +47,7 @@ struct MassArgs {
   float* split_stats;              // [splits, Hkv, t1 - t0, G, 2] of its parts, if there are several: the sums themselves
   int32_t splits;
   int32_t chunks;                  // of the query rows of a request
+  int32_t few_apart;               // requests of up to kMassFew query rows are k_mass_add_few's
   float* sums;                     // [chunks, B * Hkv, Lcap] what the chunks of query rows leave for the rows that they see, if there are several
   float* mass;
 };
@@ -337,7 +338,7 @@ __device__ __forceinline__ int first_to_see(int tile, int first, int shift) { re
 // grid (B * Hkv, tiles of kRows keys, chunks of query rows: of every request the same number).  Workgroups go round the XCDs, and within one round its
 // shader engines, in the order of their numbers, and one that waits for a place keeps the others waiting: with the tiles first, of which the later
 // ones are seen by fewer, the first engines of every XCD had twice the work of the average (8192 tokens of 32 heads 528 us); where a round of groups
-// is two to the XCD, its engines would have one request each, so their order changes from tile to tile (prompts of 5449 and 7958 tokens 570 -> 465 us).
+// is two to the XCD, its engines would have one request each, so their order changes from tile to tile (prompts of 5449 and 7958 tokens 551 -> 462 us).
 // (As many workgroups as the chip holds, which took the parts from a line with a counter, spilled registers: 489.)
 // A wave's keys come through the ring's slot of its number into registers; then the query rows stream through it as the keys do in k_mass_stats.
 template <typename TK, typename TQ>
@@ -350,7 +351,7 @@ __global__ __launch_bounds__(kMassThreads, sizeof(TK) == 4 ? 1 : 2) void k_mass_
   request_arguments<decltype(&k_mass_add<TK, TQ>)>();
   const Shape& s = a.s;
   const int G = s.G, shift = G == 4 ? 2 : G - 1, chunks = a.chunks;
-  const int bg = (blockIdx.x + 8 * (blockIdx.y / 2 + blockIdx.z)) % (s.B * s.Hkv), b = bg / s.Hkv, g = bg % s.Hkv, tile = blockIdx.y * M::kRows, len = length_of(s, a.kv.seq_lens, b);
+  const int bg = (blockIdx.x + 8 * (blockIdx.y / 2)) % (s.B * s.Hkv), b = bg / s.Hkv, g = bg % s.Hkv, tile = blockIdx.y * M::kRows, len = length_of(s, a.kv.seq_lens, b);
   if (tile >= len) return;
   const int lane = threadIdx.x & 63, wave = wave_of(), n = lane & 31, h = lane >> 5;
   int c0, c1;
@@ -359,6 +360,7 @@ __global__ __launch_bounds__(kMassThreads, sizeof(TK) == 4 ? 1 : 2) void k_mass_
   const int rows = all - chunk0 < chunk ? all : chunk0 + chunk;
   int m0 = first_to_see<M::kStage>(tile, first + c0, shift);
   m0 = m0 < chunk0 ? chunk0 : m0;
+  if (a.few_apart && all <= kMassFew) return;
   if (m0 >= rows && chunks > 1) return;                     // (k_mass_sum leaves such chunks out)
   const int key0 = tile + M::kMine * wave;
   float sum[kBlocks][16];
@@ -501,6 +503,121 @@ __global__ __launch_bounds__(kMassThreads, sizeof(TK) == 4 ? 1 : 2) void k_mass_
   }
 }
 
+// A lane's operands of a row of the cache as they are stored.
+template <typename TK, typename Op>
+struct MassRaw {
+  typedef typename std::conditional<sizeof(TK) == 1, u32x2, Op>::type Chunk;
+  Chunk x[8];
+  __device__ __forceinline__ void load(const TK* p, int h) {
+#pragma unroll
+    for (int c = 0; c < 8; ++c) x[c] = *reinterpret_cast<const Chunk*>(p + 16 * c + 8 * h);
+  }
+  __device__ __forceinline__ Op chunk(int c) const {
+    if constexpr (sizeof(TK) == 1) return fp8x8_to<Op>(x[c][0], x[c][1]);
+    else return x[c];
+  }
+};
+
+// The weights of requests of few query rows: all of them stay in LDS, and a wave streams keys through its registers, 32 at a time, the next ones on their
+// way, with nobody to wait for (32 tokens of 32 heads over 32768 rows 29.9 -> 18.4 us, where k_mass_add waits for its keys, then for the queries, and
+// has two stages of work; for 512 / 768 / 1024 / 1536 workgroups 19.7 / 18.4 / 21.3 / 21.4.  Statistics joined here: 24.1, where k_mass_join takes 4.7,
+// and 44 us in all for 40.6).  grid (B * Hkv, parts: steps of 128 keys in turn)
+template <typename TK, typename TQ>
+__global__ __launch_bounds__(kMassThreads, 3) void k_mass_add_few(MassArgs<TQ> a, int parts) {
+  request_arguments<decltype(&k_mass_add_few<TK, TQ>)>();
+  typedef typename InLds<TQ>::Op Op;
+  constexpr int kSubs = kMassFew / 32, kStep = 32 * kMassWaves;
+  __shared__ __attribute__((aligned(16))) char lds_[kMassFew * 256];
+  const Shape& s = a.s;
+  const int G = s.G, shift = G == 4 ? 2 : G - 1, bg = blockIdx.x, b = bg / s.Hkv, g = bg % s.Hkv, len = length_of(s, a.kv.seq_lens, b);
+  const int lane = threadIdx.x & 63, wave = wave_of(), n = lane & 31, h = lane >> 5;
+  int at = kStep * (int)blockIdx.y;
+  if (at >= len) return;
+  int c0, c1;
+  const int first = launch_tokens(a, b, &c0, &c1), rows = c1 > c0 ? (c1 - c0) << shift : 0, subs = (rows + 31) / 32;
+  if (rows > kMassFew) return;
+  lds_char* const lds = (lds_char*)lds_;
+  const CacheRows<TK> K(a.kv.k, a.kv, b, g);
+  auto my_row = [&](int step) {
+    const int r = step + 32 * wave + n;
+    return r < len ? r : len - 1;
+  };
+  int entry = K.entry(my_row(at));
+  u32x4 x[2 * kSubs];                                          // my pieces of the queries; rows that are not there are 0
+#pragma unroll
+  for (int i = 0; i < 2 * kSubs; ++i) {
+    const int piece = (int)threadIdx.x + kMassThreads * i, r = piece / 16;
+    x[i] = u32x4{0, 0, 0, 0};
+    if (r < rows)
+      x[i] = *reinterpret_cast<const u32x4*>(a.q + (int64_t)(c0 + (r >> shift)) * a.q_stride + (g * G + (r & (G - 1))) * kD + 8 * chunk_place(r, piece % 16));
+  }
+  f32x2t st[kSubs];
+#pragma unroll
+  for (int u = 0; u < kSubs; ++u) {
+    st[u] = f32x2t{0.f, 0.f};                                  // (their weights too)
+    if (32 * u + n < rows) st[u] = *reinterpret_cast<const f32x2t*>(a.stats + 2 * (((int64_t)g * (a.t1 - a.t0) + (c0 - a.t0)) * G + 32 * u + n));
+  }
+  MassRaw<TK, Op> raw;
+  raw.load(K.at(my_row(at), entry), h);
+  const int stride = kStep * parts;
+  entry = K.entry(my_row(at + stride));
+#pragma unroll
+  for (int i = 0; i < 2 * kSubs; ++i) *(__attribute__((address_space(3))) u32x4*)(lds + 16 * ((int)threadIdx.x + kMassThreads * i)) = x[i];
+  __syncthreads();
+  const int held = a.held ? a.held[b] : 0;
+  for (; at < len; at += stride) {
+    MassRow<Op> k[1];
+#pragma unroll
+    for (int c = 0; c < 8; ++c) k[0].x[c] = raw.chunk(c);
+    if (at + stride < len) {
+      raw.load(K.at(my_row(at + stride), entry), h);
+      entry = K.entry(my_row(at + 2 * stride));
+    }
+    const int key0 = at + 32 * wave;
+    if (key0 >= len) continue;
+    const int mine = key0 + key_of(lane & 15, h);              // the key whose sum I have in the end
+    float* const to = a.mass + (int64_t)bg * s.Lcap + mine;
+    const float old = mine < len && (a.t0 > 0 || mine < held) ? *to * (a.t0 > 0 ? 1.f : a.decay) : 0.f;
+    float sum[16];
+#pragma unroll
+    for (int r = 0; r < 16; ++r) sum[r] = 0.f;
+    const bool all_seen = key0 + 31 <= first + c0;
+#pragma unroll
+    for (int u = 0; u < kSubs; ++u) {
+      if (u >= subs) break;
+      f32x16 y[1];
+      mass_scores<false, Op, 1>(y, lds + 32 * u * 256, k, n, h, [](int) {});
+      float top = st[u][0], factor = st[u][1];
+      if (!all_seen) {                                         // (as in k_mass_add)
+        const int m = 32 * u + n, pos = m < rows ? first + c0 + (m >> shift) - key0 : -1;
+        const bool none = factor != factor;
+        if (none) top = factor = 0.f;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const float v = none ? __builtin_nanf("") : y[0][r];
+          y[0][r] = key_of(r, h) <= pos ? v : -INFINITY;
+        }
+      }
+#pragma unroll
+      for (int r = 0; r < 16; ++r) sum[r] = fmaf(__builtin_amdgcn_exp2f(fmaf(y[0][r], kMassUnit, -top)), factor, sum[r]);
+    }
+    // over the 32 lanes of a half: lane j of 16 is left with the sum of product j
+#define LFPS_HALVE(W, GIVEN)                                                      \
+  _Pragma("unroll") for (int i = 0; i < W; ++i) {                                 \
+    const bool up = lane & W;                                                     \
+    const float keep = up ? sum[i + W] : sum[i], give = up ? sum[i] : sum[i + W]; \
+    sum[i] = keep + GIVEN;                                                        \
+  }
+    LFPS_HALVE(8, row16_rotate<8>(give))
+    LFPS_HALVE(4, __shfl_xor(give, 4))
+    LFPS_HALVE(2, __shfl_xor(give, 2))
+    LFPS_HALVE(1, __shfl_xor(give, 1))
+#undef LFPS_HALVE
+    const float total = sum[0] + __shfl_xor(sum[0], 16);
+    if (!(lane & 16) && mine < len) *to = total + old;
+  }
+}
+
 // The chunks' sums, in order.  grid (rows / 256, B * Hkv).  kRows, kStage: of k_mass_add
 template <int kRows, int kStage, typename A>
 __global__ __launch_bounds__(256) void k_mass_sum(A a) {
@@ -508,6 +625,7 @@ __global__ __launch_bounds__(256) void k_mass_sum(A a) {
   if (key >= length_of(a.s, a.kv.seq_lens, b)) return;
   int c0, c1;
   const int first = launch_tokens(a, b, &c0, &c1), all = c1 > c0 ? (c1 - c0) << shift : 0, chunk = chunk_rows<kStage>(all, chunks);
+  if (a.few_apart && all <= kMassFew) return;
   const int m0 = first_to_see<kStage>(key / kRows * kRows, first + c0, shift);
   const float* const from = a.sums + (int64_t)bg * a.s.Lcap + key;
   float sum = 0.f;
@@ -535,6 +653,9 @@ static hipError_t mass_t(MassArgs<TQ> a, float* work, int64_t room, hipStream_t 
     const int64_t rows = (int64_t)n * a.s.Hq, left = room - 2 * rows;
     a.stats = work;
     a.split_stats = a.sums = work + 2 * rows;                         // (the parts are joined before there are sums)
+    const int64_t queries = (int64_t)n * a.s.G;
+    a.few_apart = few && sizeof(TQ) == 2;
+    const bool others = !a.few_apart || queries > kMassFew;           // (else no request has more)
     if (n > 0) {
       const int64_t groups = (int64_t)tiles * a.s.Hkv, by_len = (a.s.Lcap + 255) / 256;
       int64_t splits = ((few ? 1024 : 512) + groups - 1) / groups;      // (of the few ones' tiles half may be empty)
@@ -548,14 +669,21 @@ static hipError_t mass_t(MassArgs<TQ> a, float* work, int64_t room, hipStream_t 
         hipLaunchKernelGGL(k_mass_join, dim3((unsigned)((rows + 15) / 16)), dim3(256), 0, st, a.split_stats, a.stats, rows, a.splits);
     }
     // Of the query rows as many chunks as make work for the whole chip many times over: not all tiles are seen by all of them.  (The prompts above, for
-    // 2048 / 4096 / 6000 / 8192 parts: 486 / 464 / 460 / 551 us.)
-    const int64_t queries = (int64_t)n * a.s.G, key_tiles = (a.s.Lcap + M::kRows - 1) / M::kRows, wanted = 6000;
+    // 4096 / 6000 / 8192 / 12000 parts: 461 / 462 / 470 / 484 us.)
+    const int64_t key_tiles = (a.s.Lcap + M::kRows - 1) / M::kRows, wanted = 6000;
     int64_t chunks = (wanted + key_tiles * a.s.B * a.s.Hkv - 1) / (key_tiles * a.s.B * a.s.Hkv);
     if (chunks > (queries + kMassChunk - 1) / kMassChunk) chunks = (queries + kMassChunk - 1) / kMassChunk;
     if (chunks * masses > left) chunks = left / masses;
     a.chunks = (int)(chunks < 1 ? 1 : chunks);
-    hipLaunchKernelGGL((k_mass_add<TK, TQ>), dim3((unsigned)(a.s.B * a.s.Hkv), (unsigned)key_tiles, (unsigned)a.chunks), dim3(kMassThreads), 0, st, a);
-    if (a.chunks > 1)
+    if constexpr (sizeof(TQ) == 2) {
+      if (a.few_apart) {
+        const int64_t groups = (int64_t)a.s.B * a.s.Hkv, steps = (a.s.Lcap + 32 * kMassWaves - 1) / (32 * kMassWaves), most = (768 + groups - 1) / groups;
+        const int parts = (int)(steps < most ? steps : most);
+        hipLaunchKernelGGL((k_mass_add_few<TK, TQ>), dim3((unsigned)groups, (unsigned)parts), dim3(kMassThreads), 0, st, a, parts);
+      }
+    }
+    if (others) hipLaunchKernelGGL((k_mass_add<TK, TQ>), dim3((unsigned)(a.s.B * a.s.Hkv), (unsigned)key_tiles, (unsigned)a.chunks), dim3(kMassThreads), 0, st, a);
+    if (others && a.chunks > 1)
       hipLaunchKernelGGL((k_mass_sum<M::kRows, M::kStage, MassArgs<TQ>>), dim3((unsigned)((a.s.Lcap + 255) / 256), (unsigned)(a.s.B * a.s.Hkv)), dim3(256), 0, st, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.n_tokens == 0) return e;
@@ -566,7 +694,7 @@ static hipError_t mass_t(MassArgs<TQ> a, float* work, int64_t room, hipStream_t 
 hipError_t launch_attn_mass(const Shape& s, int dtype, const KvView& kv, const void* q, int64_t q_stride, const int32_t* cu, int n_tokens,
                             const int32_t* held, float decay, float* mass, float* part, int64_t part_rows, hipStream_t st) {
 #define LFPS_MASS(TK, TQ)                                                                                                              \
-  return mass_t<TK, TQ>(MassArgs<TQ>{s, kv, (const TQ*)q, q_stride, cu, held, n_tokens, 0, 0, decay, nullptr, nullptr, 1, 1, nullptr, mass}, \
+  return mass_t<TK, TQ>(MassArgs<TQ>{s, kv, (const TQ*)q, q_stride, cu, held, n_tokens, 0, 0, decay, nullptr, nullptr, 1, 1, 0, nullptr, mass}, \
                         part, part_rows * kPartFloats, st)
   if (dtype == LFPS_F32) LFPS_MASS(float, float);
   if (dtype == LFPS_F16) LFPS_MASS(_Float16, _Float16);
