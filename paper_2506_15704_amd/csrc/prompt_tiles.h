@@ -130,10 +130,13 @@ __device__ __forceinline__ void prompt_pipe(char* lds, const PromptArgs<TQ, See>
   st.limit = walk.steps(seen(token));
   lds_char* room = (lds_char*)lds + wave * (kPipeLds / kPipeWaves & ~15);
   if (lo < hi) {
-    st.q.load(a.q + (int64_t)(c0 + token) * a.q_stride + head * kD, h);
     const CacheRows<TK> K(a.kv.k, a.kv, b, g);
     const CacheRows<TV> V(a.kv.v, a.kv, b, g);
-    room = pipe_loop<kKind, TK, TV>(lds, K, V, lo, hi, walk.steps(seen(row0 >> shift)), row0 + 32 * wave < rows, st, walk);
+    auto query = [&](int i) __attribute__((always_inline)) {
+      const int x = min(row0 + 32 * wave + i, rows - 1);
+      return reinterpret_cast<const char*>(a.q + (int64_t)(c0 + (x >> shift)) * a.q_stride + (g * G + (x & (G - 1))) * kD);
+    };
+    room = pipe_loop<kKind, TK, TV>(lds, K, V, lo, hi, walk.steps(seen(row0 >> shift)), row0 + 32 * wave < rows, st, walk, query);
   }
   if (a.splits > 1) {
     if (valid) st.finish((TQ*)nullptr, a.part + (part_row(a, false, 0, b, c0, token, head) + split) * kPartFloats, h);

@@ -63,6 +63,9 @@ struct GapRows {
   __device__ __forceinline__ int row(int k) const { return k < at ? k : k + by; }
   __device__ __forceinline__ int end(int e) const { return e > at ? e + by : e; }      // of the cache's rows, for a walk that ends at e
   __device__ __forceinline__ int steps(int e) const { return e - by; }                 // and the other way round, e > at + by
+  __device__ __forceinline__ auto past_gap_from(int base) const {               // (a key's place in the gap is one unsigned comparison)
+    return [first = sinks - base, gap = (uint32_t)(from > sinks ? from - sinks : 0)](int key) { return (uint32_t)(key - first) >= gap; };
+  }
   __device__ __forceinline__ auto seen_from(int base, int limit) const {        // (no branches: a key's place in the gap is one unsigned comparison)
     return [seen = limit - base, first = sinks - base, gap = (uint32_t)(from > sinks ? from - sinks : 0)](int key) {
       return (bool)((int)(key < seen) & (int)((uint32_t)(key - first) >= gap));
@@ -186,6 +189,13 @@ struct QueryTile {
     static_assert(kTerms == 1, "");
 #pragma unroll
     for (int s = 0; s < 8; ++s) x[0][s] = *reinterpret_cast<const Op*>(q + 16 * s + 8 * h);
+    unit = kLog2e * 0.08838834764831845f;
+  }
+  // The same from 32 rows in LDS, mine the n-th.
+  __device__ __forceinline__ void load(const lds_char* rows, int n, int h) {
+    static_assert(kTerms == 1, "");
+#pragma unroll
+    for (int s = 0; s < 8; ++s) x[0][s] = *(const __attribute__((address_space(3))) Op*)(rows + n * 256 + 16 * chunk_place(n, 2 * s + h));
     unit = kLog2e * 0.08838834764831845f;
   }
   // An fp32 row.  fp16 terms are taken of the row scaled by a power of two that

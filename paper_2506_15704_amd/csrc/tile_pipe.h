@@ -185,14 +185,18 @@ struct PipeState {
     add_apart<Op>(o, weight, v, kPipeKeys, sees, lane);
   }
 
-  // Scores of keys that the row does not see.
+  // Scores of keys that the row does not see: behind its limit, and in its gap.  (One after the other: both conditions in one choice go by way of the
+  // scalar unit.)
   template <typename Rows>
   __device__ __forceinline__ void hide(f32x16 (&s)[2], int first, int h, const Rows& rows) const {
-    const auto sees = rows.seen_from(first + 4 * h, limit);
+    auto keep = [&](auto sees) __attribute__((always_inline)) {
 #pragma unroll
-    for (int b = 0; b < 2; ++b)
+      for (int b = 0; b < 2; ++b)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) s[b][r] = sees(32 * b + 8 * (r / 4) + r % 4) ? s[b][r] : -INFINITY;
+        for (int r = 0; r < 16; ++r) s[b][r] = sees(32 * b + 8 * (r / 4) + r % 4) ? s[b][r] : -INFINITY;
+    };
+    keep(AllRows().seen_from(first + 4 * h, limit));
+    if constexpr (Rows::kGap) keep(rows.past_gap_from(first + 4 * h));
   }
   __device__ __forceinline__ static float largest(const f32x16 (&s)[2]) {
     float mx[4];
@@ -311,9 +315,17 @@ constexpr int pipe_lds() { return PipeState<Op, kTerms>::kRest ? kRestAt + kPipe
 // active: the wave has rows of its own; one that has none only brings its share of the cache's.
 // Returns 8 KB of LDS that are the wave's from then on: of the four stages that nothing is on its way to any more.
 // rows: the cache's rows that [first, end) stand for.
-template <int kKind, typename TK, typename TV, typename Op, int kTerms, typename Rows = AllRows>
+// query(i): where piece lane % 16 of the wave's query row i, one of lane / 16, begins without chunk_place: they come through LDS, whole rows an
+// instruction (by lanes that each asked for their row's pieces, 32 bytes of 32 rows an instruction, they and the keys behind them took 12200 cycles of a
+// workgroup; NOW).  HeldRows: st.q is filled already.
+struct HeldRows {};
+__device__ __forceinline__ lds_char* query_room(lds_char* lds, int wave) {
+  const int stage = (wave >> 1 & 1) + 1, of_v = wave >> 2;
+  return lds + (of_v * kPipeStages + stage) * kPipeStage + (wave & 1) * (kPipeStage / 2);
+}
+template <int kKind, typename TK, typename TV, typename Op, int kTerms, typename Rows = AllRows, typename Query = HeldRows>
 __device__ __forceinline__ lds_char* pipe_loop(char* lds_, const CacheRows<TK>& K, const CacheRows<TV>& V, int first, int end, int least, bool active,
-                                          PipeState<Op, kTerms>& st, const Rows& rows = Rows()) {
+                                          PipeState<Op, kTerms>& st, const Rows& rows = Rows(), const Query& query = Query()) {
   lds_char* const lds = (lds_char*)lds_;
   const int lane = threadIdx.x & 63, wave = wave_of(), n = lane & 31, h = lane >> 5;
   const bool late = wave >= kPipeWaves / 2;
@@ -331,23 +343,58 @@ __device__ __forceinline__ lds_char* pipe_loop(char* lds_, const CacheRows<TK>& 
   auto landed = [] { __builtin_amdgcn_s_waitcnt(0x0f70); };     // vmcnt(0): what I asked for is in LDS
   int e_v = look_up(first + 2 * kPipeKeys), e_k = look_up(first + 3 * kPipeKeys), e_new = 0;      // of the next to be asked for
   const int e_first[3] = {look_up(first), look_up(first + kPipeKeys), e_v};
-#pragma unroll
-  for (int i = 0; i < 3; ++i) {                                  // K of the first three stages, V of two
+  constexpr bool kQuery = !std::is_same<Query, HeldRows>::value;
+  Feed<TK, kKind, Op> fk_first[3];                               // K of the first three stages, V of two
+  Feed<TV, kKind, Op> fv_first[2];
+  auto ask_first = [&](int i) __attribute__((always_inline)) {
     const int k = first + i * kPipeKeys, e = uniform(e_first[i]);
-    fk.aim(K, row_of(k), row_end, e, lane);
-    fk.ask(lds + i * kPipeStage, wave);
-    __builtin_amdgcn_sched_barrier(0);
-    fk.put(lds + i * kPipeStage, lane, wave);
-    if (i < 2) {
-      fv.aim(V, row_of(k), row_end, e, lane);
-      fv.ask(lds + kV + i * kPipeStage, wave);
-      fv.put(lds + kV + i * kPipeStage, lane, wave);
+    fk_first[i].aim(K, row_of(k), row_end, e, lane);
+    fk_first[i].ask(lds + i * kPipeStage, wave);
+    if constexpr (kQuery) {
+      if (i == 0) {                                              // (they lie where the other stages will, but V's first)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const int r = 4 * j + (lane >> 4);
+          __builtin_amdgcn_global_load_lds((global_char*)(query(r) + 16 * chunk_place(r, lane & 15)),
+                                           (__attribute__((address_space(3))) void*)(query_room(lds, wave) + 1024 * j), 16, 0, 0);
+        }
+      }
     }
-  }
+    __builtin_amdgcn_sched_barrier(0);
+    if (i < 2) {
+      fv_first[i].aim(V, row_of(k), row_end, e, lane);
+      fv_first[i].ask(lds + kV + i * kPipeStage, wave);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  auto put_first = [&](int i) __attribute__((always_inline)) {
+    fk_first[i].put(lds + i * kPipeStage, lane, wave);
+    if (i < 2) fv_first[i].put(lds + kV + i * kPipeStage, lane, wave);
+  };
   // (what is asked for first, K of the first stage, is what the first products wait for)
-  constexpr int kBehind = Feed<TK, kKind, Op>::kDirect && Feed<TV, kKind, Op>::kDirect ? 2 * Feed<TK, kKind, Op>::kLoads + 2 * Feed<TV, kKind, Op>::kLoads : 0;
+  constexpr bool kDirect = Feed<TK, kKind, Op>::kDirect && Feed<TV, kKind, Op>::kDirect;
+  constexpr int kLoadsK = Feed<TK, kKind, Op>::kLoads, kLoadsV = Feed<TV, kKind, Op>::kLoads, kBehind = kDirect ? (kQuery ? kLoadsV : 2 * kLoadsK + 2 * kLoadsV) : 0;
+  ask_first(0);
+  if constexpr (!kQuery) {
+    ask_first(1);
+    ask_first(2);
+  }
   __builtin_amdgcn_s_waitcnt(0x0f70 | kBehind);      // vmcnt(kBehind)
+  if constexpr (kQuery) {
+    wave_lds_order();
+    st.q.load(query_room(lds, wave), n, h);
+    __builtin_amdgcn_s_waitcnt(0xc07f);              // lgkmcnt(0): its place is free
+  }
+  put_first(0);
+  if constexpr (!kQuery) {
+    put_first(1);
+    put_first(2);
+  }
   __syncthreads();
+  if constexpr (kQuery) {
+    ask_first(1);
+    ask_first(2);
+  }
   f32x16 s[2];                                // scores of a stage
   constexpr int kAhead = kTerms == 1 ? 2 : 1, kOperands = kAhead + 1;      // groups read ahead (of two terms a group is twice as long)
   Op w[4], a[kOperands][4];                   // its weights; operands
@@ -356,6 +403,10 @@ __device__ __forceinline__ lds_char* pipe_loop(char* lds_, const CacheRows<TK>& 
     st.load_keys(a[0], lds, g, n, h);
     st.add_scores(s, a[0], g, rest);
   }
+  if constexpr (kQuery) {
+    put_first(1);
+    put_first(2);
+  }
   __syncthreads();                            // (K of the first stage has been read)
   if (late) {
     landed();
@@ -363,10 +414,13 @@ __device__ __forceinline__ lds_char* pipe_loop(char* lds_, const CacheRows<TK>& 
   }
   int k0 = first, now = 0, next = kPipeStage, last = 2 * kPipeStage;      // places of this stage, the next, the one after
   auto stage = [&](auto masked, auto works) {
-    constexpr bool kMasked = decltype(masked)::value, kWorks = decltype(works)::value;
+    constexpr bool kMasked = decltype(masked)::value != 0, kWorks = decltype(works)::value;
     // vector half
     if constexpr (kWorks) {
-      if (kMasked) st.hide(s, k0, h, rows);
+      if constexpr (kMasked) {
+        if constexpr (decltype(masked)::value == 2) st.hide(s, k0, h, rows);
+        else st.hide(s, k0, h, AllRows());
+      }
       st.follow(st.largest(s));
       const float at = st.m == -INFINITY ? 0.f : st.m - (PipeState<Op, kTerms>::kLift);
 #pragma unroll
@@ -425,18 +479,21 @@ __device__ __forceinline__ lds_char* pipe_loop(char* lds_, const CacheRows<TK>& 
     next = last;
     last = free;
   };
-  const std::true_type yes;
-  const std::false_type no;
+  const std::integral_constant<int, 2> gap;
+  const std::integral_constant<int, 1> limit;
+  const std::integral_constant<int, 0> no;
+  const std::true_type works;
+  const std::false_type idle;
   if (active) {
     if constexpr (Rows::kGap)
-      while (k0 < rows.clear && k0 < end) stage(yes, yes);
-    while (k0 + kPipeKeys <= least && k0 < end) stage(no, yes);
-    while (k0 < end) stage(yes, yes);
+      while (k0 < rows.clear && k0 < end) stage(gap, works);
+    while (k0 + kPipeKeys <= least && k0 < end) stage(no, works);
+    while (k0 < end) stage(limit, works);
   } else {
     if constexpr (Rows::kGap)
-      while (k0 < rows.clear && k0 < end) stage(yes, no);
-    while (k0 + kPipeKeys <= least && k0 < end) stage(no, no);
-    while (k0 < end) stage(yes, no);
+      while (k0 < rows.clear && k0 < end) stage(limit, idle);
+    while (k0 + kPipeKeys <= least && k0 < end) stage(no, idle);
+    while (k0 < end) stage(limit, idle);
   }
   if (!late) __syncthreads();
   // (the last stage has asked for rows of K into what is now the last stage, and of V into the next)
