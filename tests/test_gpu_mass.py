@@ -202,6 +202,49 @@ def test_what_is_not_finite_counts_where_it_is_seen(dtype):
     c.ctx.close()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32", "fp8kv"])
+@pytest.mark.parametrize("G,t,n", [(4, 20, 300), (4, 32, 32), (1, 100, 500), (2, 300, 700), (4, 600, 600)])
+def test_a_query_of_nan_counts_for_the_rows_it_sees(dtype, G, t, n):
+    """Few tokens, which a kernel of their own takes, and many: the rows behind the token's have what they have without it, to the last bit."""
+    c = CacheCase(dtype, 2 * G, 2, [n, 50], 16, seed=G)
+    q = c.randn(t + 3, 2 * G, D).to(c.q_dtype)
+    at, runs = t // 2, []
+    for spoilt in (False, True):
+        if spoilt:
+            q[at, G:] = float("nan")                                     # (the second KV head's)
+        runs.append(torch.zeros((2, 2, c.cap), device=DEV))
+        c.ctx.lfps_attn_mass(q, ints([0, t, t + 3]), c.kv, runs[-1])
+    sees = n - t + at + 1
+    assert bool(runs[0].isfinite().all()) and torch.equal(runs[0][:, 0], runs[1][:, 0]) and torch.equal(runs[0][1], runs[1][1])
+    assert bool(runs[1][0, 1, :sees].isnan().all()) and torch.equal(runs[0][0, 1, sees:], runs[1][0, 1, sees:])
+    c.ctx.close()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "fp8k", "f32"])
+@pytest.mark.parametrize("Hq,news,lens,held", [(4, [9, 5, 3, 0], [3, 20, 0, 8], [1, 17, 0, 8]), (1, [128, 1], [200, 1], [72, 0]), (2, [64, 65], [64, 300], [0, 235]),
+                                               (4, [32, 33, 1], [32, 129, 5000], [0, 96, 4999])])
+def test_few_tokens_of_some_requests(dtype, Hq, news, lens, held):
+    """Tokens at no row, one block of queries and a row more, requests of few tokens beside others."""
+    c = CacheCase(dtype, Hq, 1, lens, 16, seed=len(news) + Hq)
+    _check(c, news, held, 0.5, lead=1, extra=2)
+    c.ctx.close()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_keys_of_minus_infinity_weigh_nothing_to_few_tokens(dtype):
+    n = 100
+    c = CacheCase(dtype, 1, 1, [n], seed=6)
+    c.K[..., 5] = 0
+    c.K[0, 0, :40, 5] = float("-inf")
+    q = c.randn(n, 1, D).to(c.q_dtype)
+    q[..., 5] = 1.0
+    mass = torch.full((1, 1, n), 7.0, device=DEV)
+    c.ctx.lfps_attn_mass(q, ints([0, n]), c.kv, mass)
+    assert not bool(mass[0, 0, :40].any()) and bool((mass[0, 0, 40:] > 0).all())
+    assert abs(float(mass.double().sum()) - 60) <= 60 * (2.0 ** -19 + 3 * 2 * n * 2.0 ** -24)
+    c.ctx.close()
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_keys_of_minus_infinity_weigh_nothing(dtype):
     n = 150
