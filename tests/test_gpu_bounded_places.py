@@ -146,6 +146,26 @@ def test_steps_over_more_rows_than_the_caches_keep(dtype, layout, G):
     c.ctx.close()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32", "fp8kv"])
+@pytest.mark.parametrize("layout", [0, 16])
+def test_lengths_outside_the_cache_are_the_nearest_inside(dtype, layout):
+    cap, news = 150, [4, 60, 3, 0]
+    c = CacheCase(dtype, 4, 2, [cap] * 4, layout, seed=9)
+    clean, runs = [raw(c.K).clone(), raw(c.V).clone()], []
+    for lens in ([-5, cap + 1000, 2 ** 31 - 1, -2 ** 31], [0, cap, cap, 0]):
+        c.seq.copy_(ints(lens))
+        for x, y in zip((c.K, c.V), clean):
+            raw(x).copy_(y)
+        c.lens = [0, cap, cap, 0]
+        runs.append(_everything(c, c.kv, news, 3)[:-1] + [raw(c.K).clone(), raw(c.V).clone()])
+        held, mass = c.seq.clone(), torch.ones((4, 2, cap), device=DEV)
+        c.ctx.lfps_attn_mass(torch.zeros((0, 4, D), dtype=c.q_dtype, device=DEV), ints([0] * 5), c.kv, mass, held=held, decay=0.5)
+        runs[-1].append(mass)
+    for a, b in zip(*runs):
+        assert torch.equal(_bits(a), _bits(b))
+    c.ctx.close()
+
+
 def test_written_arrays_that_overlap_read_ones():
     from paper_2506_15704_amd.binding import LFPS_EINVAL, LfpsError
     c = CacheCase("bf16", 4, 2, [64], 16)
