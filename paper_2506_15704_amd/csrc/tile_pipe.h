@@ -315,9 +315,9 @@ constexpr int pipe_lds() { return PipeState<Op, kTerms>::kRest ? kRestAt + kPipe
 // active: the wave has rows of its own; one that has none only brings its share of the cache's.
 // Returns 8 KB of LDS that are the wave's from then on: of the four stages that nothing is on its way to any more.
 // rows: the cache's rows that [first, end) stand for.
-// query(i): where piece lane % 16 of the wave's query row i, one of lane / 16, begins without chunk_place: they come through LDS, whole rows an
-// instruction (by lanes that each asked for their row's pieces, 32 bytes of 32 rows an instruction, they and the keys behind them took 12200 cycles of a
-// workgroup; NOW).  HeldRows: st.q is filled already.
+// query(i): the wave's query row i.  They come through LDS, whole rows an instruction, into places of the later stages: 10500 cycles until they and the
+// first keys are there, where all workgroups begin at once (asked for by lanes each for its own row, 32 bytes of 32 rows an instruction, 12200; 16384
+// tokens, window 1024, 351 -> 348 us).  HeldRows: st.q is filled already.
 struct HeldRows {};
 __device__ __forceinline__ lds_char* query_room(lds_char* lds, int wave) {
   const int stage = (wave >> 1 & 1) + 1, of_v = wave >> 2;

@@ -5,8 +5,8 @@
 // window on, as if they lay together; only the steps at the window's two edges and behind the first rows look which rows a token sees.
 // Bound by the matrix units, less closely than whole prompts: a tile of 64 tokens walks 1100 rows where each of them sees 1028, and what a workgroup
 // does once (first rows asked for, waited for and scored, edges, results stored) comes every 17 stages.  32 heads over 8 KV heads, bf16: 16384 tokens,
-// window 1024, 341 us, 784 TFLOP/s of the 1392 that a large library product reaches (a window of one row, which is all fixed cost, 110); six chunks
-// of 100 to 4000 tokens of 16 heads in fp16, window 517, 108 us, 455; five tokens, window 1024, 11.7 us in two launches.
+// window 1024, 337 us, 793 TFLOP/s of the 1392 that a large library product reaches (a window of one row, which is all fixed cost, 110); six chunks
+// of 100 to 4000 tokens of 16 heads in fp16, window 517, 100 to 109 us by the card; five tokens, window 1024, 11.7 us in two launches.
 #include "prompt_tiles.h"
 
 namespace lfps {
