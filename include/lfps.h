@@ -335,7 +335,7 @@ int lfps_window_attn_decode(lfps_ctx* ctx, const float* q, const lfps_kv* kv, in
  *   held   [B] int32: rows that have a weight already (0 after a prompt's first call, the rows before the new ones later); NULL: none, mass
  *          is written whole.  decay in [0, 1].
  *   mass   [B, Hkv, max_seq_len] fp32, 16-byte aligned; rows from n_b on are left as they were
- * kv->v is not read.  Products and sums are fp32; sums come in the same order every time. */
+ * mass must not overlap what is read.  kv->v is not read.  Products and sums are fp32; sums come in the same order every time. */
 int lfps_attn_mass(lfps_ctx* ctx, const void* q, int64_t stride_t, const int32_t* cu, int32_t n_tokens, const lfps_kv* kv, const int32_t* held,
                    float decay, float* mass, void* stream);
 /* lfps_full_attn_decode that adds its weights up too (q, out [B, Hq, D] fp32; mass as above, the one token of a request being its row n_b - 1).

@@ -20,7 +20,6 @@ namespace {
 
 constexpr int kMassThreads = 256, kMassWaves = kMassThreads / 64;
 constexpr int kMassChunk = 1024;                       // query rows that a workgroup of k_mass_add takes at least, if there are as many
-constexpr int kMassFew = 128;                          // query rows of a request that k_mass_add_few takes at most
 constexpr int kMassRing = 4;                           // stages of streamed rows in LDS
 constexpr float kMassLazy = 6.f;                       // growth of a maximum, in powers of two, that is let pass
 constexpr float kMassUnit = kLog2e * 0.08838834764831845f;      // from products to scores in powers of two
@@ -47,7 +46,7 @@ struct MassArgs {
   float* split_stats;              // [splits, Hkv, t1 - t0, G, 2] of its parts, if there are several: the sums themselves
   int32_t splits;
   int32_t chunks;                  // of the query rows of a request
-  int32_t few_apart;               // requests of up to kMassFew query rows are k_mass_add_few's
+  int32_t few_rows;                // requests of up to so many query rows are k_mass_add_few's (-1: none, not even those of no tokens)
   float* sums;                     // [chunks, B * Hkv, Lcap] what the chunks of query rows leave for the rows that they see, if there are several
   float* mass;
 };
@@ -351,7 +350,8 @@ __global__ __launch_bounds__(kMassThreads, sizeof(TK) == 4 ? 1 : 2) void k_mass_
   request_arguments<decltype(&k_mass_add<TK, TQ>)>();
   const Shape& s = a.s;
   const int G = s.G, shift = G == 4 ? 2 : G - 1, chunks = a.chunks;
-  const int bg = (blockIdx.x + 8 * (blockIdx.y / 2)) % (s.B * s.Hkv), b = bg / s.Hkv, g = bg % s.Hkv, tile = blockIdx.y * M::kRows, len = length_of(s, a.kv.seq_lens, b);
+  const int bg = (blockIdx.x + 8 * (blockIdx.y / 2)) % (s.B * s.Hkv), b = bg / s.Hkv, g = bg % s.Hkv, tile = blockIdx.y * M::kRows;
+  const int len = length_of(s, a.kv.seq_lens, b);
   if (tile >= len) return;
   const int lane = threadIdx.x & 63, wave = wave_of(), n = lane & 31, h = lane >> 5;
   int c0, c1;
@@ -360,7 +360,7 @@ __global__ __launch_bounds__(kMassThreads, sizeof(TK) == 4 ? 1 : 2) void k_mass_
   const int rows = all - chunk0 < chunk ? all : chunk0 + chunk;
   int m0 = first_to_see<M::kStage>(tile, first + c0, shift);
   m0 = m0 < chunk0 ? chunk0 : m0;
-  if (a.few_apart && all <= kMassFew) return;
+  if (all <= a.few_rows) return;
   if (m0 >= rows && chunks > 1) return;                     // (k_mass_sum leaves such chunks out)
   const int key0 = tile + M::kMine * wave;
   float sum[kBlocks][16];
@@ -521,13 +521,13 @@ struct MassRaw {
 // The weights of requests of few query rows: all of them stay in LDS, and a wave streams keys through its registers, 32 at a time, the next ones on their
 // way, with nobody to wait for (32 tokens of 32 heads over 32768 rows 29.9 -> 18.4 us, where k_mass_add waits for its keys, then for the queries, and
 // has two stages of work; for 512 / 768 / 1024 / 1536 workgroups 19.7 / 18.4 / 21.3 / 21.4.  Statistics joined here: 24.1, where k_mass_join takes 4.7,
-// and 44 us in all for 40.6).  grid (B * Hkv, parts: steps of 128 keys in turn)
-template <typename TK, typename TQ>
-__global__ __launch_bounds__(kMassThreads, 3) void k_mass_add_few(MassArgs<TQ> a, int parts) {
-  request_arguments<decltype(&k_mass_add_few<TK, TQ>)>();
+// and 44 us in all for 40.6; 64 tokens, 256 rows, 70 -> 60 in all).  kFew: query rows that there is room for.  grid (B * Hkv, parts: steps of 128 keys in turn)
+template <typename TK, typename TQ, int kFew>
+__global__ __launch_bounds__(kMassThreads, kFew == 128 ? 3 : 2) void k_mass_add_few(MassArgs<TQ> a, int parts) {
+  request_arguments<decltype(&k_mass_add_few<TK, TQ, kFew>)>();
   typedef typename InLds<TQ>::Op Op;
-  constexpr int kSubs = kMassFew / 32, kStep = 32 * kMassWaves;
-  __shared__ __attribute__((aligned(16))) char lds_[kMassFew * 256];
+  constexpr int kSubs = kFew / 32, kStep = 32 * kMassWaves;
+  __shared__ __attribute__((aligned(16))) char lds_[kFew * 256];
   const Shape& s = a.s;
   const int G = s.G, shift = G == 4 ? 2 : G - 1, bg = blockIdx.x, b = bg / s.Hkv, g = bg % s.Hkv, len = length_of(s, a.kv.seq_lens, b);
   const int lane = threadIdx.x & 63, wave = wave_of(), n = lane & 31, h = lane >> 5;
@@ -535,7 +535,7 @@ __global__ __launch_bounds__(kMassThreads, 3) void k_mass_add_few(MassArgs<TQ> a
   if (at >= len) return;
   int c0, c1;
   const int first = launch_tokens(a, b, &c0, &c1), rows = c1 > c0 ? (c1 - c0) << shift : 0, subs = (rows + 31) / 32;
-  if (rows > kMassFew) return;
+  if (rows > a.few_rows) return;
   lds_char* const lds = (lds_char*)lds_;
   const CacheRows<TK> K(a.kv.k, a.kv, b, g);
   auto my_row = [&](int step) {
@@ -625,7 +625,7 @@ __global__ __launch_bounds__(256) void k_mass_sum(A a) {
   if (key >= length_of(a.s, a.kv.seq_lens, b)) return;
   int c0, c1;
   const int first = launch_tokens(a, b, &c0, &c1), all = c1 > c0 ? (c1 - c0) << shift : 0, chunk = chunk_rows<kStage>(all, chunks);
-  if (a.few_apart && all <= kMassFew) return;
+  if (all <= a.few_rows) return;
   const int m0 = first_to_see<kStage>(key / kRows * kRows, first + c0, shift);
   const float* const from = a.sums + (int64_t)bg * a.s.Lcap + key;
   float sum = 0.f;
@@ -654,8 +654,8 @@ static hipError_t mass_t(MassArgs<TQ> a, float* work, int64_t room, hipStream_t 
     a.stats = work;
     a.split_stats = a.sums = work + 2 * rows;                         // (the parts are joined before there are sums)
     const int64_t queries = (int64_t)n * a.s.G;
-    a.few_apart = few && sizeof(TQ) == 2;
-    const bool others = !a.few_apart || queries > kMassFew;           // (else no request has more)
+    a.few_rows = sizeof(TQ) == 4 ? -1 : (few ? 128 : ((int64_t)a.n_tokens * a.s.G <= 256 * (int64_t)a.s.B ? 256 : -1));
+    const bool others = queries > a.few_rows;                         // (else no request has more)
     if (n > 0) {
       const int64_t groups = (int64_t)tiles * a.s.Hkv, by_len = (a.s.Lcap + 255) / 256;
       int64_t splits = ((few ? 1024 : 512) + groups - 1) / groups;      // (of the few ones' tiles half may be empty)
@@ -676,10 +676,12 @@ static hipError_t mass_t(MassArgs<TQ> a, float* work, int64_t room, hipStream_t 
     if (chunks * masses > left) chunks = left / masses;
     a.chunks = (int)(chunks < 1 ? 1 : chunks);
     if constexpr (sizeof(TQ) == 2) {
-      if (a.few_apart) {
-        const int64_t groups = (int64_t)a.s.B * a.s.Hkv, steps = (a.s.Lcap + 32 * kMassWaves - 1) / (32 * kMassWaves), most = (768 + groups - 1) / groups;
+      if (a.few_rows > 0) {
+        const int64_t groups = (int64_t)a.s.B * a.s.Hkv, steps = (a.s.Lcap + 32 * kMassWaves - 1) / (32 * kMassWaves), most = ((few ? 768 : 512) + groups - 1) / groups;
         const int parts = (int)(steps < most ? steps : most);
-        hipLaunchKernelGGL((k_mass_add_few<TK, TQ>), dim3((unsigned)groups, (unsigned)parts), dim3(kMassThreads), 0, st, a, parts);
+        const dim3 grid((unsigned)groups, (unsigned)parts);
+        if (few) hipLaunchKernelGGL((k_mass_add_few<TK, TQ, 128>), grid, dim3(kMassThreads), 0, st, a, parts);
+        else hipLaunchKernelGGL((k_mass_add_few<TK, TQ, 256>), grid, dim3(kMassThreads), 0, st, a, parts);
       }
     }
     if (others) hipLaunchKernelGGL((k_mass_add<TK, TQ>), dim3((unsigned)(a.s.B * a.s.Hkv), (unsigned)key_tiles, (unsigned)a.chunks), dim3(kMassThreads), 0, st, a);

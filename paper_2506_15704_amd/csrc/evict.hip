@@ -2,16 +2,16 @@
 // the largest accumulated weight (equal ones: the lower rows; NaN: as the least).  They move to the front, in order, and with them their weights.
 //
 // k_evict_plan, a workgroup a (request, KV head), or where that leaves CUs without work several that all find the cut and share the rest: the weight at
-// the cut by three passes of a histogram over the bits of its order-preserving key, then the rows that are kept, in order: every wave has a stretch of the rows, counts what it keeps, and writes it behind what the waves
-// before it keep.  Up to 32768 rows stay in registers from the first pass to the last; of more, every pass reads them again.
+// the cut by three passes of a histogram over the bits of its order-preserving key, then the rows that are kept, in order: every wave has a stretch of
+// the rows, counts what it keeps, and writes it behind what the waves before it keep.  Up to 32768 rows stay in registers from the first pass to the last; of more, every pass reads them again.
 // k_evict_move carries the rows.  In place (kept rows only ever move down) a workgroup takes a slice of every row in order, a stretch at a
 // time: all of it is read before any of it is written, and what later stretches read lies behind what this one writes, so that they are asked
 // for before it is.
 //
 // Few requests are bound by latency: one of 32768 rows cut to a quarter, 8 heads in bf16, 40 us: the plan 17.8 (keys read, three histograms of which each
 // waits for the one before, list written), the move 22 (two stretches in a row; the bytes 14).  (Their first forms took 107 together; with
-// the keys in LDS the plan took 38.)  Many are bound by the bytes: 32 requests of 300 to 9000 rows cut to about half into other FP8 pages, 0.44 GB 112 us: the plan
-// 17, the move 80 to 91, 4.4 to 5 TB/s.
+// the keys in LDS the plan took 38.)  Many are bound by the bytes: 32 requests of 300 to 9000 rows cut to about half into other FP8 pages,
+// 0.44 GB 112 us: the plan 17, the move 80 to 91, 4.4 to 5 TB/s.
 #include "tile_attn.h"
 
 namespace lfps {

@@ -222,7 +222,7 @@ def test_a_query_of_nan_counts_for_the_rows_it_sees(dtype, G, t, n):
 
 @pytest.mark.parametrize("dtype", ["bf16", "f16", "fp8k", "f32"])
 @pytest.mark.parametrize("Hq,news,lens,held", [(4, [9, 5, 3, 0], [3, 20, 0, 8], [1, 17, 0, 8]), (1, [128, 1], [200, 1], [72, 0]), (2, [64, 65], [64, 300], [0, 235]),
-                                               (4, [32, 33, 1], [32, 129, 5000], [0, 96, 4999])])
+                                               (4, [32, 33, 1], [32, 129, 5000], [0, 96, 4999]), (4, [64, 65, 1], [3000, 70, 1], [2936, 5, 0]), (2, [128], [128], [0])])
 def test_few_tokens_of_some_requests(dtype, Hq, news, lens, held):
     """Tokens at no row, one block of queries and a row more, requests of few tokens beside others."""
     c = CacheCase(dtype, Hq, 1, lens, 16, seed=len(news) + Hq)
