@@ -11,7 +11,7 @@
 // Long prompts are bound by the vector unit: a score costs three instructions, one of them an exponential of four times an ordinary one's cycles, in either
 // kernel (81 % of the busy SIMDs' time in the first).  32 heads over 8 KV heads: 8192 tokens in bf16 620 us, two products of 550 GFLOP in all at 890 TFLOP/s;
 // prompts of 5449 and 7958 tokens over FP8 pages 842 to 880 (by the profiler k_mass_stats 475, k_mass_add 460, k_mass_sum 5).  Requests of few tokens
-// (k_mass_add_few) are bound by the bytes of K, read twice: 32 tokens over 32768 rows 37 us, 20 + 4.7 + 18 by the profiler, where K's 67 MB are 14.
+// (k_mass_few) are bound by the bytes of K, read twice: 32 tokens over 32768 rows 37 to 40 us by the card, 17.6 + 4.7 + 18.5 by the profiler, where K's 67 MB are 14.
 #include "tile_attn.h"
 
 namespace lfps {
@@ -26,10 +26,10 @@ constexpr float kMassUnit = kLog2e * 0.08838834764831845f;      // from products
 
 // Blocks of 32 rows that a wave keeps in registers: of 16-bit operands two, so that a row read from LDS serves two products.  A stage of streamed
 // rows is 16 KB.
-template <typename Op, int kBlocks_ = std::is_same<Op, float>::value ? 1 : 2>
+template <typename Op>
 struct MassShape {
   static constexpr bool kF32 = std::is_same<Op, float>::value;
-  static constexpr int kBlocks = kBlocks_, kMine = 32 * kBlocks, kRows = kMassWaves * kMine;       // of a wave; of a workgroup
+  static constexpr int kBlocks = kF32 ? 1 : 2, kMine = 32 * kBlocks, kRows = kMassWaves * kMine;       // of a wave; of a workgroup
   static constexpr int kRowBytes = kF32 ? 512 : 256, kStage = kF32 ? 32 : 64, kSubs = kStage / 32, kBytes = kStage * kRowBytes;
 };
 
@@ -46,7 +46,7 @@ struct MassArgs {
   float* split_stats;              // [splits, Hkv, t1 - t0, G, 2] of its parts, if there are several: the sums themselves
   int32_t splits;
   int32_t chunks;                  // of the query rows of a request
-  int32_t few_rows;                // requests of up to so many query rows are k_mass_add_few's (-1: none, not even those of no tokens)
+  int32_t few_rows;                // requests of up to so many query rows are k_mass_few's (-1: none, not even those of no tokens)
   float* sums;                     // [chunks, B * Hkv, Lcap] what the chunks of query rows leave for the rows that they see, if there are several
   float* mass;
 };
@@ -144,12 +144,11 @@ __device__ __forceinline__ int launch_tokens(const A& a, int b, int* c0, int* c1
 // Stage j of keys is in LDS slot j % 4.  While a wave's weights of 32 keys are made, the products of the next 32 run; when the last 32 of stage j - 1
 // are, a barrier says that nobody reads its slot any more and that stage j is there, and stage j + 3 is asked for (FP8: it comes from registers when
 // its turn is next but one).
-// kBlocks: blocks of 32 rows of a wave.  Where the requests have no more than 128 query rows each, one block gives all four waves some: 32 tokens of
-// 32 heads over 32768 rows 25 -> 21 us.
-template <typename TK, typename TQ, int kBlocks>
+template <typename TK, typename TQ>
 __global__ __launch_bounds__(kMassThreads, sizeof(TK) == 4 ? 1 : 2) void k_mass_stats(MassArgs<TQ> a, int tiles) {
   typedef typename InLds<TQ>::Op Op;
-  typedef MassShape<Op, kBlocks> M;
+  typedef MassShape<Op> M;
+  constexpr int kBlocks = M::kBlocks;
   __shared__ __attribute__((aligned(16))) char lds_[kMassRing * M::kBytes];
   const Shape& s = a.s;
   const int G = s.G, shift = G == 4 ? 2 : G - 1, per = M::kRows / G;
@@ -162,7 +161,7 @@ __global__ __launch_bounds__(kMassThreads, sizeof(TK) == 4 ? 1 : 2) void k_mass_
   int c0, c1;
   const int first = launch_tokens(a, b, &c0, &c1);
   const int row0 = (x - first_tile(b)) * M::kRows, rows = c1 > c0 ? (c1 - c0) << shift : 0;
-  if (row0 < 0 || row0 >= rows) return;
+  if (row0 < 0 || row0 >= rows || (a.few_rows == 128 && rows <= 128)) return;      // (of 256 rows k_mass_few's statistics spill registers: 64 / 60 us in all)
   const int lane = threadIdx.x & 63, wave = wave_of(), n = lane & 31, h = lane >> 5;
   auto seen = [&](int m) {                                     // keys that query row m sees
     const int y = first + c0 + (m >> shift) + 1;
@@ -506,115 +505,172 @@ __global__ __launch_bounds__(kMassThreads, sizeof(TK) == 4 ? 1 : 2) void k_mass_
 // A lane's operands of a row of the cache as they are stored.
 template <typename TK, typename Op>
 struct MassRaw {
-  typedef typename std::conditional<sizeof(TK) == 1, u32x2, Op>::type Chunk;
-  Chunk x[8];
+  static constexpr int kChunks = sizeof(TK) == 4 ? 16 : 8;
+  typedef typename std::conditional<sizeof(TK) == 1, u32x2, typename std::conditional<sizeof(TK) == 4, f32x4, Op>::type>::type Chunk;
+  Chunk x[kChunks];
   __device__ __forceinline__ void load(const TK* p, int h) {
 #pragma unroll
-    for (int c = 0; c < 8; ++c) x[c] = *reinterpret_cast<const Chunk*>(p + 16 * c + 8 * h);
+    for (int c = 0; c < kChunks; ++c) x[c] = *reinterpret_cast<const Chunk*>(p + kD / kChunks * c + kD / kChunks / 2 * h);
   }
-  __device__ __forceinline__ Op chunk(int c) const {
+  __device__ __forceinline__ auto chunk(int c) const {
     if constexpr (sizeof(TK) == 1) return fp8x8_to<Op>(x[c][0], x[c][1]);
     else return x[c];
   }
 };
 
-// The weights of requests of few query rows: all of them stay in LDS, and a wave streams keys through its registers, 32 at a time, the next ones on their
-// way, with nobody to wait for (32 tokens of 32 heads over 32768 rows 29.9 -> 18.4 us, where k_mass_add waits for its keys, then for the queries, and
-// has two stages of work; for 512 / 768 / 1024 / 1536 workgroups 19.7 / 18.4 / 21.3 / 21.4.  Statistics joined here: 24.1, where k_mass_join takes 4.7,
-// and 44 us in all for 40.6; 64 tokens, 256 rows, 70 -> 60 in all).  kFew: query rows that there is room for.  grid (B * Hkv, parts: steps of 128 keys in turn)
-template <typename TK, typename TQ, int kFew>
-__global__ __launch_bounds__(kMassThreads, kFew == 128 ? 3 : 2) void k_mass_add_few(MassArgs<TQ> a, int parts) {
-  request_arguments<decltype(&k_mass_add_few<TK, TQ, kFew>)>();
+// Requests of few query rows, up to kFew: all of these stay in LDS, and a wave streams keys of its own through its registers, 32 at a time, the next ones on
+// their way, with nobody to wait for.  kStats: the rows' largest scores and sums over my keys (grid y: a part of them each); else the weights (in turn).
+// grid (B * Hkv, parts: steps of 128 keys in turn).  32 tokens of 32 heads over 32768 rows: statistics 19.6 -> 17.6 us, where only the waves with query
+// rows of their own had work in k_mass_stats; weights 29.9 -> 18.4, where k_mass_add waits for its keys, then for the queries, and has two stages of work (for
+// 512 / 768 / 1024 / 1536 workgroups 19.7 / 18.4 / 21.3 / 21.4; statistics joined here: 24.1, where k_mass_join takes 4.7, and 44 us in all for 40.6).
+// 64 tokens, 256 rows: 70 -> 60 us in all.  fp32, six requests of 4 to 40 tokens of 4 heads over 9000 to 20600 rows: 159 -> 123 us, kernels that
+// find no request among them.
+template <typename TK, typename TQ, int kFew, bool kStats>
+__global__ __launch_bounds__(kMassThreads, !kStats && kFew == 128 && sizeof(TQ) == 2 ? 3 : 2) void k_mass_few(MassArgs<TQ> a, int parts) {
+  request_arguments<decltype(&k_mass_few<TK, TQ, kFew, kStats>)>();
   typedef typename InLds<TQ>::Op Op;
-  constexpr int kSubs = kFew / 32, kStep = 32 * kMassWaves;
-  __shared__ __attribute__((aligned(16))) char lds_[kFew * 256];
+  typedef MassShape<Op> M;
+  constexpr int kSubs = kFew / 32, kStep = 32 * kMassWaves, kPieces = M::kRowBytes / 16, kMinePieces = kFew * kPieces / kMassThreads;
+  __shared__ __attribute__((aligned(16))) char lds_[kFew * M::kRowBytes + (kStats ? kMassWaves * kFew * 8 : 0)];
   const Shape& s = a.s;
   const int G = s.G, shift = G == 4 ? 2 : G - 1, bg = blockIdx.x, b = bg / s.Hkv, g = bg % s.Hkv, len = length_of(s, a.kv.seq_lens, b);
   const int lane = threadIdx.x & 63, wave = wave_of(), n = lane & 31, h = lane >> 5;
   int at = kStep * (int)blockIdx.y;
-  if (at >= len) return;
+  if (at >= len && !kStats) return;
   int c0, c1;
   const int first = launch_tokens(a, b, &c0, &c1), rows = c1 > c0 ? (c1 - c0) << shift : 0, subs = (rows + 31) / 32;
-  if (rows > a.few_rows) return;
+  if (rows > a.few_rows || (kStats && rows == 0)) return;
   lds_char* const lds = (lds_char*)lds_;
   const CacheRows<TK> K(a.kv.k, a.kv, b, g);
   auto my_row = [&](int step) {
     const int r = step + 32 * wave + n;
     return r < len ? r : len - 1;
   };
-  int entry = K.entry(my_row(at));
-  u32x4 x[2 * kSubs];                                          // my pieces of the queries; rows that are not there are 0
-#pragma unroll
-  for (int i = 0; i < 2 * kSubs; ++i) {
-    const int piece = (int)threadIdx.x + kMassThreads * i, r = piece / 16;
-    x[i] = u32x4{0, 0, 0, 0};
-    if (r < rows)
-      x[i] = *reinterpret_cast<const u32x4*>(a.q + (int64_t)(c0 + (r >> shift)) * a.q_stride + (g * G + (r & (G - 1))) * kD + 8 * chunk_place(r, piece % 16));
-  }
+  const int64_t count = a.t1 - a.t0, row0 = ((int64_t)g * count + (c0 - a.t0)) * G;      // of the statistics
+  float top[kSubs], l[kSubs];
   f32x2t st[kSubs];
 #pragma unroll
   for (int u = 0; u < kSubs; ++u) {
-    st[u] = f32x2t{0.f, 0.f};                                  // (their weights too)
-    if (32 * u + n < rows) st[u] = *reinterpret_cast<const f32x2t*>(a.stats + 2 * (((int64_t)g * (a.t1 - a.t0) + (c0 - a.t0)) * G + 32 * u + n));
+    top[u] = -INFINITY;
+    l[u] = 0.f;
+    st[u] = f32x2t{0.f, 0.f};                                  // (of rows that are not there: their weights too)
   }
-  MassRaw<TK, Op> raw;
-  raw.load(K.at(my_row(at), entry), h);
-  const int stride = kStep * parts;
-  entry = K.entry(my_row(at + stride));
+  if (at < len) {
+    int entry = K.entry(my_row(at));
+    u32x4 x[kMinePieces];                                      // my pieces of the queries; rows that are not there are 0
 #pragma unroll
-  for (int i = 0; i < 2 * kSubs; ++i) *(__attribute__((address_space(3))) u32x4*)(lds + 16 * ((int)threadIdx.x + kMassThreads * i)) = x[i];
-  __syncthreads();
-  const int held = a.held ? a.held[b] : 0;
-  for (; at < len; at += stride) {
-    MassRow<Op> k[1];
-#pragma unroll
-    for (int c = 0; c < 8; ++c) k[0].x[c] = raw.chunk(c);
-    if (at + stride < len) {
-      raw.load(K.at(my_row(at + stride), entry), h);
-      entry = K.entry(my_row(at + 2 * stride));
+    for (int i = 0; i < kMinePieces; ++i) {
+      const int piece = (int)threadIdx.x + kMassThreads * i, r = piece / kPieces, place = piece % kPieces;
+      const int chunk = M::kF32 ? chunk_place_f32(r, place) : chunk_place(r, place);
+      x[i] = u32x4{0, 0, 0, 0};
+      if (r < rows)
+        x[i] = *reinterpret_cast<const u32x4*>(a.q + (int64_t)(c0 + (r >> shift)) * a.q_stride + (g * G + (r & (G - 1))) * kD + 16 / (int)sizeof(TQ) * chunk);
     }
-    const int key0 = at + 32 * wave;
-    if (key0 >= len) continue;
-    const int mine = key0 + key_of(lane & 15, h);              // the key whose sum I have in the end
-    float* const to = a.mass + (int64_t)bg * s.Lcap + mine;
-    const float old = mine < len && (a.t0 > 0 || mine < held) ? *to * (a.t0 > 0 ? 1.f : a.decay) : 0.f;
-    float sum[16];
+    if constexpr (!kStats) {
 #pragma unroll
-    for (int r = 0; r < 16; ++r) sum[r] = 0.f;
-    const bool all_seen = key0 + 31 <= first + c0;
+      for (int u = 0; u < kSubs; ++u)
+        if (32 * u + n < rows) st[u] = *reinterpret_cast<const f32x2t*>(a.stats + 2 * (row0 + 32 * u + n));
+    }
+    MassRaw<TK, Op> raw;
+    raw.load(K.at(my_row(at), entry), h);
+    const int stride = kStep * parts;
+    entry = K.entry(my_row(at + stride));
 #pragma unroll
-    for (int u = 0; u < kSubs; ++u) {
-      if (u >= subs) break;
-      f32x16 y[1];
-      mass_scores<false, Op, 1>(y, lds + 32 * u * 256, k, n, h, [](int) {});
-      float top = st[u][0], factor = st[u][1];
-      if (!all_seen) {                                         // (as in k_mass_add)
-        const int m = 32 * u + n, pos = m < rows ? first + c0 + (m >> shift) - key0 : -1;
-        const bool none = factor != factor;
-        if (none) top = factor = 0.f;
+    for (int i = 0; i < kMinePieces; ++i) *(__attribute__((address_space(3))) u32x4*)(lds + 16 * ((int)threadIdx.x + kMassThreads * i)) = x[i];
+    __syncthreads();
+    const int held = a.held ? a.held[b] : 0;
+    for (; at < len; at += stride) {
+      MassRow<Op> k[1];
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const float v = none ? __builtin_nanf("") : y[0][r];
-          y[0][r] = key_of(r, h) <= pos ? v : -INFINITY;
+      for (int c = 0; c < MassRaw<TK, Op>::kChunks; ++c) k[0].x[c] = raw.chunk(c);
+      if (at + stride < len) {
+        raw.load(K.at(my_row(at + stride), entry), h);
+        entry = K.entry(my_row(at + 2 * stride));
+      }
+      const int key0 = at + 32 * wave;
+      if (key0 >= len) continue;
+      const int mine = key0 + key_of(lane & 15, h);            // the key whose sum I have in the end
+      float* const to = a.mass + (int64_t)bg * s.Lcap + mine;
+      float old = 0.f;
+      if constexpr (!kStats) old = mine < len && (a.t0 > 0 || mine < held) ? *to * (a.t0 > 0 ? 1.f : a.decay) : 0.f;
+      float sum[16];
+#pragma unroll
+      for (int r = 0; r < 16; ++r) sum[r] = 0.f;
+      const bool all_seen = key0 + 31 <= first + c0;
+#pragma unroll
+      for (int u = 0; u < kSubs; ++u) {
+        if (u >= subs) break;
+        f32x16 y[1];
+        mass_scores<false, Op, 1>(y, lds + 32 * u * M::kRowBytes, k, n, h, [](int) {});
+        float from = st[u][0], factor = st[u][1];
+        if (!all_seen) {                                       // (as in k_mass_add)
+          const int m = 32 * u + n, pos = m < rows ? first + c0 + (m >> shift) - key0 : -1;
+          const bool none = !kStats && factor != factor;
+          if (none) from = factor = 0.f;
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const float v = none ? __builtin_nanf("") : y[0][r];
+            y[0][r] = key_of(r, h) <= pos ? v : -INFINITY;
+          }
+        }
+        if constexpr (kStats) {
+          float mx = fmaxf(y[0][0], y[0][1]);
+#pragma unroll
+          for (int r = 2; r < 16; r += 2) mx = fmaxf(fmaxf(mx, y[0][r]), y[0][r + 1]);
+          mx *= kMassUnit;
+          const bool grows = mx > top[u] + kMassLazy;
+          const float shrink = grows ? __builtin_amdgcn_exp2f(top[u] - mx) : 1.f;      // (0 on the first keys)
+          top[u] = grows ? mx : top[u];
+          from = top[u] == -INFINITY ? 0.f : top[u];
+          float e[4] = {l[u] * shrink, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int r = 0; r < 16; ++r) e[r % 4] += __builtin_amdgcn_exp2f(fmaf(y[0][r], kMassUnit, -from));
+          l[u] = (e[0] + e[1]) + (e[2] + e[3]);
+          __builtin_amdgcn_sched_barrier(0);                   // (registers: one block's products at a time)
+        } else {
+#pragma unroll
+          for (int r = 0; r < 16; ++r) sum[r] = fmaf(__builtin_amdgcn_exp2f(fmaf(y[0][r], kMassUnit, -from)), factor, sum[r]);
         }
       }
-#pragma unroll
-      for (int r = 0; r < 16; ++r) sum[r] = fmaf(__builtin_amdgcn_exp2f(fmaf(y[0][r], kMassUnit, -top)), factor, sum[r]);
-    }
-    // over the 32 lanes of a half: lane j of 16 is left with the sum of product j
+      if constexpr (!kStats) {
+        // over the 32 lanes of a half: lane j of 16 is left with the sum of product j
 #define LFPS_HALVE(W, GIVEN)                                                      \
   _Pragma("unroll") for (int i = 0; i < W; ++i) {                                 \
-    const bool up = lane & W;                                                     \
-    const float keep = up ? sum[i + W] : sum[i], give = up ? sum[i] : sum[i + W]; \
-    sum[i] = keep + GIVEN;                                                        \
+        const bool up = lane & W;                                                     \
+        const float keep = up ? sum[i + W] : sum[i], give = up ? sum[i] : sum[i + W]; \
+        sum[i] = keep + GIVEN;                                                        \
   }
-    LFPS_HALVE(8, row16_rotate<8>(give))
-    LFPS_HALVE(4, __shfl_xor(give, 4))
-    LFPS_HALVE(2, __shfl_xor(give, 2))
-    LFPS_HALVE(1, __shfl_xor(give, 1))
+        LFPS_HALVE(8, row16_rotate<8>(give))
+        LFPS_HALVE(4, __shfl_xor(give, 4))
+        LFPS_HALVE(2, __shfl_xor(give, 2))
+        LFPS_HALVE(1, __shfl_xor(give, 1))
 #undef LFPS_HALVE
-    const float total = sum[0] + __shfl_xor(sum[0], 16);
-    if (!(lane & 16) && mine < len) *to = total + old;
+        const float total = sum[0] + __shfl_xor(sum[0], 16);
+        if (!(lane & 16) && mine < len) *to = total + old;
+      }
+    }
+  }
+  if constexpr (kStats) {
+    // a row's parts: of the two halves of a wave, then of the four waves
+    typedef __attribute__((address_space(3))) f32x2t* Parts;
+    const Parts left = (Parts)(lds + kFew * M::kRowBytes);
+    auto from_there = [](float t, float y, float mx) { return y != y ? y : (t == -INFINITY ? 0.f : y * __builtin_amdgcn_exp2f(t - mx)); };
+#pragma unroll
+    for (int u = 0; u < kSubs; ++u) {
+      const float other_top = __shfl_xor(top[u], 32), other = __shfl_xor(l[u], 32), mx = fmaxf(top[u], other_top);
+      if (h == 0) left[wave * kFew + 32 * u + n] = f32x2t{mx, from_there(top[u], l[u], mx) + from_there(other_top, other, mx)};
+    }
+    __syncthreads();
+    const int m = threadIdx.x;
+    if (m < rows) {
+      float mx = -INFINITY, sum = 0.f;
+#pragma unroll
+      for (int w = 0; w < kMassWaves; ++w) mx = fmaxf(mx, left[w * kFew + m][0]);
+#pragma unroll
+      for (int w = 0; w < kMassWaves; ++w) sum += from_there(left[w * kFew + m][0], left[w * kFew + m][1], mx);
+      if (a.splits > 1) *reinterpret_cast<f32x2t*>(a.split_stats + 2 * (blockIdx.y * count * s.Hq + row0 + m)) = f32x2t{mx, sum};
+      else *reinterpret_cast<f32x2t*>(a.stats + 2 * (row0 + m)) = f32x2t{mx == -INFINITY ? 0.f : mx, sum == 0.f ? 0.f : 1.f / sum};
+    }
   }
 }
 
@@ -642,10 +698,22 @@ template <typename TK, typename TQ>
 static hipError_t mass_t(MassArgs<TQ> a, float* work, int64_t room, hipStream_t st) {
   typedef MassShape<typename InLds<TQ>::Op> M;
   const int64_t most = room / 2 / a.s.Hq;                            // tokens that the workspace has room for
-  typedef MassShape<typename InLds<TQ>::Op, 1> Few;
-  const bool few = (int64_t)a.n_tokens * a.s.G <= (int64_t)Few::kRows * a.s.B;
-  const int per = (few ? Few::kRows : M::kRows) / a.s.G;
-  const int64_t masses = (int64_t)a.s.B * a.s.Hkv * a.s.Lcap;
+  // (by the average: what a request has is known on the device)
+  const int64_t all = (int64_t)a.n_tokens * a.s.G, wide = M::kF32 ? 128 : 256;
+  a.few_rows = all <= (int64_t)128 * a.s.B ? 128 : (all <= wide * a.s.B ? (int)wide : -1);
+  const int per = M::kRows / a.s.G;
+  const int64_t groups = (int64_t)a.s.B * a.s.Hkv, masses = groups * a.s.Lcap, steps = (a.s.Lcap + 32 * kMassWaves - 1) / (32 * kMassWaves);
+  auto few = [&](auto stats, int64_t workgroups, int64_t most_parts) {
+    constexpr bool kStats = decltype(stats)::value;
+    int64_t parts = (workgroups + groups - 1) / groups;
+    parts = parts < steps ? parts : steps;
+    parts = parts < most_parts ? parts : most_parts;
+    parts = parts < 1 ? 1 : parts;
+    if (kStats) a.splits = (int)parts;
+    const dim3 grid((unsigned)groups, (unsigned)parts);
+    if (kStats || a.few_rows == 128) hipLaunchKernelGGL((k_mass_few<TK, TQ, 128, kStats>), grid, dim3(kMassThreads), 0, st, a, (int)parts);
+    else hipLaunchKernelGGL((k_mass_few<TK, TQ, M::kF32 ? 128 : 256, false>), grid, dim3(kMassThreads), 0, st, a, (int)parts);
+  };
   for (int t0 = 0; t0 == 0 || t0 < a.n_tokens; t0 = a.t1) {           // (also of no tokens: what is held decays)
     a.t0 = t0;
     a.t1 = a.n_tokens - t0 > most ? t0 + (int)most : a.n_tokens;
@@ -654,17 +722,19 @@ static hipError_t mass_t(MassArgs<TQ> a, float* work, int64_t room, hipStream_t 
     a.stats = work;
     a.split_stats = a.sums = work + 2 * rows;                         // (the parts are joined before there are sums)
     const int64_t queries = (int64_t)n * a.s.G;
-    a.few_rows = sizeof(TQ) == 4 ? -1 : (few ? 128 : ((int64_t)a.n_tokens * a.s.G <= 256 * (int64_t)a.s.B ? 256 : -1));
     const bool others = queries > a.few_rows;                         // (else no request has more)
     if (n > 0) {
-      const int64_t groups = (int64_t)tiles * a.s.Hkv, by_len = (a.s.Lcap + 255) / 256;
-      int64_t splits = ((few ? 1024 : 512) + groups - 1) / groups;      // (of the few ones' tiles half may be empty)
-      if (splits * rows * 2 > left) splits = left / 2 / rows;
-      if (splits > by_len) splits = by_len;
-      a.splits = (int)(splits > kMaxSplits ? kMaxSplits : (splits < 1 ? 1 : splits));
-      const dim3 grid((unsigned)(groups * a.splits));
-      if (few) hipLaunchKernelGGL((k_mass_stats<TK, TQ, 1>), grid, dim3(kMassThreads), 0, st, a, tiles);
-      else hipLaunchKernelGGL((k_mass_stats<TK, TQ, M::kBlocks>), grid, dim3(kMassThreads), 0, st, a, tiles);
+      const int64_t by_room = left / 2 / rows < kMaxSplits ? left / 2 / rows : kMaxSplits;
+      if (a.few_rows == 128) {
+        few(std::true_type{}, 512, by_room);
+      } else {
+        const int64_t tile_groups = (int64_t)tiles * a.s.Hkv, by_len = (a.s.Lcap + 255) / 256;
+        int64_t splits = (512 + tile_groups - 1) / tile_groups;
+        if (splits > by_room) splits = by_room;
+        if (splits > by_len) splits = by_len;
+        a.splits = (int)(splits < 1 ? 1 : splits);
+      }
+      if (others || a.few_rows != 128) hipLaunchKernelGGL((k_mass_stats<TK, TQ>), dim3((unsigned)(tiles * a.s.Hkv * a.splits)), dim3(kMassThreads), 0, st, a, tiles);
       if (a.splits > 1)
         hipLaunchKernelGGL(k_mass_join, dim3((unsigned)((rows + 15) / 16)), dim3(256), 0, st, a.split_stats, a.stats, rows, a.splits);
     }
@@ -675,15 +745,7 @@ static hipError_t mass_t(MassArgs<TQ> a, float* work, int64_t room, hipStream_t 
     if (chunks > (queries + kMassChunk - 1) / kMassChunk) chunks = (queries + kMassChunk - 1) / kMassChunk;
     if (chunks * masses > left) chunks = left / masses;
     a.chunks = (int)(chunks < 1 ? 1 : chunks);
-    if constexpr (sizeof(TQ) == 2) {
-      if (a.few_rows > 0) {
-        const int64_t groups = (int64_t)a.s.B * a.s.Hkv, steps = (a.s.Lcap + 32 * kMassWaves - 1) / (32 * kMassWaves), most = ((few ? 768 : 512) + groups - 1) / groups;
-        const int parts = (int)(steps < most ? steps : most);
-        const dim3 grid((unsigned)groups, (unsigned)parts);
-        if (few) hipLaunchKernelGGL((k_mass_add_few<TK, TQ, 128>), grid, dim3(kMassThreads), 0, st, a, parts);
-        else hipLaunchKernelGGL((k_mass_add_few<TK, TQ, 256>), grid, dim3(kMassThreads), 0, st, a, parts);
-      }
-    }
+    if (a.few_rows > 0) few(std::false_type{}, a.few_rows == 128 && !M::kF32 ? 768 : 512, steps);
     if (others) hipLaunchKernelGGL((k_mass_add<TK, TQ>), dim3((unsigned)(a.s.B * a.s.Hkv), (unsigned)key_tiles, (unsigned)a.chunks), dim3(kMassThreads), 0, st, a);
     if (others && a.chunks > 1)
       hipLaunchKernelGGL((k_mass_sum<M::kRows, M::kStage, MassArgs<TQ>>), dim3((unsigned)((a.s.Lcap + 255) / 256), (unsigned)(a.s.B * a.s.Hkv)), dim3(256), 0, st, a);
