@@ -523,8 +523,8 @@ struct MassRaw {
 // grid (B * Hkv, parts: steps of 128 keys in turn).  32 tokens of 32 heads over 32768 rows: statistics 19.6 -> 17.6 us, where only the waves with query
 // rows of their own had work in k_mass_stats; weights 29.9 -> 18.4, where k_mass_add waits for its keys, then for the queries, and has two stages of work (for
 // 512 / 768 / 1024 / 1536 workgroups 19.7 / 18.4 / 21.3 / 21.4; statistics joined here: 24.1, where k_mass_join takes 4.7, and 44 us in all for 40.6).
-// 64 tokens, 256 rows: 70 -> 60 us in all.  fp32, six requests of 4 to 40 tokens of 4 heads over 9000 to 20600 rows: 159 -> 123 us, kernels that
-// find no request among them.
+// 64 tokens, 256 rows: 70 -> 60 us in all.  fp32, six requests of 4 to 40 tokens of 4 heads over 9000 to 20600 rows: 159 -> 123 us, of which
+// ten are launches that find no request of more.
 template <typename TK, typename TQ, int kFew, bool kStats>
 __global__ __launch_bounds__(kMassThreads, !kStats && kFew == 128 && sizeof(TQ) == 2 ? 3 : 2) void k_mass_few(MassArgs<TQ> a, int parts) {
   request_arguments<decltype(&k_mass_few<TK, TQ, kFew, kStats>)>();
