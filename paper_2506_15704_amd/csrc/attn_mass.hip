@@ -603,7 +603,8 @@ __global__ __launch_bounds__(kMassThreads, !kStats && kFew == 128 && sizeof(TQ) 
         f32x16 y[1];
         mass_scores<false, Op, 1>(y, lds + 32 * u * M::kRowBytes, k, n, h, [](int) {});
         float from = st[u][0], factor = st[u][1];
-        if (!all_seen) {                                       // (as in k_mass_add)
+        // (as in k_mass_add; and a row that is not there is 0, whose product with an infinity is not, so that no statistics hide it)
+        if (!all_seen || (!kStats && 32 * u + 32 > rows)) {
           const int m = 32 * u + n, pos = m < rows ? first + c0 + (m >> shift) - key0 : -1;
           const bool none = !kStats && factor != factor;
           if (none) from = factor = 0.f;

@@ -245,6 +245,35 @@ def test_keys_of_minus_infinity_weigh_nothing_to_few_tokens(dtype):
     c.ctx.close()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("G,t", [(1, 3), (1, 33), (1, 100), (2, 50), (4, 1), (4, 3), (4, 8), (4, 40), (4, 59)])
+def test_infinite_keys_weigh_nothing_to_few_tokens_far_behind_them(dtype, sign, G, t):
+    """All tokens see all of these keys; the last block of 32 query rows is full, or is not."""
+    n = 500
+    c = CacheCase(dtype, 2 * G, 2, [n, 9], seed=t)
+    c.K[..., 5] = 0
+    hidden = torch.zeros(n, dtype=torch.bool, device=DEV)
+    hidden[:40] = hidden[100:131] = hidden[300] = True
+    c.K[0, :, :n, 5] = torch.where(hidden, -sign * float("inf"), 0.0).to(c.kd)
+    q = c.randn(t + 9, 2 * G, D).to(c.q_dtype)
+    q[..., 5] = sign
+    mass = torch.full((2, 2, n), 7.0, device=DEV)
+    c.ctx.lfps_attn_mass(q, ints([0, t, t + 9]), c.kv, mass)
+    j = torch.arange(n, device=DEV)[~hidden]
+    for g in range(2):
+        assert not bool(mass[0, g, hidden].any())
+        K = c.values(c.K, 0, 0, n)[g][j]
+        x = q[:t, g * G:g * G + G].double().reshape(t * G, D)
+        unseen = j > torch.arange(n - t, n, device=DEV).repeat_interleave(G).view(-1, 1)
+        w = torch.softmax((x @ K.T.contiguous() / D ** 0.5).masked_fill(unseen, float("-inf")), 1)
+        dots = (x.abs() @ K.abs().T.contiguous() / D ** 0.5).masked_fill(unseen, 0).amax(1, keepdim=True)
+        tol = (w * _relative(dots, n)).sum(0) + (t * G + 4) * 2.0 ** -24 * w.sum(0) + 1e-30
+        assert bool(((mass[0, g, j].double() - w.sum(0)).abs() <= tol).all())
+    assert bool(mass[1, :, :9].isfinite().all())
+    c.ctx.close()
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_keys_of_minus_infinity_weigh_nothing(dtype):
     n = 150
