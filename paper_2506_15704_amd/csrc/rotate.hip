@@ -3,9 +3,9 @@
 // ((a, b) -> (a cos - b sin, b cos + a sin), angle = position[axis of the pair] * frequency of the pair), and keys and values go into the
 // cache as lfps_append puts them there, each value rounded once.
 //
-// An angle is reduced in 64 bits: position * frequency / 2 pi as a product and its rounding error, of which the nearest quarter turn is
-// taken off before it becomes fp32, so that a position of 2^24 is turned as exactly as one of 16; the sine and cosine of what is left, at
-// most pi / 4, are their Taylor sums.  A wave has a token's angles, made by a lane a pair, and serves eight or sixteen of its head rows; other
+// An angle is reduced in 64 bits: position * frequency (up to 55 bits) as a product and its rounding error, and of it / 2 pi whole turns taken off before
+// the product is rounded, then the nearest quarter turn before it becomes fp32, so that a position of 2^31 is turned as exactly as one of 16; the sine
+// and cosine of what is left, at most pi / 4, are their Taylor sums.  A wave has a token's angles, made by a lane a pair, and serves eight or sixteen of its head rows; other
 // waves make them again.
 //
 // Bound by the bytes: eight prompts of 1000 to 6000 tokens, 32 + 16 heads in bf16, 0.63 GB in and out, 116 us, 5.4 TB/s (a large copy reaches 5.0; part
@@ -20,9 +20,8 @@ namespace {
 // 2 pi * turns -> cosine and sine
 __device__ __forceinline__ f32x2t turn(int position, float frequency) {
   constexpr double kHi = 0.15915494309189535, kLo = -9.8393381857794e-18;      // 1 / (2 pi)
-  const double p = (double)position * (double)frequency;
-  const double x = p * kHi;
-  double f = x - __builtin_rint(x) + (fma(p, kHi, -x) + p * kLo);
+  const double p = (double)position * (double)frequency, rest = fma((double)position, (double)frequency, -p);
+  double f = fma(p, kHi, -__builtin_rint(p * kHi)) + fma(p, kLo, rest * kHi);
   const double quarter = __builtin_rint(4.0 * f);
   f -= 0.25 * quarter;
   const float y = (float)(f * 6.283185307179586), z = y * y;

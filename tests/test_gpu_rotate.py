@@ -1,4 +1,6 @@
 """Norms and turns of the newest tokens' heads on their way into the cache, against the formulas in 64 bits."""
+import math
+
 import pytest
 import torch
 
@@ -153,6 +155,34 @@ def test_a_position_far_out_is_turned_as_exactly_as_a_near_one():
     c.ctx.lfps_rotate_append(c.ctx.rotary(inv_freq=freq), x, v, v, pos.to(torch.int32), ints([0, 64]), c.kv, out)
     ref, size = _turned(x, None, 0, pos, [0] * 64, freq, False)
     assert bool(((out.double() - ref).abs() <= (2.0 ** -21 + 80 * 2.0 ** -24) * size).all())
+    c.ctx.close()
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_sines_of_far_positions_near_whole_half_turns(interleaved):
+    """Pairs (0, 1) become (-sin, cos) with no rounding of their own.  Position and frequency have 55 bits together, so the angle is taken here as a sum
+    of two that 64 bits hold.  The reduced angle is rounded once (2^-24 of it), its sine's and cosine's sums twice more: less than 4 * 2^-24 of either,
+    which is next to nothing where the sine is small.  The reduction in two terms leaves 2^-45."""
+    c = CacheCase("f32", 1, 1, [128], seed=8)
+    far = 2 ** 31 - torch.randint(1, 2 ** 29, (128,), device=DEV, generator=c.gen)
+    pos = torch.where(torch.arange(128, device=DEV) % 2 == 0, far, -far)
+    freq = 0.5 + 0.5 * torch.rand(64, device=DEV, generator=c.gen)
+    x, out = torch.zeros((128, 1, D), device=DEV), torch.zeros((128, 1, D), device=DEV)
+    first, second = (slice(0, None, 2), slice(1, None, 2)) if interleaved else (slice(0, 64), slice(64, None))
+    x[..., second] = 1
+    c.ctx.lfps_rotate_append(c.ctx.rotary(inv_freq=freq, interleaved=interleaved), x, x, x, pos.to(torch.int32), ints([0, 128]), c.kv, out)
+    got_sin, got_cos = -out[:, 0, first].double().cpu(), out[:, 0, second].double().cpu()
+    small = 0
+    for t, p in enumerate(pos.tolist()):
+        high, low = p >> 16 << 16, p & 0xFFFF
+        for i, f in enumerate(freq.double().tolist()):
+            a, b = high * f, low * f                                # (31 - 16 and 16 bits times 24: exact)
+            sin = math.sin(a) * math.cos(b) + math.cos(a) * math.sin(b)
+            cos = math.cos(a) * math.cos(b) - math.sin(a) * math.sin(b)
+            small += min(abs(sin), abs(cos)) < 2.0 ** -5
+            assert abs(float(got_sin[t, i]) - sin) <= 4 * 2.0 ** -24 * abs(sin) + 2.0 ** -45, (p, f)
+            assert abs(float(got_cos[t, i]) - cos) <= 4 * 2.0 ** -24 * abs(cos) + 2.0 ** -45, (p, f)
+    assert small > 100
     c.ctx.close()
 
 
