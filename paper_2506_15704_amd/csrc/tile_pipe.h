@@ -371,25 +371,24 @@ __device__ __forceinline__ lds_char* pipe_loop(char* lds_, const CacheRows<TK>& 
     fk_first[i].put(lds + i * kPipeStage, lane, wave);
     if (i < 2) fv_first[i].put(lds + kV + i * kPipeStage, lane, wave);
   };
-  // (what is asked for first, K of the first stage, is what the first products wait for)
   constexpr bool kDirect = Feed<TK, kKind, Op>::kDirect && Feed<TV, kKind, Op>::kDirect;
-  constexpr int kLoadsK = Feed<TK, kKind, Op>::kLoads, kLoadsV = Feed<TV, kKind, Op>::kLoads, kBehind = kDirect ? (kQuery ? kLoadsV : 2 * kLoadsK + 2 * kLoadsV) : 0;
+  constexpr int kBehind = kDirect ? Feed<TV, kKind, Op>::kLoads : 0;      // requests behind those for the queries
   ask_first(0);
-  if constexpr (!kQuery) {
-    ask_first(1);
-    ask_first(2);
-  }
-  __builtin_amdgcn_s_waitcnt(0x0f70 | kBehind);      // vmcnt(kBehind)
   if constexpr (kQuery) {
+    __builtin_amdgcn_s_waitcnt(0x0f70 | kBehind);      // vmcnt(kBehind)
     wave_lds_order();
     st.q.load(query_room(lds, wave), n, h);
-    __builtin_amdgcn_s_waitcnt(0xc07f);              // lgkmcnt(0): its place is free
+    __builtin_amdgcn_s_waitcnt(0xc07f);                // lgkmcnt(0): its place is free
+  } else {
+    ask_first(1);
+    ask_first(2);
   }
   put_first(0);
   if constexpr (!kQuery) {
     put_first(1);
     put_first(2);
   }
+  landed();      // (V of the first stage too: the early waves read all of it before the next barrier that has a wait in front of it)
   __syncthreads();
   if constexpr (kQuery) {
     ask_first(1);
