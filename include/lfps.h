@@ -313,7 +313,8 @@ typedef struct {
 } lfps_rotary;
 /*   q, k_new, v_new  [n_tokens, Hq or Hkv, D] of cfg.kv_dtype, element (t, h, c) at t*stride_t + h*D + c (slices of one fused projection; rows 16-byte
  *              aligned, stride_t >= Hq*D)
- *   positions  [n_axes, n_tokens] int32, any values; NULL: a token's cache row
+ *   positions  [n_axes, n_tokens] int32, any values; NULL: a token's cache row, which is its place in the text as long as no rows were evicted:
+ *              after lfps_evict new rows lie below the places at which the kept keys were turned, and positions have to be given
  *   q_out      [n_tokens, Hq, D], contiguous, 16-byte aligned, of q_out_dtype: LFPS_F32 (what the decode steps take: one token a request makes [B, Hq, D])
  *              or cfg.kv_dtype (lfps_prompt_attn, lfps_window_attn).  It must not overlap the inputs.  A token at no row gets zeros, rows of
  *              tokens of no request are left as they were.
@@ -345,7 +346,7 @@ int lfps_full_attn_mass_decode(lfps_ctx* ctx, const float* q, const lfps_kv* kv,
 
 /* Eviction: every KV head of request b keeps m_b = min(n_b, budget[b]) of its rows: the first n_sink, the n_recent newest (as far as there is room), and
  * between them those of the largest mass (of equal ones the lower rows; NaN counts as least).  The kept rows move to the front in order: row i of the
- * result is row kept[b,g,i] of K and V.  Keys stay as they were turned.
+ * result is row kept[b,g,i] of K and V.  Keys stay as they were turned: from then on lfps_rotate_append has to be given positions.
  *   mass, mass_out [B, Hkv, max_seq_len] fp32; mass_out[b,g,i] = mass[b,g,kept[b,g,i]]
  *   budget [B] int32, clamped to [0, n_b];  lens_out [B] int32: m_b
  *   kept   [B, Hkv, max_seq_len] int32.  Entries of mass_out and kept from m_b on are left as they were.

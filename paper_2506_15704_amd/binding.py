@@ -463,8 +463,8 @@ class Lfps:
 
     def lfps_rotate_append(self, rot: lfps_rotary, q, k_new, v_new, positions, cu, kv: lfps_kv, q_out):
         """q, k_new, v_new: [tokens, heads, D] of kv_dtype, packed (slices of one fused projection: equal token strides); positions: [n_axes, tokens]
-        int32, [tokens] for one axis, or None (the cache rows); q_out: [tokens, Hq, D], fp32 or kv_dtype.  The cache behind the view is
-        written."""
+        int32, [tokens] for one axis, or None (the cache rows: not after an eviction); q_out: [tokens, Hq, D], fp32 or kv_dtype.  The
+        cache behind the view is written."""
         d, T = self.device, int(q.shape[0])
         pq, sq = _token_rows(q, self.kv_torch_dtype, self.Hq, "q", d)
         pk, sk = _token_rows(k_new, self.kv_torch_dtype, self.Hkv, "k_new", d)

@@ -1,4 +1,5 @@
 """What rotation, windows, accumulated weights and eviction refuse, as far as it shows without a GPU, and the struct that describes a rotation."""
+import ast
 import ctypes
 import os
 import re
@@ -40,3 +41,16 @@ def test_weights_have_to_be_on_the_gpu():
         assert "q_weight" in str(e)
     else:
         raise AssertionError("a host tensor was taken")
+
+
+def test_the_documented_cache_that_evicts_turns_by_given_positions():
+    """After an eviction a token's row is not its place in the text."""
+    readme = open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(b.__file__))), "README.md")).read()
+    evicting = 0
+    for block in re.findall(r"```python\n(.*?)```", readme, flags=re.S):
+        calls = {n.func.attr: n for n in ast.walk(ast.parse(block)) if isinstance(n, ast.Call) and isinstance(n.func, ast.Attribute)}
+        if "lfps_evict" in calls:
+            evicting += 1
+            positions = calls["lfps_rotate_append"].args[4]
+            assert not (isinstance(positions, ast.Constant) and positions.value is None)
+    assert evicting
