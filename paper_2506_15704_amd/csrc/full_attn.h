@@ -13,10 +13,14 @@ constexpr int kAttnThreads = 256;       // full attention
 __host__ __device__ __forceinline__ int rows_per_split(int n, int n_split) { return (((n + n_split - 1) / n_split) + 15) & ~15; }
 struct RowsOf { int b, g, begin, end; int64_t part; int at, by; };      // (from row `at` on: the cache's row `by` further up)
 // Further arguments of the kernels: what else than all rows of a request they take or leave.
-template <typename... Own>
-constexpr int attn_waves() { return (std::is_same<Own, OwnRows>::value || ... || (sizeof...(Own) == 0)) ? 1 : 3; }
 struct WindowRows { int32_t window, n_sink; };        // the newest `window` rows of a request and its first n_sink
 struct ScoresTo { float* score; int64_t stride; };    // all rows, whose scores go to score [B, Hq, stride] (no grouping: in powers of two)
+// Waves a SIMD that the compiler has to leave room for.  Only windows of four heads over 16-bit rows need more registers than three leave, and spill 1 to 6
+// of them outside the loop: shorter walks gain, longer ones lose.  us, three / as many registers as it takes: 32 requests, window 512 20.8 / 22.2, 4096
+// 94.4 / 92.4, 64 requests 178 / 172, one, 4096 13.4 / 13.4.  With scores 6 to 43 would be spilled, up to ten of them in every turn of the loop: 16 requests of
+// 2000 to 32768 rows, slabs 320 / 256, pages 279 / 265; 16 of 4096 rows, slabs 69.5 / 51.0, pages 57.7 / 56.2 (of 300 to 4096, pages 42.8 / 46.2).
+template <typename... Own>
+constexpr int attn_waves() { return (std::is_same<Own, WindowRows>::value || ...) ? 3 : 1; }
 // The rows of a window in order: the first `at` of the cache, then those from `at + by` on, `count` in all.
 __device__ __forceinline__ void window_rows(const WindowRows& w, int n, int* at, int* by, int* count) {
   const int lo = n > w.window ? n - w.window : 0;

@@ -4,8 +4,8 @@
 //   mass[b, g, j] = (j < held_b ? decay * mass[b, g, j] : 0) + sum_{h in g} softmax_j(q[b, h] . K[b, g, j] / sqrt(D))
 //
 // so that K and V are read once.  The scores are 4 G bytes a row on the way out and back beside 4 D of K and V in 16 bits.  Bound by the bytes: 16
-// requests of 2000 to 32768 rows, bf16 pages, 1.21 GB 250 to 265 us by the card, 4.6 to 4.9 TB/s, where the attention alone takes 200 (with a wave a head
-// and two passes over K 2411).  The scores' stores are 23 of the difference, V's rows behind the last one 12, this kernel 13; stores of four
+// requests of 2000 to 32768 rows, bf16 pages, 1.21 GB 258 us, 4.7 TB/s, where the attention alone takes 200 (with a wave a head and two passes over K
+// 2411, with registers for three waves a SIMD 266: attn_waves).  The scores' stores are 23 of the difference, V's rows behind the last one 12, this kernel 13; stores of four
 // tiles at a time through LDS, scores with the heads side by side, stores past the caches and rows of zeros for those behind the last one
 // were no faster.
 #include "full_attn.h"

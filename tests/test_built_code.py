@@ -68,3 +68,11 @@ def test_the_barriers_of_the_batch_kernels_are_common_to_all_waves(device_object
     assert len(kernels) >= 36
     for name, text in kernels.items():
         assert 3 <= len(re.findall(r"\bs_barrier\b", text)) <= 4, name
+
+
+def test_steps_that_leave_scores_keep_their_registers(device_objects):
+    """None is put into memory and fetched back in the loop over the rows."""
+    kernels = {name: text for name, text in _disassembly(device_objects, "k_full_attn").items() if "ScoresTo" in name}
+    assert len(kernels) >= 24
+    for name, text in kernels.items():
+        assert not re.search(r"\bscratch_(load|store)", text), name
