@@ -324,7 +324,8 @@ int lfps_rotate_append(lfps_ctx* ctx, const lfps_rotary* rot, const void* q, con
                        void* stream);
 
 /* lfps_prompt_attn and lfps_full_attn_decode over a sliding window and the first rows: the token at row p sees the rows j <= p with
- * j > p - window (window >= 1: its own row is the last of them) or j < n_sink.  Arguments else as there; out must not overlap q. */
+ * j > p - window (window >= 1: its own row is the last of them) or j < n_sink.  Arguments and roundings else as there (lfps_window_attn of 16-bit types:
+ * weights of 16 bits for the product with V, bf16 over FP8 caches; the decode form fp32 throughout); out must not overlap q. */
 int lfps_window_attn(lfps_ctx* ctx, const void* q, int64_t stride_t, const int32_t* cu, int32_t n_tokens, const lfps_kv* kv, int32_t window,
                      int32_t n_sink, void* out, void* stream);
 int lfps_window_attn_decode(lfps_ctx* ctx, const float* q, const lfps_kv* kv, int32_t window, int32_t n_sink, float* out, void* stream);

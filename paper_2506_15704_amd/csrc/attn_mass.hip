@@ -196,7 +196,8 @@ __global__ __launch_bounds__(kMassThreads, sizeof(TK) == 4 ? 1 : 2) void k_mass_
     const int stages = (hi - lo + M::kStage - 1) / M::kStage;
     auto slot = [&](int j) { return lds + (j & (kMassRing - 1)) * M::kBytes; };
     auto row_of = [&](int j) { return lo + j * M::kStage; };
-    // stage j, whose places have been looked up; then the look-up of the next one comes first, so that waiting for it is no wait for the rows
+    // stage j, whose places have been looked up; then the look-up of the next one comes first: waiting for it need be no wait for the rows (the compiler,
+    // which does not know here whether there are pages, makes it one for all requests)
     auto ask = [&](int j) {
       at.aim(K, row_of(j), hi, lane);
       __builtin_amdgcn_sched_barrier(0);
@@ -430,7 +431,8 @@ __global__ __launch_bounds__(kMassThreads, sizeof(TK) == 4 ? 1 : 2) void k_mass_
     answered_but<0>();
     __syncthreads();
     const int subs = (rows - m0 + 31) / 32;
-    auto turn = [&](int i) __attribute__((always_inline)) {      // as in k_mass_stats; of stage j - 1 the statistics have been read too
+    // as in k_mass_stats; of stage j - 1 the statistics have been read too.  (The compiler puts a wait for all requests in front of most of these barriers.)
+    auto turn = [&](int i) __attribute__((always_inline)) {
       if ((i + 1) % M::kSubs != 0 || i + 1 >= subs) return;
       const int j = (i + 1) / M::kSubs;
       if (j + 2 < stages) answered_but<2 * kRequests>();
